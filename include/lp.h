@@ -305,6 +305,47 @@ lp_status lp_sgd_update(struct lp_net* net, void* stream, int aux, uint32_t mask
 lp_status lp_net_set_fused_update(struct lp_net* net, int on, float lr, float momentum, float weight_decay,
                                   float* const* velocity, float* const* master);
 
+/* Softmax cross-entropy of a linear classifier over many classes.  The logits l = x w^T + b [rows, classes] are formed a tile
+ * or a piece at a time and never handed out: beside the head of the last module (lp_module_forward, lp_local_loss_grad, which
+ * keep them) this is the loss of a classifier whose classes are too many for that, or of one that stands at every position of
+ * a module's output, y[k] read as [N*H*W, C] (the local classifiers of layer-wise greedy training; dfeatures is then a
+ * terminal adjoint dy[k] for lp_module_backward).
+ *     lse_n = log sum_v exp(l_nv),  row_loss_n = lse_n - l_n,label(n),  loss = sum row_loss / max(1, number of rows that count)
+ * A row counts when its label is in [0, classes); any other label (-1, say) leaves it out: row_loss 0, gradient 0, and
+ * nothing of what its features hold reaches a sum (its lse is still written).  A class is switched off by a bias of minus infinity.
+ * Sums, statistics, loss and the gradients of weight and bias are fp32.  LP_BF16: features, weight and dfeatures are
+ * bf16, the probabilities are held as a sum of two bf16 for dweight and as one for dfeatures.  LP_F32: all fp32, products from
+ * operands split into three bf16.  Results do not depend on the order in which workgroups run: the same bits on every call. */
+typedef struct {
+    int rows;              /* >= 0 */
+    int channels;          /* 1 .. 65536 */
+    int classes;           /* 1 .. 2^24 */
+    int dtype;             /* lp_dtype of features, weight and dfeatures */
+    int64_t ld_features;   /* elements from a row to the next; 0: channels */
+    int64_t ld_weight;
+    int64_t ld_dfeatures;
+} lp_linear_ce_desc;
+
+/* Device memory that a call needs besides its operands (backward = 0: lp_linear_ce_forward, 1: lp_linear_ce_backward).  Host
+ * only.  Errors: LP_ERR_INVALID_ARG, LP_ERR_SHAPE, LP_ERR_DTYPE. */
+lp_status lp_linear_ce_workspace_bytes(const lp_linear_ce_desc* d, int backward, size_t* bytes);
+
+/* features [rows, channels], weight [classes, channels], bias [classes] fp32 or NULL, labels int32 [rows]; loss: one float;
+ * row_loss [rows] or NULL; lse [rows].  features and weight 16-byte aligned.  workspace: 256-byte aligned, lent until
+ * the work has run; it holds nothing between calls, and calls that may overlap in time need one each (graphs captured
+ * over one workspace must not be replayed at the same time).  The work runs on the device that is current at the call, which
+ * has to be the one of `stream` and of the tensors.  Errors: LP_ERR_INVALID_ARG, LP_ERR_SHAPE, LP_ERR_DTYPE, LP_ERR_WORKSPACE,
+ * LP_ERR_HIP. */
+lp_status lp_linear_ce_forward(const lp_linear_ce_desc* d, void* stream, const void* features, const void* weight, const float* bias,
+                               const int32_t* labels, float* loss, float* row_loss, float* lse, void* workspace, size_t workspace_bytes);
+
+/* Gradients of loss_scale * loss, from lse as lp_linear_ce_forward wrote it for the same operands.  dfeatures [rows, channels]
+ * in the storage type, dweight [classes, channels] fp32 without gaps, dbias [classes] fp32: each may be NULL; overwritten.
+ * dweight 16-byte aligned; features and weight must not be among the outputs.  Otherwise as lp_linear_ce_forward. */
+lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const void* features, const void* weight, const float* bias,
+                                const int32_t* labels, const float* lse, float loss_scale, void* dfeatures, float* dweight,
+                                float* dbias, void* workspace, size_t workspace_bytes);
+
 /* Correction of the auxiliary variables that follows the adjoint recursion in Sec. 4.1 (the update of lambda_k,
  * 1 <= k <= K-1): one gradient step of the relaxed objective with respect to x_k,
  *     x[k] <- x[k] - eta * ( scale*(rho*(x[k] - y_prev[k-1]) - lam_prev[k-1]) + dx[k] ),

@@ -17,6 +17,7 @@
 
 #include "../../include/lp.h"
 #include "lp_addr.h"
+#include "lp_classes.h"
 #include "lp_kernels.h"
 #include "lp_wgsplit.h"
 
@@ -3172,6 +3173,283 @@ lp_status lp_sgd_update(struct lp_net* net, void* stream, int aux, uint32_t mask
         if (err != hipSuccess) return fail(LP_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(err));
     }
     return LP_OK;
+}
+
+// ----------------------------------------------------------------------------------------------------
+// Cross-entropy of a linear classifier over many classes (kernels: lp_classes.hip)
+// ----------------------------------------------------------------------------------------------------
+namespace {
+
+// How a product of I x J outputs over K (pairs of planes included) is cut into workgroups.
+struct TilePlan { int cfg, ti, tj, slices, kchunk; };
+
+static int div_up(int a, int b) { return (a + b - 1) / b; }
+
+static TilePlan tile_plan(int cfg, int I, int J, int K, int slices) {
+    int bi, bj, wi, wj;
+    ce_tile_size(cfg, &bi, &bj, &wi, &wj);
+    TilePlan t;
+    t.cfg = cfg; t.ti = div_up(I, bi); t.tj = div_up(J, bj);
+    t.kchunk = div_up(div_up(K, 64), std::max(1, slices)) * 64;
+    t.slices = std::max(1, div_up(K, t.kchunk));
+    return t;
+}
+// Largest tile that still gives the chip's 256 compute units something to do.
+static int tile_cfg(int I, int J, bool big) {
+    const long t256 = (long)div_up(I, 256) * div_up(J, 256), t128 = (long)div_up(I, 128) * div_up(J, 128);
+    if (J <= 32) return 3;
+    if (big && t256 >= 192) return 0;
+    return t128 >= 256 ? 1 : 2;
+}
+// A gradient product: cut along the reduction where its tiles are few, in pieces of at least four k-tiles.
+static TilePlan grad_plan(int I, int J, int K, int pairs, bool few_cols, bool may_cut) {
+    int cfg = tile_cfg(I, J, true);
+    if (cfg == 3 && !few_cols) cfg = 2;
+    TilePlan t = tile_plan(cfg, I, J, K, 1);
+    const int want = cfg == 2 || cfg == 3 ? 768 : 512, tiles = t.ti * t.tj;
+    if (may_cut && tiles * 2 <= want) t = tile_plan(cfg, I, J, K, std::max(1, std::min(want / tiles, div_up(K, 64) * pairs / 4)));
+    return t;
+}
+
+struct CePlan {
+    int N, C, V, K, nplanes, nprob;          // K: channels rounded up to eight; planes of the operands, of the probabilities
+    bool pack_x, pack_w, cut;                // cut: partial logits instead of tiles that finish their rows
+    long ldx, ldw, lddx;
+    GemmPairs logits, dx, dw;
+    TilePlan tl, tx, tw;
+    int piece, pieces, ldv;                  // classes of a piece of the probabilities
+    size_t o_x, o_w, o_partial, o_slices, o_bsum, o_bcnt, o_ticket, o_mask, o_count, o_prob, o_dx, o_dw, o_colsum, bytes;
+    int parts, colparts;
+};
+
+constexpr size_t kProbBytes = (size_t)512 << 20;
+
+static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
+    if (!d) return fail(LP_ERR_INVALID_ARG, "descriptor is NULL");
+    if (d->dtype != LP_F32 && d->dtype != LP_BF16) return fail(LP_ERR_DTYPE, "dtype %d is neither LP_F32 nor LP_BF16", d->dtype);
+    if (d->rows < 0 || d->channels < 1 || d->classes < 1) return fail(LP_ERR_INVALID_ARG, "rows %d, channels %d, classes %d", d->rows, d->channels, d->classes);
+    if (d->rows > (1 << 26) || d->channels > 65536 || d->classes > (1 << 24))
+        return fail(LP_ERR_SHAPE, "rows %d, channels %d, classes %d: at most 2^26, 65536 and 2^24", d->rows, d->channels, d->classes);
+    p.N = d->rows; p.C = d->channels; p.V = d->classes; p.K = (p.C + 7) & ~7;
+    p.ldx = d->ld_features ? d->ld_features : p.C; p.ldw = d->ld_weight ? d->ld_weight : p.C; p.lddx = d->ld_dfeatures ? d->ld_dfeatures : p.C;
+    for (const long ld : {p.ldx, p.ldw, p.lddx})
+        if (ld < p.C || ld > (1l << 40)) return fail(LP_ERR_SHAPE, "a row stride of %ld for %d channels", ld, p.C);
+    const bool low = d->dtype == LP_BF16;
+    p.nplanes = low ? 1 : 3; p.nprob = low ? 2 : 3;
+    // bf16 rows of whole 16-byte vectors are read where they are (the strides of a tile's rows within 32 bits)
+    auto direct = [&](long ld) { return low && p.C % 8 == 0 && ld % 8 == 0 && ld <= (1l << 20); };
+    p.pack_x = !direct(p.ldx); p.pack_w = !direct(p.ldw);
+    const GemmPairs one{1, 0, 0}, six{6, 0x201100, 0x021010};
+    p.logits = low ? one : six; p.dx = p.logits; p.dw = low ? GemmPairs{2, 0, 0x10} : six;
+
+    int cfg = tile_cfg(p.V, p.N, true);
+    if (cfg == 0 && !low && backward) cfg = 1;                   // three planes of a 256 x 256 tile do not fit into LDS
+    p.tl = tile_plan(cfg, p.V, std::max(1, p.N), p.K, 1);
+    if ((long)p.tl.ti * p.tl.tj > (1l << 30)) return fail(LP_ERR_SHAPE, "%d rows x %d classes in one call", p.N, p.V);
+    const int tiles = p.tl.ti * p.tl.tj;
+    p.cut = cfg >= 2 && tiles < 128;
+    if (p.cut) p.tl = tile_plan(cfg, p.V, std::max(1, p.N), p.K, std::max(1, std::min(512 / tiles, div_up(p.K, 64) * p.logits.n / 4)));
+    int bi, bj, wi, wj;
+    ce_tile_size(p.tl.cfg, &bi, &bj, &wi, &wj);
+    p.parts = p.tl.ti * wi;
+    p.colparts = p.tl.tj * wj;
+    const size_t N = p.N, V8 = (p.V + 7) & ~7;
+    p.pieces = 1; p.piece = p.V; p.ldv = (int)V8;
+    // (the rows of a tile within 32 bits: at most 2^20 classes a piece)
+    if (backward && !p.cut && ((size_t)p.nprob * 2 * N * V8 > kProbBytes || p.V > (1 << 20))) {
+        p.piece = (int)std::min<size_t>(1 << 20, std::max<size_t>(256, kProbBytes / (p.nprob * 2 * std::max<size_t>(N, 1)) / 256 * 256));
+        p.pieces = div_up(p.V, p.piece);
+        p.piece = std::min(p.V, div_up(div_up(p.V, p.pieces), 256) * 256);
+        p.pieces = div_up(p.V, p.piece);
+        p.ldv = (p.piece + 7) & ~7;
+    }
+    WsAlloc ws;
+    const size_t plane_rows = (size_t)p.nplanes * 2 * p.K;
+    p.o_x = p.pack_x ? ws.take(plane_rows * N) : 0;
+    p.o_w = p.pack_w ? ws.take(plane_rows * p.V) : 0;
+    p.o_slices = p.cut ? ws.take((size_t)p.tl.slices * N * V8 * 4) : 0;
+    if (!backward) {
+        p.o_partial = p.cut ? 0 : ws.take(N * p.parts * sizeof(float2));
+        p.o_bsum = ws.take((N + 3) / 4 * 4);
+        p.o_bcnt = ws.take((N + 3) / 4 * 4);
+        p.o_ticket = ws.take(4);
+    } else {
+        p.tx = grad_plan(p.C, std::max(1, p.N), p.piece, p.dx.n, true, true);
+        p.tw = grad_plan(p.C, p.piece, std::max(1, p.N), p.dw.n, false, p.pieces == 1);
+        p.o_mask = ws.take((N + 63) / 64 * 8);
+        p.o_count = ws.take(4);
+        p.o_prob = ws.take((size_t)p.nprob * 2 * N * p.ldv);
+        p.o_dx = ws.take((size_t)p.tx.slices * N * p.K * 4);
+        p.o_dw = p.tw.slices > 1 ? ws.take((size_t)p.tw.slices * p.V * p.K * 4) : 0;
+        p.o_colsum = p.cut ? 0 : ws.take((size_t)p.colparts * p.ldv * 4);
+    }
+    p.bytes = std::max<size_t>(ws.off, 256);
+    return LP_OK;
+}
+
+static lp_status hip_status(hipError_t err) {
+    return err == hipSuccess ? LP_OK : fail(LP_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(err));
+}
+
+// operands of the products: where they lie, or laid out in the workspace
+static lp_status ce_operands(const CePlan& p, int dtype, const void* x, const void* w, char* ws, GemmOperand& X, GemmOperand& W, hipStream_t s) {
+    X.extent = p.N; W.extent = p.V;
+    X.plane = (size_t)p.N * p.K * 2; W.plane = (size_t)p.V * p.K * 2;
+    hipError_t err = hipSuccess;
+    if (p.pack_x) {
+        X.base = ws + p.o_x; X.ld = p.K;
+        err = launch_ce_pack(x, p.ldx, p.N, p.C, dtype, ws + p.o_x, X.plane, p.K, s);
+    } else { X.base = (const char*)x; X.ld = (int)p.ldx; }
+    if (p.pack_w) {
+        W.base = ws + p.o_w; W.ld = p.K;
+        if (err == hipSuccess) err = launch_ce_pack(w, p.ldw, p.V, p.C, dtype, ws + p.o_w, W.plane, p.K, s);
+    } else { W.base = (const char*)w; W.ld = (int)p.ldw; }
+    return hip_status(err);
+}
+
+static lp_status ce_check(const CePlan& p, const void* x, const void* w, const int32_t* labels, const void* ws, size_t ws_bytes) {
+    if (!w || (p.N > 0 && (!x || !labels))) return fail(LP_ERR_INVALID_ARG, "features, weight or labels is NULL");
+    if (misaligned(x) || misaligned(w)) return fail(LP_ERR_INVALID_ARG, "features or weight is not 16-byte aligned");
+    if (!ws || ws_bytes < p.bytes) return fail(LP_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : (size_t)0, p.bytes);
+    if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(LP_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+    return LP_OK;
+}
+
+static CeLogits ce_logits(const CePlan& p, const GemmOperand& X, const GemmOperand& W, const float* bias, int v0, int V) {
+    CeLogits a;
+    memset(&a, 0, sizeof(a));
+    a.x = X; a.w = W;
+    a.w.base += (size_t)v0 * W.ld * 2; a.w.extent = V;
+    a.pairs = p.logits; a.K = p.K; a.kchunk = p.tl.kchunk;
+    a.V = V; a.N = p.N; a.v0 = v0; a.V_all = p.V;
+    int bi, bj, wi, wj;
+    ce_tile_size(p.tl.cfg, &bi, &bj, &wi, &wj);
+    a.tiles_i = div_up(V, bi); a.tiles_j = p.tl.tj; a.band = 8;
+    a.bias = bias ? bias + v0 : nullptr;
+    return a;
+}
+
+}  // namespace
+
+lp_status lp_linear_ce_workspace_bytes(const lp_linear_ce_desc* d, int backward, size_t* bytes) {
+    if (!bytes) return fail(LP_ERR_INVALID_ARG, "bytes is NULL");
+    CePlan p;
+    const lp_status st = ce_plan(d, backward != 0, p);
+    if (st == LP_OK) *bytes = p.bytes;
+    return st;
+}
+
+lp_status lp_linear_ce_forward(const lp_linear_ce_desc* d, void* stream, const void* features, const void* weight, const float* bias,
+                               const int32_t* labels, float* loss, float* row_loss, float* lse, void* workspace, size_t workspace_bytes) {
+    CePlan p;
+    lp_status st = ce_plan(d, false, p);
+    if (st == LP_OK) st = ce_check(p, features, weight, labels, workspace, workspace_bytes);
+    if (st != LP_OK) return st;
+    if (!loss || (p.N > 0 && !lse)) return fail(LP_ERR_INVALID_ARG, "loss or lse is NULL");
+    hipStream_t s = (hipStream_t)stream;
+    char* const ws = (char*)workspace;
+    if (p.N == 0) return hip_status(launch_ce_zero(loss, 1, s));
+    GemmOperand X, W;
+    if ((st = ce_operands(p, d->dtype, features, weight, ws, X, W, s)) != LP_OK) return st;
+    CeLogits a = ce_logits(p, X, W, bias, 0, p.V);
+    a.ticket = (int*)(ws + p.o_ticket);
+    CeRows r;
+    memset(&r, 0, sizeof(r));
+    if (p.cut) {
+        a.slices = (float*)(ws + p.o_slices); a.ldv = (p.V + 7) & ~7; a.slice = (size_t)p.N * a.ldv;
+        r.slices = a.slices; r.slice = a.slice; r.nslices = p.tl.slices; r.ldv = a.ldv;
+        st = hip_status(launch_ce_slices(a, p.tl.slices, p.tl.cfg, s));
+    } else {
+        a.partial = (float2*)(ws + p.o_partial); a.parts = p.parts;
+        r.partial = a.partial; r.parts = p.parts;
+        st = hip_status(launch_ce_stats(a, p.tl.cfg, s));
+    }
+    if (st != LP_OK) return st;
+    r.N = p.N; r.V = p.V; r.K = p.K; r.labels = labels; r.bias = bias; r.w = W; r.x = X; r.pairs = p.logits;
+    r.lse = lse; r.row_loss = row_loss; r.loss = loss;
+    r.bsum = (float*)(ws + p.o_bsum); r.bcnt = (int*)(ws + p.o_bcnt); r.ticket = (int*)(ws + p.o_ticket);
+    return hip_status(launch_ce_rows(r, s));
+}
+
+lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const void* features, const void* weight, const float* bias,
+                                const int32_t* labels, const float* lse, float loss_scale, void* dfeatures, float* dweight,
+                                float* dbias, void* workspace, size_t workspace_bytes) {
+    CePlan p;
+    lp_status st = ce_plan(d, true, p);
+    if (st == LP_OK) st = ce_check(p, features, weight, labels, workspace, workspace_bytes);
+    if (st != LP_OK) return st;
+    if (p.N > 0 && !lse) return fail(LP_ERR_INVALID_ARG, "lse is NULL");
+    if (misaligned(dweight)) return fail(LP_ERR_INVALID_ARG, "dweight is not 16-byte aligned");
+    hipStream_t s = (hipStream_t)stream;
+    char* const ws = (char*)workspace;
+    if (p.N == 0) {
+        if (dweight) st = hip_status(launch_ce_zero(dweight, (size_t)p.V * p.C, s));
+        if (st == LP_OK && dbias) st = hip_status(launch_ce_zero(dbias, p.V, s));
+        return st;
+    }
+    if (!dfeatures && !dweight && !dbias) return LP_OK;
+    GemmOperand X, W;
+    if ((st = ce_operands(p, d->dtype, features, weight, ws, X, W, s)) != LP_OK) return st;
+    unsigned long long* const mask = (unsigned long long*)(ws + p.o_mask);
+    int* const count = (int*)(ws + p.o_count);
+    if ((st = hip_status(launch_ce_labels(labels, p.N, p.V, mask, count, s))) != LP_OK) return st;
+    char* const prob = ws + p.o_prob;
+    const size_t pplane = (size_t)p.N * p.ldv * 2;
+    GemmOperand P{prob, pplane, p.ldv, 0};
+    CeFinish f;
+    memset(&f, 0, sizeof(f));
+    auto blocks = [](size_t rows, int cols) { return (int)std::min<size_t>((rows * ((cols + 3) / 4) + 255) / 256, 4096); };
+    f.labels = labels; f.count = count; f.scale = loss_scale; f.N = p.N; f.V_all = p.V;
+    f.colsum = p.cut ? nullptr : (float*)(ws + p.o_colsum); f.parts = p.colparts; f.ld_colsum = p.ldv;
+    f.prob = (const unsigned short*)prob; f.pplane = pplane; f.nplanes = p.nprob; f.ldv = p.ldv;
+    for (int v0 = 0, piece = 0; piece < p.pieces; ++piece, v0 += p.piece) {
+        const int V = std::min(p.piece, p.V - v0);
+        CeLogits a = ce_logits(p, X, W, bias, v0, V);
+        a.lse = lse; a.labels = labels; a.prob = prob; a.pplane = pplane; a.ldv = p.ldv;
+        if (p.cut) {
+            a.slices = (float*)(ws + p.o_slices); a.slice = (size_t)p.N * a.ldv;
+            CeRows r;
+            memset(&r, 0, sizeof(r));
+            r.N = p.N; r.V = p.V; r.labels = labels; r.bias = bias; r.slices = a.slices; r.slice = a.slice; r.nslices = p.tl.slices; r.ldv = a.ldv;
+            r.lse = const_cast<float*>(lse);
+            st = hip_status(launch_ce_slices(a, p.tl.slices, p.tl.cfg, s));
+            if (st == LP_OK) st = hip_status(launch_ce_prob(r, (unsigned short*)prob, pplane, p.nprob, s));
+        } else {
+            a.colsum = dbias ? (float*)(ws + p.o_colsum) : nullptr; a.ld_colsum = p.ldv;
+            st = hip_status(launch_ce_prob_tiles(a, p.nprob, p.tl.cfg, s));
+        }
+        if (st != LP_OK) return st;
+        CeGrad g;
+        if (dweight) {
+            memset(&g, 0, sizeof(g));
+            const TilePlan t = p.tw;
+            int bi, bj, wi, wj;
+            ce_tile_size(t.cfg, &bi, &bj, &wi, &wj);
+            g.a = X; g.a.extent = p.K; g.b = P; g.b.extent = p.ldv; g.pairs = p.dw;
+            g.K = p.N; g.kchunk = t.kchunk; g.J = V;
+            g.tiles_i = t.ti; g.tiles_j = div_up(V, bj); g.band = 8; g.mask = mask;
+            if (t.slices > 1) { g.out = (float*)(ws + p.o_dw); g.slice = (size_t)p.V * p.K; g.ldo = p.K; g.I = p.K; g.vec = 1; }
+            else { g.out = dweight + (size_t)v0 * p.C; g.ldo = p.C; g.I = p.C; g.vec = p.C % 4 == 0; g.count = count; g.scale = loss_scale; }
+            if ((st = hip_status(launch_ce_dw(g, t.slices, t.cfg, s))) != LP_OK) return st;
+        }
+        if (dfeatures) {
+            memset(&g, 0, sizeof(g));
+            const TilePlan t = p.tx;
+            g.a = W; g.a.base += (size_t)v0 * W.ld * 2; g.a.extent = p.K; g.b = P; g.b.extent = p.N; g.pairs = p.dx;
+            g.K = V; g.kchunk = div_up(div_up(V, 64), t.slices) * 64; g.I = p.K; g.J = p.N;
+            g.tiles_i = t.ti; g.tiles_j = t.tj; g.band = 8;
+            g.out = (float*)(ws + p.o_dx); g.slice = (size_t)p.N * p.K; g.ldo = p.K; g.vec = 1; g.add = piece > 0;
+            if ((st = hip_status(launch_ce_dx(g, t.slices, t.cfg, s))) != LP_OK) return st;
+        }
+        // the bias of this piece: with the last one beside the other sums
+        f.blocks_b = dbias ? div_up(V, 64) : 0; f.V = V; f.dbias = dbias ? dbias + v0 : nullptr;
+        if (piece + 1 < p.pieces && (st = hip_status(launch_ce_finish(f, d->dtype, s))) != LP_OK) return st;
+    }
+    f.x = CeSum{(float*)(ws + p.o_dx), (size_t)p.N * p.K, p.tx.slices, p.K, dfeatures, (size_t)p.lddx, p.N, p.C};
+    f.w = CeSum{(float*)(ws + p.o_dw), (size_t)p.V * p.K, p.tw.slices, p.K, dweight, (size_t)p.C, p.V, p.C};
+    f.blocks_x = dfeatures ? blocks(p.N, p.C) : 0;
+    f.blocks_w = dweight && p.tw.slices > 1 ? blocks(p.V, p.C) : 0;
+    return hip_status(launch_ce_finish(f, d->dtype, s));
 }
 
 lp_status lp_aux_variable_update(struct lp_net* net, void* stream, void* const* x, const void* const* y_prev,

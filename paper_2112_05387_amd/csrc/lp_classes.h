@@ -1,0 +1,71 @@
+// Launch descriptors of the linear classifier's cross-entropy (lp_classes.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "lp_gemm.h"
+
+namespace lp {
+
+// l = X W^T over one piece of the classes (rows i: classes v0 .. v0 + V - 1, columns j: samples)
+struct CeLogits {
+    GemmOperand w, x;
+    GemmPairs pairs;
+    int K, kchunk;                      // channels, and how many of them a slice has
+    int V, N, v0, V_all;
+    int tiles_i, tiles_j, band;
+    const float* bias;                  // of the piece, or null
+    int* ticket;                        // set to zero for the kernel behind this one, or null
+    float2* partial; int parts;         // statistics: [N][parts] (maximum, sum), base 2
+    float* slices; size_t slice;        // partial logits: [slices][N][ldv]
+    int ldv;                            // row length of slices / prob, a multiple of 8
+    const float* lse; const int* labels;
+    char* prob; size_t pplane;          // probabilities: planes of bf16 [N][ldv]
+    float* colsum; int ld_colsum;       // their sums over the samples of every wave's tile, or null
+};
+struct CeRows {
+    int N, V, K;
+    const int* labels;
+    const float* bias;
+    const float2* partial; int parts;
+    const float* slices; size_t slice; int nslices, ldv;
+    GemmOperand w, x; GemmPairs pairs;
+    float *lse, *row_loss, *loss;
+    float* bsum; int* bcnt; int* ticket;
+};
+// out[j][i] (+)= sum_k a[k][i] * b[..]; i channels, j samples or classes
+struct CeGrad {
+    GemmOperand a, b;
+    GemmPairs pairs;
+    int K, kchunk, I, J;
+    int tiles_i, tiles_j, band;
+    float* out; size_t slice; int ldo;
+    int vec, add;                       // 16-byte stores (I a multiple of four then); add to what is there
+    const int* count; float scale;      // scaled by scale / count, or not
+    const unsigned long long* mask;
+};
+struct CeSum { const float* part; size_t slice; int nslices, ldp; void* out; size_t ldo; int rows, cols; };
+struct CeFinish {
+    CeSum x, w;
+    int blocks_x, blocks_w, blocks_b;
+    const int* labels; const int* count; float scale;
+    int N, V, V_all;                    // V: classes of the bias here
+    const float* colsum; int parts, ld_colsum;
+    const unsigned short* prob; size_t pplane; int nplanes, ldv;
+    float* dbias;
+};
+
+// tiles: 0 256 x 256, 1 128 x 128, 2 64 x 64, 3 128 x 32 (few samples); waves along either side
+void ce_tile_size(int cfg, int* bi, int* bj, int* wi, int* wj);
+hipError_t launch_ce_pack(const void* src, long ld_src, int rows, int cols, int dtype, void* dst, size_t plane, int ld, hipStream_t s);
+hipError_t launch_ce_labels(const int* labels, int N, int V, unsigned long long* mask, int* count, hipStream_t s);
+hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s);
+hipError_t launch_ce_prob_tiles(const CeLogits& a, int planes, int cfg, hipStream_t s);
+hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t s);
+hipError_t launch_ce_rows(const CeRows& a, hipStream_t s);
+hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int planes, hipStream_t s);
+hipError_t launch_ce_dx(const CeGrad& a, int slices, int cfg, hipStream_t s);
+hipError_t launch_ce_dw(const CeGrad& a, int slices, int cfg, hipStream_t s);
+hipError_t launch_ce_finish(const CeFinish& a, int dtype, hipStream_t s);
+hipError_t launch_ce_zero(float* p, size_t n, hipStream_t s);
+
+}  // namespace lp

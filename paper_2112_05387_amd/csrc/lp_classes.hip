@@ -1,0 +1,583 @@
+// Softmax cross-entropy of a linear classifier over many classes (gfx950), logits never handed out:
+//
+//   l_nv = sum_c x_nc w_vc + b_v,   lse_n = log sum_v exp l_nv,   loss_n = lse_n - l_n,y(n)
+//   d_nv = (exp(l_nv - lse_n) - [v = y(n)]) / count,   dX = d W,   dW = d^T X,   db_v = sum_n d_nv
+//
+// Four products, each on the matrix cores with what follows it as its epilogue.  Forward: l = X W^T, of which a workgroup keeps the
+// maximum and the sum of exponentials of its classes for every row (the statistics of all tiles are joined by a small kernel that
+// also takes the label's own logit, a dot product).  Backward: the same product once more, whose epilogue turns a tile into
+// probabilities; they go to memory, piece of the classes by piece, and are read from there by the two gradient products.  Keeping
+// the logits would save one product of four and cost 4 bytes a logit.
+//
+// Precision.  bf16: products of bf16 are exact, sums are fp32.  The probabilities are kept as two bf16 (16 bits) for dW, which is
+// fp32, and dX, which is bf16, reads the first of them: its own rounding is as large.  p - 1 of the label is formed in
+// fp32 before it is split, so a small p beside it is kept by the second part.
+// fp32: every operand as three bf16 (24 bits), six of the nine products (the others are below 2^-25): six products at the rate of
+// the 16-bit instruction take less than half of the time of one in fp32.
+//
+// Rows whose label is no class (ignored): probability zero in the epilogue by selection, and their features count as zero in
+// dW whatever they hold (a bit a row, read by the loads): no infinity or NaN in them reaches a sum.
+//
+// Few tiles (small mini-batches, few classes) are cut along the reduction, partial results in fp32, and joined by the kernel
+// that needs all of a row anyway (softmax) or by the one that rounds (gradients); no atomics, the order of every sum is fixed.
+#include "lp_classes.h"
+
+#include <algorithm>
+
+#include "lp_gemm.h"
+#include "lp_kernels.h"
+
+namespace lp {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kInf = __builtin_inff();
+
+__device__ __forceinline__ float bf16_up(unsigned bits) { return __uint_as_float(bits << 16); }
+// nearest bf16 of a finite value stays finite: the last step up to infinity would leave a rest that is none
+__device__ __forceinline__ unsigned bf16_part(float x) {
+    const unsigned b = float_to_bf16_bits(x);
+    return (b & 0x7fffu) == 0x7f80u && (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u ? __float_as_uint(x) >> 16 : b;
+}
+// x as a sum of NP bf16; infinities and NaN in the first alone
+template <int NP> __device__ __forceinline__ void split_bf16(float x, unsigned (&b)[NP]) {
+    b[0] = bf16_part(x);
+    const bool fin = (b[0] & 0x7f80u) != 0x7f80u;
+#pragma unroll
+    for (int p = 1; p < NP; ++p) {
+        x -= bf16_up(b[p - 1]);
+        b[p] = fin ? float_to_bf16_bits(x) : 0u;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// Operands in the form the products want: rows of ld elements (a multiple of 8, zeros behind the last), NP planes
+// ---------------------------------------------------------------------------------------------------------------------------------
+template <class T, int NP> __global__ __launch_bounds__(256) void ce_pack_kernel(const T* __restrict__ src, long ld_src, int rows, int cols, unsigned short* __restrict__ dst,
+                                                                                 size_t plane, int ld) {
+    const int cpr = ld >> 3;                                      // chunks of eight elements in a row
+    const size_t n = (size_t)rows * cpr;
+    for (size_t t = (size_t)blockIdx.x * 256 + threadIdx.x; t < n; t += (size_t)gridDim.x * 256) {
+        const int r = (int)(t / cpr), c = (int)(t - (size_t)r * cpr) * 8;
+        const T* s = src + (size_t)r * ld_src + c;
+        unsigned short out[NP][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (sizeof(T) == 2) out[0][e] = c + e < cols ? reinterpret_cast<const unsigned short*>(s)[e] : 0;
+            else {
+                unsigned b[NP];
+                split_bf16<NP>(c + e < cols ? to_float(s[e]) : 0.f, b);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) out[p][e] = (unsigned short)b[p];
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            u32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = out[p][2 * e] | ((unsigned)out[p][2 * e + 1] << 16);
+            *reinterpret_cast<u32x4*>(dst + p * plane + (size_t)r * ld + c) = v;
+        }
+    }
+}
+
+__device__ __forceinline__ bool is_class(int y, int V) { return (unsigned)y < (unsigned)V; }
+
+// bit n & 63 of word n >> 6: row n counts; and how many do.  One workgroup.
+__global__ __launch_bounds__(1024) void ce_labels_kernel(const int* __restrict__ labels, int N, int V, unsigned long long* __restrict__ mask, int* __restrict__ count) {
+    __shared__ int s[16];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int c = 0;
+    for (int n0 = wave * 64; n0 < N; n0 += 1024) {
+        const int n = n0 + lane;
+        const unsigned long long m = __ballot(n < N && is_class(labels[n < N ? n : 0], V));
+        c += __popcll(m);
+        if (lane == 0) mask[n0 >> 6] = m;
+    }
+    if (lane == 0) s[wave] = c;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int t = 0;
+        for (int i = 0; i < 16; ++i) t += s[i];
+        *count = t;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// l = X W^T: rows i are classes, columns j are samples, so that a lane has four consecutive classes of one sample and the
+// statistics of a sample are sums inside a lane and over two lanes
+// ---------------------------------------------------------------------------------------------------------------------------------
+enum LogitsMode { LM_STATS, LM_PROB, LM_SLICE };
+
+template <class T, int MODE, int NP, int WAVES> __global__ __launch_bounds__(T::NT, WAVES) void ce_logits_kernel(const CeLogits a) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0 && a.ticket) *a.ticket = 0;
+    int ti, tj;
+    gemm_tile_of(blockIdx.x, a.tiles_i * a.tiles_j, a.tiles_i, a.tiles_j, a.band, ti, tj);
+    const int i0 = ti * T::BI, j0 = tj * T::BJ;
+    typename T::Acc acc;
+#pragma unroll
+    for (int i = 0; i < T::TI / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < T::TJ / 32; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    const int kb = blockIdx.y * a.kchunk;
+    T::run(a.w, a.x, a.pairs, i0, j0, kb, min(a.K, kb + a.kchunk), (GemmMask)nullptr, smem, acc);
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wi = wave / (T::BJ / T::TJ), wj = wave % (T::BJ / T::TJ);
+    const int lr = lane & 31, h = lane >> 5;
+    const int ib = i0 + wi * T::TI, jb = j0 + wj * T::TJ;      // first class of the piece, first sample of this wave
+    constexpr int FI = T::TI / 32, FJ = T::TJ / 32;
+
+    if constexpr (MODE == LM_SLICE) {
+        float* const out = a.slices + (size_t)blockIdx.y * a.slice;
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) {
+            const int n = jb + j * 32 + lr;
+            if (n >= a.N) continue;
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int v = ib + i * 32 + 8 * q + 4 * h;
+                    if (v < a.ldv) *reinterpret_cast<f32x4*>(out + (size_t)n * a.ldv + v) = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                }
+        }
+        return;
+    }
+    // to base 2, with the bias; classes beyond the last: minus infinity
+    const bool ragged = i0 + T::BI > a.V;
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int v = ib + i * 32 + T::row(r, lane);
+            const float b = a.bias ? a.bias[min(v, a.V - 1)] * kLog2e : 0.f;
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) {
+                acc[i][j][r] = fmaf(acc[i][j][r], kLog2e, b);
+                if (ragged && v >= a.V) acc[i][j][r] = -kInf;
+            }
+        }
+    if constexpr (MODE == LM_STATS) {
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) {
+            float m = -kInf;
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) m = fmaxf(m, acc[i][j][r]);
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const float m0 = m == -kInf ? 0.f : m;              // nothing but minus infinity: a sum of zero
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r & 3] += __builtin_amdgcn_exp2f(acc[i][j][r] - m0);
+            float t = (s[0] + s[1]) + (s[2] + s[3]);
+            t += __shfl_xor(t, 32);
+            const int n = jb + j * 32 + lr;
+            if (h == 0 && n < a.N) a.partial[(size_t)n * a.parts + ti * (T::BI / T::TI) + wi] = make_float2(m, t);
+        }
+    } else {
+        // probabilities: 32 samples of the wave at a time through LDS, from where they go out as 16-byte pieces of rows
+        constexpr int PITCH = T::TI * 2 + 16, EP = 32 * PITCH, CPR = T::TI / 8, RPL = 64 / CPR;
+        unsigned char* const E0 = smem + wave * (NP * EP);
+        const int c = lane % CPR, jr = lane / CPR;
+        float cs[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) cs[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) {
+            const int n = jb + j * 32 + lr;
+            const int y = n < a.N ? a.labels[n] : -1;
+            const bool valid = is_class(y, a.V_all);
+            const float shift = n < a.N ? a.lse[n] * kLog2e : 0.f;
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float p[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[e] = valid ? __builtin_amdgcn_exp2f(acc[i][j][4 * q + e] - shift) : 0.f;
+                    unsigned char* const d = E0 + lr * PITCH + (i * 32 + 8 * q + 4 * h) * 2;
+#pragma unroll
+                    for (int k = 0; k < NP; ++k) {
+                        const unsigned lo = pack_bf16x2(p[0], p[1]), hi = pack_bf16x2(p[2], p[3]);
+                        *reinterpret_cast<u32x2*>(d + k * EP) = u32x2{lo, hi};
+                        p[0] -= __uint_as_float(lo << 16); p[1] -= __uint_as_float(lo & 0xffff0000u);
+                        p[2] -= __uint_as_float(hi << 16); p[3] -= __uint_as_float(hi & 0xffff0000u);
+                    }
+                }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            const int at = y - a.v0 - ib;                        // the label's class, where it is one of this wave's
+            if (h == 0 && valid && (unsigned)at < (unsigned)T::TI) {
+                unsigned short* const d = reinterpret_cast<unsigned short*>(E0 + lr * PITCH + at * 2);
+                float p = 0.f;
+#pragma unroll
+                for (int k = NP - 1; k >= 0; --k) p += bf16_up(d[k * (EP / 2)]);
+                unsigned b[NP];
+                split_bf16<NP>(p - 1.f, b);
+#pragma unroll
+                for (int k = 0; k < NP; ++k) d[k * (EP / 2)] = (unsigned short)b[k];
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            const int v = ib + c * 8;
+#pragma unroll
+            for (int t = 0; t < 32 / RPL; ++t) {
+                const int row = t * RPL + jr, no = jb + j * 32 + row;
+#pragma unroll
+                for (int k = 0; k < NP; ++k) {
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(E0 + k * EP + row * PITCH + c * 16);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        cs[2 * e] += __uint_as_float(w[e] << 16);
+                        cs[2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
+                    }
+                    if (no < a.N && v < a.ldv) *reinterpret_cast<u32x4*>(a.prob + k * a.pplane + ((size_t)no * a.ldv + v) * 2) = w;
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            __builtin_amdgcn_s_waitcnt(0xc07f);                  // read before the next 32 samples overwrite it
+        }
+        if (a.colsum) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int o = CPR; o < 64; o <<= 1) cs[e] += __shfl_xor(cs[e], o);
+            const int v = ib + c * 8;
+            if (jr == 0 && v < a.ld_colsum) {
+                float* const d = a.colsum + (size_t)(tj * (T::BJ / T::TJ) + wj) * a.ld_colsum + v;
+                *reinterpret_cast<f32x4*>(d) = f32x4{cs[0], cs[1], cs[2], cs[3]};
+                *reinterpret_cast<f32x4*>(d + 4) = f32x4{cs[4], cs[5], cs[6], cs[7]};
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// The end of the forward pass: a wave a row.  (m, s) of the tiles (or the partial logits themselves) to lse, the label's logit, the
+// row's loss; the last workgroup to arrive adds up what all of them left, in the order of the rows.
+// ---------------------------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
+    const float t = fmaxf(m, m2), t0 = t == -kInf ? 0.f : t;
+    s = s * __builtin_amdgcn_exp2f(m - t0) + s2 * __builtin_amdgcn_exp2f(m2 - t0);
+    m = t;
+}
+
+template <bool SLICES> __global__ __launch_bounds__(256) void ce_rows_kernel(const CeRows a) {
+    __shared__ float s_loss[4];
+    __shared__ int s_cnt[4];
+    __shared__ int s_last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.x * 4 + wave;
+    float loss = 0.f;
+    int counts = 0;
+    if (n < a.N) {
+        const int y = a.labels[n];
+        const bool valid = is_class(y, a.V);
+        float m = -kInf, s = 0.f, own = 0.f;
+        if constexpr (SLICES) {
+            const float* const row = a.slices + (size_t)n * a.ldv;
+            for (int v = lane; v < a.V; v += 64) {
+                float l = row[v];
+                for (int k = 1; k < a.nslices; ++k) l += row[k * a.slice + v];
+                if (a.bias) l += a.bias[v];
+                if (v == y) own = l;
+                join(m, s, l * kLog2e, 1.f);
+            }
+        } else {
+            const float2* const row = a.partial + (size_t)n * a.parts;
+            for (int t = lane; t < a.parts; t += 64) { const float2 v = row[t]; join(m, s, v.x, v.y); }
+            if (valid)
+                for (int p = 0; p < a.pairs.n; ++p) {
+                    const unsigned short* const x = reinterpret_cast<const unsigned short*>(a.x.base + ((a.pairs.b >> (4 * p)) & 15) * a.x.plane) + (size_t)n * a.x.ld;
+                    const unsigned short* const w = reinterpret_cast<const unsigned short*>(a.w.base + ((a.pairs.a >> (4 * p)) & 15) * a.w.plane) + (size_t)y * a.w.ld;
+                    for (int c = lane * 8; c < a.K; c += 512) {
+                        const u32x4 xv = *reinterpret_cast<const u32x4*>(x + c), wv = *reinterpret_cast<const u32x4*>(w + c);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            own = fmaf(__uint_as_float(xv[e] << 16), __uint_as_float(wv[e] << 16), own);
+                            own = fmaf(__uint_as_float(xv[e] & 0xffff0000u), __uint_as_float(wv[e] & 0xffff0000u), own);
+                        }
+                    }
+                }
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o);
+            join(m, s, m2, s2);
+            own += __shfl_xor(own, o);
+        }
+        const float lse = (m + __builtin_amdgcn_logf(s)) * kLn2;       // log2
+        if (!SLICES && valid && a.bias) own += a.bias[y];
+        loss = valid ? lse - own : 0.f;
+        counts = valid ? 1 : 0;
+        if (lane == 0) {
+            a.lse[n] = lse;
+            if (a.row_loss) a.row_loss[n] = loss;
+        }
+    }
+    if (lane == 0) { s_loss[wave] = loss; s_cnt[wave] = counts; }
+    __syncthreads();
+    if (tid == 0) {
+        // device scope: the sums are read by a workgroup of another XCD
+        __hip_atomic_store(a.bsum + blockIdx.x, (s_loss[0] + s_loss[1]) + (s_loss[2] + s_loss[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(a.bcnt + blockIdx.x, s_cnt[0] + s_cnt[1] + s_cnt[2] + s_cnt[3], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_last = __hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    double t = 0.0;
+    int c = 0;
+    for (int b = tid; b < (int)gridDim.x; b += 256) {
+        t += __hip_atomic_load(a.bsum + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        c += __hip_atomic_load(a.bcnt + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __shared__ double s_t[4];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { t += __shfl_xor(t, o); c += __shfl_xor(c, o); }
+    if (lane == 0) { s_t[wave] = t; s_cnt[wave] = c; }
+    __syncthreads();
+    if (tid == 0) {
+        const int all = s_cnt[0] + s_cnt[1] + s_cnt[2] + s_cnt[3];
+        *a.loss = (float)(((s_t[0] + s_t[1]) + (s_t[2] + s_t[3])) / (double)(all > 1 ? all : 1));
+    }
+}
+
+// Probabilities from partial logits (few tiles): a workgroup a row
+template <int NP> __global__ __launch_bounds__(256) void ce_prob_kernel(const CeRows a, unsigned short* __restrict__ prob, size_t pplane) {
+    const int n = blockIdx.x, y = a.labels[n];
+    const bool valid = is_class(y, a.V);
+    const float shift = a.lse[n] * kLog2e;
+    const float* const row = a.slices + (size_t)n * a.ldv;
+    for (int v = threadIdx.x * 2; v < a.ldv; v += 512) {
+        unsigned b[2][NP];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float p = 0.f;
+            if (valid && v + e < a.V) {
+                float l = row[v + e];
+                for (int k = 1; k < a.nslices; ++k) l += row[k * a.slice + v + e];
+                if (a.bias) l += a.bias[v + e];
+                p = __builtin_amdgcn_exp2f(fmaf(l, kLog2e, -shift));
+                if (v + e == y) p -= 1.f;
+            }
+            split_bf16<NP>(p, b[e]);
+        }
+#pragma unroll
+        for (int k = 0; k < NP; ++k) *reinterpret_cast<unsigned*>(prob + k * (pplane / 2) + (size_t)n * a.ldv + v) = b[0][k] | (b[1][k] << 16);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// The two gradient products: rows i are channels, columns j are samples (dX) or classes (dW)
+// ---------------------------------------------------------------------------------------------------------------------------------
+template <class T, int WAVES> __global__ __launch_bounds__(T::NT, WAVES) void ce_grad_kernel(const CeGrad a) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    int ti, tj;
+    gemm_tile_of(blockIdx.x, a.tiles_i * a.tiles_j, a.tiles_i, a.tiles_j, a.band, ti, tj);
+    const int i0 = ti * T::BI, j0 = tj * T::BJ;
+    typename T::Acc acc;
+#pragma unroll
+    for (int i = 0; i < T::TI / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < T::TJ / 32; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    const int kb = blockIdx.y * a.kchunk;
+    T::run(a.a, a.b, a.pairs, i0, j0, kb, min(a.K, kb + a.kchunk), (GemmMask)a.mask, smem, acc);
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wi = wave / (T::BJ / T::TJ), wj = wave % (T::BJ / T::TJ);
+    const int lr = lane & 31, h = lane >> 5;
+    const float g = a.count ? a.scale / (float)max(*a.count, 1) : 1.f;
+    float* const out = a.out + (size_t)blockIdx.y * a.slice;
+#pragma unroll
+    for (int j = 0; j < T::TJ / 32; ++j) {
+        const int col = j0 + wj * T::TJ + j * 32 + lr;
+        if (col >= a.J) continue;
+#pragma unroll
+        for (int i = 0; i < T::TI / 32; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = i0 + wi * T::TI + i * 32 + 8 * q + 4 * h;
+                float* const d = out + (size_t)col * a.ldo + c;
+                f32x4 v = {acc[i][j][4 * q] * g, acc[i][j][4 * q + 1] * g, acc[i][j][4 * q + 2] * g, acc[i][j][4 * q + 3] * g};
+                if (a.vec) {
+                    if (c < a.I) {
+                        if (a.add) v += *reinterpret_cast<const f32x4*>(d);
+                        *reinterpret_cast<f32x4*>(d) = v;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (c + e < a.I) d[e] = v[e];
+                }
+            }
+    }
+}
+
+// Sums of the partial results, scaled, rounded to the type of the gradient; rows without a class are zero.  And the bias.
+template <class T> __global__ __launch_bounds__(256) void ce_finish_kernel(const CeFinish a) {
+    const float g = a.scale / (float)max(*a.count, 1);
+    const int b = blockIdx.x;
+    if (b < a.blocks_x + a.blocks_w) {
+        const bool x = b < a.blocks_x;
+        const CeSum& s = x ? a.x : a.w;
+        const size_t t0 = (size_t)(x ? b : b - a.blocks_x) * 256 + threadIdx.x;
+        const int vpr = (s.cols + 3) >> 2;
+        const size_t n = (size_t)s.rows * vpr, stride = (size_t)(x ? a.blocks_x : a.blocks_w) * 256;
+        for (size_t t = t0; t < n; t += stride) {
+            const int r = (int)(t / vpr), c = (int)(t - (size_t)r * vpr) * 4;
+            const float* const p = s.part + (size_t)r * s.ldp + c;
+            f32x4 v = *reinterpret_cast<const f32x4*>(p);
+            for (int k = 1; k < s.nslices; ++k) v += *reinterpret_cast<const f32x4*>(p + k * s.slice);
+            const bool live = !x || is_class(a.labels[r], a.V_all);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = live ? v[e] * g : 0.f;
+            if (x) {
+                T* const d = reinterpret_cast<T*>(s.out) + (size_t)r * s.ldo + c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < s.cols) d[e] = from_float<T>(v[e]);
+            } else {
+                float* const d = reinterpret_cast<float*>(s.out) + (size_t)r * s.ldo + c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < s.cols) d[e] = v[e];
+            }
+        }
+        return;
+    }
+    // bias: 64 classes a workgroup, its four waves a quarter of the parts each
+    __shared__ float s_b[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, v = (b - a.blocks_x - a.blocks_w) * 64 + lane;
+    float t = 0.f;
+    if (v < a.V) {
+        if (a.colsum) {
+            for (int k = wave; k < a.parts; k += 4) t += a.colsum[(size_t)k * a.ld_colsum + v];
+        } else {
+            for (int n = wave; n < a.N; n += 4)
+                for (int p = 0; p < a.nplanes; ++p) t += bf16_up(a.prob[p * (a.pplane / 2) + (size_t)n * a.ldv + v]);
+        }
+    }
+    s_b[wave][lane] = t;
+    __syncthreads();
+    if (wave == 0 && v < a.V) a.dbias[v] = ((s_b[0][lane] + s_b[1][lane]) + (s_b[2][lane] + s_b[3][lane])) * g;
+}
+
+__global__ __launch_bounds__(256) void ce_zero_kernel(float* p, size_t n) {
+    for (size_t t = (size_t)blockIdx.x * 256 + threadIdx.x; t < n; t += (size_t)gridDim.x * 256) p[t] = 0.f;
+}
+
+// tiles: big (one workgroup a compute unit), middle (two), small (many), few samples
+template <bool AKR, bool BKR, bool M> using TBig = GemmTile<bf16_t, AKR, BKR, 2, 4, 4, 2, 2, M>;
+template <bool AKR, bool BKR, bool M> using TMid = GemmTile<bf16_t, AKR, BKR, 2, 2, 2, 2, 2, M>;
+template <bool AKR, bool BKR, bool M> using TSmall = GemmTile<bf16_t, AKR, BKR, 2, 2, 1, 1, 4, M>;
+template <bool AKR, bool BKR, bool M> using TFew = GemmTile<bf16_t, AKR, BKR, 4, 1, 1, 1, 3, M>;
+
+template <class K, class A> hipError_t launch(K kernel, OncePerDevice& once, dim3 grid, int threads, int lds, hipStream_t s, const A& args) {
+    if (const hipError_t e = raise_lds_limit(once, {(const void*)kernel}, lds); e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, args);
+    return hipGetLastError();
+}
+
+template <class T, int MODE, int NP, int WAVES> hipError_t launch_logits_t(const CeLogits& a, int slices, hipStream_t s) {
+    static OncePerDevice once;
+    constexpr int EP = MODE == LM_PROB ? T::NW * NP * 32 * (T::TI * 2 + 16) : 0;
+    return launch(ce_logits_kernel<T, MODE, NP, WAVES>, once, dim3(a.tiles_i * a.tiles_j, slices), T::NT, std::max(T::LDS, EP), s, a);
+}
+template <class T, int WAVES> hipError_t launch_grad_t(const CeGrad& a, int slices, hipStream_t s) {
+    static OncePerDevice once;
+    return launch(ce_grad_kernel<T, WAVES>, once, dim3(a.tiles_i * a.tiles_j, slices), T::NT, T::LDS, s, a);
+}
+
+}  // namespace
+
+void ce_tile_size(int cfg, int* bi, int* bj, int* wi, int* wj) {
+    static const int d[4][4] = {{256, 256, 2, 4}, {128, 128, 2, 2}, {64, 64, 2, 2}, {128, 32, 4, 1}};
+    *bi = d[cfg][0]; *bj = d[cfg][1]; *wi = d[cfg][2]; *wj = d[cfg][3];
+}
+
+hipError_t launch_ce_pack(const void* src, long ld_src, int rows, int cols, int dtype, void* dst, size_t plane, int ld, hipStream_t s) {
+    const size_t n = (size_t)rows * (ld >> 3);
+    if (n == 0) return hipSuccess;
+    const dim3 grid((unsigned)std::min<size_t>((n + 255) / 256, 1u << 16));
+    if (dtype == 1) hipLaunchKernelGGL((ce_pack_kernel<bf16_t, 1>), grid, dim3(256), 0, s, (const bf16_t*)src, ld_src, rows, cols, (unsigned short*)dst, plane / 2, ld);
+    else hipLaunchKernelGGL((ce_pack_kernel<float, 3>), grid, dim3(256), 0, s, (const float*)src, ld_src, rows, cols, (unsigned short*)dst, plane / 2, ld);
+    return hipGetLastError();
+}
+hipError_t launch_ce_labels(const int* labels, int N, int V, unsigned long long* mask, int* count, hipStream_t s) {
+    hipLaunchKernelGGL(ce_labels_kernel, dim3(1), dim3(1024), 0, s, labels, N, V, mask, count);
+    return hipGetLastError();
+}
+hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s) {
+    switch (cfg) {
+        case 0: return launch_logits_t<TBig<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
+        case 1: return launch_logits_t<TMid<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
+        case 2: return launch_logits_t<TSmall<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
+        default: return launch_logits_t<TFew<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
+    }
+}
+hipError_t launch_ce_prob_tiles(const CeLogits& a, int planes, int cfg, hipStream_t s) {
+    if (planes == 2) switch (cfg) {
+        case 0: return launch_logits_t<TBig<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
+        case 1: return launch_logits_t<TMid<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
+        case 2: return launch_logits_t<TSmall<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
+        default: return launch_logits_t<TFew<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
+    }
+    switch (cfg) {
+        case 1: return launch_logits_t<TMid<false, false, false>, LM_PROB, 3, 2>(a, 1, s);
+        case 2: return launch_logits_t<TSmall<false, false, false>, LM_PROB, 3, 2>(a, 1, s);
+        default: return launch_logits_t<TFew<false, false, false>, LM_PROB, 3, 2>(a, 1, s);
+    }
+}
+hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t s) {
+    if (cfg == 2) return launch_logits_t<TSmall<false, false, false>, LM_SLICE, 1, 2>(a, slices, s);
+    return launch_logits_t<TFew<false, false, false>, LM_SLICE, 1, 2>(a, slices, s);
+}
+hipError_t launch_ce_rows(const CeRows& a, hipStream_t s) {
+    const dim3 grid((a.N + 3) / 4);
+    if (a.slices) hipLaunchKernelGGL(ce_rows_kernel<true>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(ce_rows_kernel<false>, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int planes, hipStream_t s) {
+    if (planes == 2) hipLaunchKernelGGL(ce_prob_kernel<2>, dim3(a.N), dim3(256), 0, s, a, prob, pplane);
+    else hipLaunchKernelGGL(ce_prob_kernel<3>, dim3(a.N), dim3(256), 0, s, a, prob, pplane);
+    return hipGetLastError();
+}
+hipError_t launch_ce_dx(const CeGrad& a, int slices, int cfg, hipStream_t s) {
+    switch (cfg) {
+        case 0: return launch_grad_t<TBig<true, false, false>, 2>(a, slices, s);
+        case 1: return launch_grad_t<TMid<true, false, false>, 2>(a, slices, s);
+        case 2: return launch_grad_t<TSmall<true, false, false>, 2>(a, slices, s);
+        default: return launch_grad_t<TFew<true, false, false>, 2>(a, slices, s);
+    }
+}
+hipError_t launch_ce_dw(const CeGrad& a, int slices, int cfg, hipStream_t s) {
+    switch (cfg) {
+        case 0: return launch_grad_t<TBig<true, true, true>, 2>(a, slices, s);
+        case 1: return launch_grad_t<TMid<true, true, true>, 2>(a, slices, s);
+        default: return launch_grad_t<TSmall<true, true, true>, 2>(a, slices, s);
+    }
+}
+hipError_t launch_ce_finish(const CeFinish& a, int dtype, hipStream_t s) {
+    const int blocks = a.blocks_x + a.blocks_w + a.blocks_b;
+    if (blocks == 0) return hipSuccess;
+    if (dtype == 1) hipLaunchKernelGGL(ce_finish_kernel<bf16_t>, dim3(blocks), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(ce_finish_kernel<float>, dim3(blocks), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+hipError_t launch_ce_zero(float* p, size_t n, hipStream_t s) {
+    if (n == 0) return hipSuccess;
+    hipLaunchKernelGGL(ce_zero_kernel, dim3((unsigned)std::min<size_t>((n + 255) / 256, 4096)), dim3(256), 0, s, p, n);
+    return hipGetLastError();
+}
+
+}  // namespace lp

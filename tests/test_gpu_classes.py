@@ -1,0 +1,282 @@
+"""Cross-entropy of a linear classifier over many classes against its definition in 64 bits.
+
+Tolerances, element by element, from the magnitudes that a result is the sum of.  A sum of K products in fp32 on the matrix
+cores is off by a random walk of roundings and a drift (a matrix instruction cuts towards zero what lies below its
+largest addend), together at most (K / 16 + 4 sqrt(K) + 16) 2^-24 of the sum of the products' magnitudes at four standard
+deviations.  A probability takes over the errors of its logit and of its row's lse, and the rounding of its parts: bf16 2^-8 of
+itself in one part, 2^-16 in two; three parts 2^-24."""
+import math
+
+import pytest
+
+from tests.gpu_common import say
+
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24
+
+
+def _steps(k):
+    return (k / 16 + 4 * math.sqrt(k) + 16) * U32
+
+
+def _inputs(n, c, v, dtype, bias=True, ignored=0.0, seed=0, spread=6.0):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda")
+    w = r(v, c) / math.sqrt(c)
+    y = torch.randint(0, v, (n,), generator=g, device="cuda")
+    x = r(n, c) + spread * torch.rand((n, 1), generator=g, device="cuda") * w[y]
+    if ignored:
+        y = torch.where(torch.rand(n, generator=g, device="cuda") < ignored, -1, y)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    return x.to(t), w.to(t), (r(v) if bias else None), y.to(torch.int32)
+
+
+def _reference(x, w, b, y, scale=1.0):
+    """Results in 64 bits and how far an element may be off."""
+    import torch
+    low = x.dtype == torch.bfloat16
+    v, c = w.shape
+    n = x.shape[0]
+    valid = (y >= 0) & (y < v)
+    xd, wd = x.double(), w.double()
+    xk = torch.where(valid[:, None], xd, 0)
+    l = xd @ wd.t()
+    mag = xd.abs() @ wd.abs().t()
+    if b is not None:
+        l = l + b.double()
+        mag = mag + b.double().abs()
+    tl = _steps(c) * mag + 4 * U32 * l.abs()
+    lse = torch.logsumexp(l, 1)
+    tlse = tl.max(1).values + 8 * U32 * (lse.abs() + 1)
+    at = torch.where(valid, y, 0).long()[:, None]
+    own = l.gather(1, at)[:, 0]
+    rows = torch.where(valid, lse - own, 0)
+    trows = torch.where(valid, tlse + tl.gather(1, at)[:, 0] + 4 * U32 * (lse.abs() + own.abs()), 0)
+    count = max(1, int(valid.sum()))
+    out = {"loss": (rows.sum()[None] / count, trows.sum()[None] / count + 4 * U32 * rows.sum()[None] / count), "row_loss": (rows, trows), "lse": (lse, tlse)}
+    p = torch.exp(l - lse[:, None]) * valid[:, None]
+    tp = p * (tl + tlse[:, None] + 8 * U32 * (l.abs() + lse.abs()[:, None]))
+    d = p.scatter_add(1, at, -valid.double()[:, None])
+    g = abs(scale) / count
+    part = 2.0 ** -16 if low else 4 * U32
+    td = (tp + part * d.abs()) * valid[:, None]
+    out["dweight"] = (scale / count * (d.t() @ xk), g * (td.t() @ xk.abs() + 2 * _steps(n) * (d.abs().t() @ xk.abs())))
+    out["dbias"] = (scale / count * d.sum(0), g * (td.sum(0) + _steps(n) * d.abs().sum(0)))
+    dx = scale / count * (d @ wd)
+    if low:
+        td = td + 2.0 ** -8 * d.abs()
+    out["dfeatures"] = (dx, g * (td @ wd.abs() + 2 * _steps(v) * (d.abs() @ wd.abs())) + (2.0 ** -8 if low else 4 * U32) * dx.abs())
+    return out
+
+
+def _run(x, w, b, y, scale=1.0):
+    from paper_2112_05387_amd import ops
+    loss, row_loss, lse = ops.linear_ce_forward(x, w, y, bias=b)
+    dx, dw, db = ops.linear_ce_backward(x, w, y, lse, bias=b, scale=scale)
+    out = {"loss": loss, "row_loss": row_loss, "lse": lse, "dfeatures": dx, "dweight": dw}
+    if db is not None:
+        out["dbias"] = db
+    return out
+
+
+def _compare(got, want, what):
+    worst = {}
+    for k, t in got.items():
+        ref, tol = want[k]
+        assert t.shape == ref.shape, k
+        off = (t.double() - ref).abs()
+        assert bool(off.isfinite().all()), f"{what}: {k} is not finite"
+        # below the smallest numbers of the type nothing is held
+        worst[k] = float((off / (tol + 1e-37)).max()) if off.numel() else 0.0
+    say(f"{what}: largest share of the tolerance " + ", ".join(f"{k} {v:.2f}" for k, v in worst.items()))
+    assert all(v <= 1.0 for v in worst.values()), worst
+
+
+SHAPES = [
+    # rows, channels, classes: few tiles, cut along the channels
+    (1, 1, 1), (1, 16, 10), (4, 8, 2), (33, 17, 5), (65, 640, 100), (256, 16, 10), (130, 72, 257), (64, 2048, 1000), (5, 1000, 63),
+    # few rows and many classes; tiles of 64, 128, 256; ragged on every side
+    (1, 128, 20000), (31, 200, 17001), (300, 333, 3001), (1000, 64, 8200), (1025, 40, 17000), (2500, 96, 8195), (8192, 40, 90),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,v", SHAPES)
+def test_matches_the_definition(n, c, v, dtype):
+    x, w, b, y = _inputs(n, c, v, dtype, bias=(n + c) % 2 == 0, ignored=0.2 if n > 3 else 0.0, seed=n + c + v)
+    _compare(_run(x, w, b, y, scale=3.0), _reference(x, w, b, y, scale=3.0), f"{n} x {c} -> {v} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_pieces_of_the_classes(dtype):
+    """Probabilities of all classes would take more than the workspace holds at once: several pieces, the last one ragged."""
+    from paper_2112_05387_amd import binding as B
+    n, c, v = (4096, 32, 40003) if dtype == "bf16" else (4096, 16, 27003)
+    d = B.lp_linear_ce_desc(n, c, v, B.LP_BF16 if dtype == "bf16" else B.LP_F32, 0, 0, 0)
+    whole = (4 if dtype == "bf16" else 6) * n * v
+    assert B.lp_linear_ce_workspace_bytes(d, True) < whole + (32 << 20)
+    x, w, b, y = _inputs(n, c, v, dtype, ignored=0.1, seed=7)
+    _compare(_run(x, w, b, y), _reference(x, w, b, y), f"pieces {n} x {c} -> {v} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,v", [(40, 24, 70), (300, 64, 4000)])
+def test_row_strides_and_padding(n, c, v, dtype):
+    """Rows inside wider tensors, whose other columns hold NaN."""
+    import torch
+    x, w, b, y = _inputs(n, c, v, dtype, seed=3)
+    for pad in (8, 5):
+        xs, ws = (torch.full((t.shape[0], c + pad), float("nan"), dtype=t.dtype, device="cuda") for t in (x, w))
+        xs[:, :c], ws[:, :c] = x, w
+        _compare(_run(xs[:, :c], ws[:, :c], b, y), _reference(x, w, b, y), f"row stride {c + pad} {dtype}")
+    # other orders are copied
+    _compare(_run(x.t().contiguous().t(), w, b, y), _reference(x, w, b, y), "columns first")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,v", [(70, 32, 50), (600, 64, 9000)])
+def test_left_out_rows_may_hold_anything(n, c, v, dtype):
+    import torch
+    x, w, b, y = _inputs(n, c, v, dtype, seed=11)
+    y[1::7] = -1
+    y[2::7] = v                  # beyond the classes
+    y[3::7] = -2 ** 31
+    want = _reference(x, w, b, y)
+    bad = x.clone()
+    bad[1::7] = float("nan")
+    bad[2::7] = float("inf")
+    bad[3::7, 0] = float("-inf")
+    got = _run(bad, w, b, y)
+    keep = (y >= 0) & (y < v)
+    assert bool((got["dfeatures"][~keep] == 0).all()) and bool((got["row_loss"][~keep] == 0).all())
+    got["lse"] = torch.where(keep, got["lse"], want["lse"][0].float())
+    _compare(got, want, f"left-out rows {n} {dtype}")
+
+
+@pytest.mark.parametrize("n,v", [(9, 30), (500, 9000)])
+def test_no_row_counts(n, v):
+    import torch
+    x, w, b, y = _inputs(n, 16, v, "bf16", seed=1)
+    got = _run(x, w, b, torch.full_like(y, -1))
+    for k in ("loss", "row_loss", "dfeatures", "dweight", "dbias"):
+        assert bool((got[k] == 0).all()), k
+
+
+def test_no_rows():
+    import torch
+    x, w, b, y = _inputs(3, 16, 20, "f32")
+    got = _run(x[:0], w, b, y[:0])
+    assert got["lse"].shape == (0,) and got["dfeatures"].shape == (0, 16)
+    assert float(got["loss"]) == 0 and not bool(got["dweight"].any()) and not bool(got["dbias"].any())
+
+
+@pytest.mark.parametrize("n,v", [(12, 40), (300, 9000)])
+def test_classes_switched_off(n, v):
+    """A bias of minus infinity, or of the type's lowest value, takes a class out; a row whose own class is out has an infinite
+    (a very large) loss and the gradient of the rest."""
+    import torch
+    x, w, b, y = _inputs(n, 32, v, "f32", seed=5)
+    off = torch.zeros(v, dtype=torch.bool, device="cuda")
+    off[::3] = True
+    y = torch.where(off[y.long()], (y + 1) % v, y)
+    y = torch.where(off[y.long()], (y + 1) % v, y).to(torch.int32)
+    assert not bool(off[y.long()].any())
+    for low in (float("-inf"), torch.finfo(torch.float32).min):
+        bias = torch.where(off, low, b)
+        got = _run(x, w, bias, y)
+        keep = ~off
+        new = torch.cumsum(keep.long(), 0) - 1
+        part = _reference(x, w[keep], b[keep], new[y.long()].to(torch.int32))
+        assert not bool(got["dweight"][off].any()) and not bool(got["dbias"][off].any())
+        got["dweight"], got["dbias"] = got["dweight"][keep], got["dbias"][keep]
+        _compare(got, part, f"classes off, bias {low}")
+    y[0] = 0                       # off
+    got = _run(x, w, torch.where(off, float("-inf"), b), y)
+    assert float(got["row_loss"][0]) == float("inf") and float(got["loss"]) == float("inf")
+    assert bool(got["dfeatures"].isfinite().all()) and bool(got["row_loss"][1:].isfinite().all())
+    # every class off: the formula has no value, in that row alone there is none here (its bias is every row's, so all rows)
+    got = _run(x, w, torch.full_like(b, float("-inf")), y)
+    assert bool(got["lse"].eq(float("-inf")).all()) and bool(got["row_loss"].isnan().all())
+
+
+@pytest.mark.parametrize("n,c,v", [(64, 48, 300), (700, 64, 9000)])
+def test_not_a_number_stays_in_its_row(n, c, v):
+    import torch
+    x, w, b, y = _inputs(n, c, v, "bf16", seed=2)
+    x[5, 3] = float("nan")
+    x[6, 3] = float("inf")
+    got = _run(x, w, b, y)
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[5:7] = False
+    assert bool(got["lse"][rest].isfinite().all()) and bool(got["dfeatures"][rest].isfinite().all())
+    assert bool(got["lse"][5:7].isnan().all()) and bool(got["loss"].isnan().all())
+
+
+@pytest.mark.parametrize("dtype,n,c,v", [("f32", 64, 40, 200), ("bf16", 64, 40, 200), ("f32", 500, 64, 9000), ("bf16", 3000, 64, 9000)])
+def test_same_bits_again_and_on_another_stream(dtype, n, c, v):
+    import torch
+    x, w, b, y = _inputs(n, c, v, dtype, ignored=0.1, seed=9)
+    first = _run(x, w, b, y)
+    again = _run(x, w, b, y)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        other = _run(x, w, b, y)
+    torch.cuda.synchronize()
+    for k in first:
+        assert torch.equal(first[k], again[k]) and torch.equal(first[k], other[k]), k
+
+
+def test_in_a_graph():
+    """Captured once, replayed on new inputs with eager calls between the replays; two graphs, each with memory of its own."""
+    import torch
+    shapes = [("bf16", 600, 64, 9000), ("f32", 64, 40, 200)]
+    graphs = []
+    for dtype, n, c, v in shapes:
+        x, w, b, y = _inputs(n, c, v, dtype, ignored=0.1, seed=20)
+        _run(x, w, b, y)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = _run(x, w, b, y)
+        graphs.append((g, x, w, b, y, out, (dtype, n, c, v)))
+    for turn in range(3):
+        for g, x, w, b, y, out, (dtype, n, c, v) in graphs:
+            for t, s in zip((x, w, b, y), _inputs(n, c, v, dtype, ignored=0.1, seed=30 + turn)):
+                t.copy_(s)
+            g.replay()
+            eager = _run(x, w, b, y)
+            torch.cuda.synchronize()
+            for k in eager:
+                assert torch.equal(out[k], eager[k]), (turn, k)
+
+
+@pytest.mark.parametrize("n,c,v", [(30, 12, 40), (300, 32, 9000)])
+def test_gradient_against_differences(n, c, v):
+    """Central differences of the loss in a random direction.  The loss of about log v is rounded at 2^-23 of itself, more than ten
+    times over; the third derivative in a direction of unit entries is below the sum of |direction| cubed."""
+    import torch
+    from paper_2112_05387_amd import ops
+    x, w, b, y = _inputs(n, c, v, "f32", ignored=0.1, seed=4)
+    loss, _, lse = ops.linear_ce_forward(x, w, y, bias=b)
+    grads = ops.linear_ce_backward(x, w, y, lse, bias=b)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    for i, t in enumerate((x, w, b)):
+        d = torch.sign(torch.randn(t.shape, generator=gen, device="cuda")) / math.sqrt(t.shape[-1])
+        h = 2.0 ** -8
+        f = []
+        for s in (h, -h):
+            a = [x, w, b]
+            a[i] = t + s * d
+            f.append(float(ops.linear_ce_forward(a[0], a[1], y, bias=a[2])[0]))
+        slope = (f[0] - f[1]) / (2 * h)
+        want = float((grads[i].double() * d.double()).sum())
+        # logits move by at most |x||d| <= 3 sigma: third derivative of log sum exp <= 2 (2 * move)^3 / 6
+        move = 3.0 * (1.0 if i == 2 else float((x if i == 1 else w).float().norm(dim=1).mean()) / math.sqrt(c) * 1.5)
+        tol = h * h * (2 * move) ** 3 / 3 + 16 * 2 ** -23 * float(loss) / h
+        say(f"difference {slope:.6f}, gradient {want:.6f}, tolerance {tol:.6f}")
+        assert abs(slope - want) <= tol
