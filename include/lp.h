@@ -287,6 +287,54 @@ lp_status lp_sgd_update(struct lp_net* net, void* stream, int aux, uint32_t mask
                         const float* const* dparams, float* const* velocity, float* const* master, float lr,
                         float momentum, float weight_decay);
 
+/* Orthogonalised matrices: for every matrix U of the list, five (`steps`) Newton-Schulz products
+ *     X = U / max(|U|_F, 1e-7);   X <- a X + b (X X^T) X + c (X X^T)^2 X,   (a, b, c) = (3.4445, -4.7750, 2.0315)
+ * (X^T X for a tall matrix), which take every singular value s > 0 of U / |U|_F towards one (0.7 .. 1.2 after five steps from s
+ * > 0.01 or so) and leave the singular vectors.  Each U [rows, cols] in fp32 or bf16, any row stride; the result in either type;
+ * `out` may be `in` (with the same row stride and type).  Sizes may differ from matrix to matrix; rows or cols of 0 are passed
+ * over.  Products of operands held in two fp16 parts, sums in fp32, |U| in fp64; bit-identical from call to call. */
+typedef struct {
+    int rows, cols;              /* 0 .. 2^20; the shorter side at most 16384 */
+    int dtype_in, dtype_out;     /* lp_dtype */
+    const void* in;
+    void* out;
+    int64_t ld_in, ld_out;       /* elements from a row to the next; 0: cols */
+} lp_matrix;
+#define LP_ORTHO_MAX_STEPS 16
+#define LP_ORTHO_MAX_MATRICES 4096
+
+/* Workspace as in lp_linear_ce_forward: 256-byte aligned, one for calls that may overlap in time.  `mats` is read by the call
+ * itself.  The work runs on the current device.  Errors: LP_ERR_INVALID_ARG, LP_ERR_SHAPE, LP_ERR_DTYPE, LP_ERR_WORKSPACE,
+ * LP_ERR_HIP. */
+lp_status lp_orthogonalize_workspace_bytes(int n, const lp_matrix* mats, size_t* bytes);
+lp_status lp_orthogonalize(void* stream, int n, const lp_matrix* mats, int steps, void* workspace, size_t workspace_bytes);
+
+/* Parameter update by orthogonalised momentum.  For a tensor with `orthogonal` set, read as a matrix [rows, cols] (a filter
+ * [Cout][R][S][Cin] as Cout rows),
+ *     v <- momentum * v + g;   u = g + momentum * v (nesterov) or v;   O = u orthogonalised as above;
+ *     W <- (1 - lr * weight_decay) * W - lr * sqrt(max(1, rows / cols)) * O,
+ * for any other one the rule of lp_sgd_update with rest_lr (momentum and weight decay as for the others).
+ * velocity and master as in lp_sgd_update (velocity always required; master NULL: the stored parameters are read). */
+typedef struct { float lr, momentum, weight_decay, rest_lr; int nesterov, steps; } lp_muon_opts;
+typedef struct {
+    int rows, cols;              /* >= 1, as lp_matrix where orthogonal; rows * cols elements */
+    int dtype;                   /* lp_dtype of the parameter */
+    int orthogonal;
+    size_t offset;               /* byte offset in params, a multiple of the element size */
+    size_t grad_offset;          /* byte offset in grads, velocity and master, a multiple of 4 */
+} lp_muon_tensor;
+/* A packed set of tensors: params, grads, velocity and master 16-byte aligned.  No two tensors may share elements. */
+lp_status lp_muon_step_workspace_bytes(int n, const lp_muon_tensor* tensors, size_t* bytes);
+lp_status lp_muon_step(void* stream, int n, const lp_muon_tensor* tensors, void* params, const float* grads, float* velocity,
+                       float* master, const lp_muon_opts* opts, void* workspace, size_t workspace_bytes);
+/* The same for the modules (aux = 0) or AuxNets (aux = 1) that `mask` selects, arguments as lp_sgd_update's: every
+ * convolution filter is orthogonalised, batch-norm tensors and the head's bias are not, the head's weight where `head` is set.
+ * The workspace is not the net's (which keeps the activations). */
+lp_status lp_muon_workspace_bytes(const struct lp_net* net, int aux, uint32_t mask, int head, size_t* bytes);
+lp_status lp_muon_update(struct lp_net* net, void* stream, int aux, uint32_t mask, int head, void* const* params,
+                         const float* const* dparams, float* const* velocity, float* const* master, const lp_muon_opts* opts,
+                         void* workspace, size_t workspace_bytes);
+
 /* The same update INSIDE the backward pass (Sec. 4.1 states the update of W_{kn+m} right after the adjoint at that
  * layer, inside the backward loop of Algorithm 1, not as a pass of its own).  While switched on, lp_module_backward
  * and lp_local_step update params[k] of the selected modules in place (the const of their params argument

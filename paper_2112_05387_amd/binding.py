@@ -14,7 +14,7 @@ LP_T_CONV, LP_T_BN_GAMMA, LP_T_BN_BETA, LP_T_FC_W, LP_T_FC_B = 0, 1, 2, 3, 4
 
 EXPORTS = ["lp_net_create", "lp_net_destroy", "lp_net_param_bytes", "lp_net_num_tensors", "lp_net_tensor_info",
            "lp_net_workspace_bytes", "lp_net_set_workspace", "lp_auxnet_forward", "lp_auxnet_forward_static", "lp_module_forward",
-           "lp_local_loss_grad", "lp_module_backward", "lp_al_multiplier_update", "lp_aux_variable_update", "lp_auxnet_distill_grad", "lp_sgd_update", "lp_reauxnet_grad", "lp_linear_ce_workspace_bytes", "lp_linear_ce_forward", "lp_linear_ce_backward", "lp_net_set_stream_lanes", "lp_local_step", "lp_net_set_residual_output", "lp_net_set_deterministic",
+           "lp_local_loss_grad", "lp_module_backward", "lp_al_multiplier_update", "lp_aux_variable_update", "lp_auxnet_distill_grad", "lp_sgd_update", "lp_reauxnet_grad", "lp_linear_ce_workspace_bytes", "lp_linear_ce_forward", "lp_linear_ce_backward", "lp_orthogonalize_workspace_bytes", "lp_orthogonalize", "lp_muon_step_workspace_bytes", "lp_muon_step", "lp_muon_workspace_bytes", "lp_muon_update", "lp_net_set_stream_lanes", "lp_local_step", "lp_net_set_residual_output", "lp_net_set_deterministic",
            "lp_debug_im2col_offsets", "lp_debug_keep_gradients", "lp_debug_unit_count", "lp_debug_unit_info",
            "lp_debug_module_info", "lp_debug_filter_load_extent", "lp_debug_conv_geometry", "lp_debug_conv_offsets", "lp_debug_mfma_peak", "lp_debug_layer_kernels", "lp_debug_stream_lanes", "lp_debug_separate_passes", "lp_debug_linear_kernels",
            "lp_debug_saved_tensor", "lp_net_set_fused_update", "lp_profile_enable", "lp_profile_fetch", "lp_last_error", "lp_version"]
@@ -74,6 +74,22 @@ class lp_linear_ce_desc(ctypes.Structure):
                 ("ld_features", c_int64), ("ld_weight", c_int64), ("ld_dfeatures", c_int64)]
 
 
+LP_ORTHO_MAX_STEPS, LP_ORTHO_MAX_MATRICES = 16, 4096
+
+
+class lp_matrix(ctypes.Structure):
+    _fields_ = [("rows", c_int), ("cols", c_int), ("dtype_in", c_int), ("dtype_out", c_int), ("in_", c_void_p), ("out", c_void_p),
+                ("ld_in", c_int64), ("ld_out", c_int64)]
+
+
+class lp_muon_opts(ctypes.Structure):
+    _fields_ = [("lr", c_float), ("momentum", c_float), ("weight_decay", c_float), ("rest_lr", c_float), ("nesterov", c_int), ("steps", c_int)]
+
+
+class lp_muon_tensor(ctypes.Structure):
+    _fields_ = [("rows", c_int), ("cols", c_int), ("dtype", c_int), ("orthogonal", c_int), ("offset", c_size_t), ("grad_offset", c_size_t)]
+
+
 class lp_profile_rec(ctypes.Structure):
     _fields_ = [("kind", c_int), ("cfg", c_int), ("nprob", c_int), ("blocks", c_int), ("ms", c_float), ("flops", ctypes.c_double),
                 ("bytes", ctypes.c_double)]
@@ -123,6 +139,13 @@ def lib():
         L.lp_linear_ce_workspace_bytes.argtypes = [cep, c_int, POINTER(c_size_t)]
         L.lp_linear_ce_forward.argtypes = [cep] + [c_void_p] * 9 + [c_size_t]
         L.lp_linear_ce_backward.argtypes = [cep] + [c_void_p] * 6 + [c_float] + [c_void_p] * 4 + [c_size_t]
+        op = POINTER(lp_muon_opts)
+        L.lp_orthogonalize_workspace_bytes.argtypes = [c_int, POINTER(lp_matrix), POINTER(c_size_t)]
+        L.lp_orthogonalize.argtypes = [c_void_p, c_int, POINTER(lp_matrix), c_int, c_void_p, c_size_t]
+        L.lp_muon_step_workspace_bytes.argtypes = [c_int, POINTER(lp_muon_tensor), POINTER(c_size_t)]
+        L.lp_muon_step.argtypes = [c_void_p, c_int, POINTER(lp_muon_tensor)] + [c_void_p] * 4 + [op, c_void_p, c_size_t]
+        L.lp_muon_workspace_bytes.argtypes = [c_void_p, c_int, c_uint32, c_int, POINTER(c_size_t)]
+        L.lp_muon_update.argtypes = [c_void_p, c_void_p, c_int, c_uint32, c_int, vpp, vpp, vpp, vpp, op, c_void_p, c_size_t]
         L.lp_net_set_fused_update.argtypes = [c_void_p, c_int, c_float, c_float, c_float, vpp, vpp]
         L.lp_aux_variable_update.argtypes = [c_void_p, c_void_p, vpp, vpp, vpp, vpp, c_float, c_float, c_float]
         L.lp_debug_im2col_offsets.argtypes = [c_void_p] + [c_int] * 7 + [c_void_p, c_void_p, c_void_p, c_int]
@@ -310,6 +333,39 @@ def lp_linear_ce_forward(desc, stream, features, weight, bias, labels, loss, row
 def lp_linear_ce_backward(desc, stream, features, weight, bias, labels, lse, loss_scale, dfeatures, dweight, dbias, ws, ws_bytes):
     _check(lib().lp_linear_ce_backward(ctypes.byref(desc), stream, features, weight, bias, labels, lse, float(loss_scale), dfeatures,
                                        dweight, dbias, ws, ws_bytes))
+
+
+def lp_orthogonalize_workspace_bytes(mats):
+    """mats: a ctypes array of lp_matrix"""
+    b = c_size_t()
+    _check(lib().lp_orthogonalize_workspace_bytes(len(mats), mats, ctypes.byref(b)))
+    return b.value
+
+
+def lp_orthogonalize(stream, mats, steps, ws, ws_bytes):
+    _check(lib().lp_orthogonalize(stream, len(mats), mats, int(steps), ws, ws_bytes))
+
+
+def lp_muon_step_workspace_bytes(tensors):
+    """tensors: a ctypes array of lp_muon_tensor"""
+    b = c_size_t()
+    _check(lib().lp_muon_step_workspace_bytes(len(tensors), tensors, ctypes.byref(b)))
+    return b.value
+
+
+def lp_muon_step(stream, tensors, params, grads, velocity, master, opts, ws, ws_bytes):
+    _check(lib().lp_muon_step(stream, len(tensors), tensors, params, grads, velocity, master, ctypes.byref(opts), ws, ws_bytes))
+
+
+def lp_muon_workspace_bytes(net, aux, mask, head):
+    b = c_size_t()
+    _check(lib().lp_muon_workspace_bytes(net, int(aux), mask, int(head), ctypes.byref(b)))
+    return b.value
+
+
+def lp_muon_update(net, stream, aux, mask, head, params, dparams, velocity, master, opts, ws, ws_bytes):
+    _check(lib().lp_muon_update(net, stream, int(aux), mask, int(head), _ptr_array(params), _ptr_array(dparams), _ptr_array(velocity),
+                                None if master is None else _ptr_array(master), ctypes.byref(opts), ws, ws_bytes))
 
 
 def lp_net_set_fused_update(net, on, lr=0.0, momentum=0.0, weight_decay=0.0, velocity=None, master=None):

@@ -12,6 +12,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -19,6 +20,7 @@
 #include "lp_addr.h"
 #include "lp_classes.h"
 #include "lp_kernels.h"
+#include "lp_ortho.h"
 #include "lp_wgsplit.h"
 
 using namespace lp;
@@ -2569,6 +2571,14 @@ static std::vector<int> lanes_of(const lp_net* net, uint32_t module_mask, bool w
         if ((module_mask >> k) & 1u) out.push_back(k < (int)net->lane.size() ? net->lane[k] : 0);
     return out;
 }
+// host memory for the lists is all that can run out here
+template <class F> static lp_status guarded(F f) {
+    try {
+        return f();
+    } catch (const std::bad_alloc&) {
+        return fail(LP_ERR_INVALID_ARG, "out of host memory");
+    }
+}
 static bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
 }  // namespace
@@ -3450,6 +3460,274 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
     f.blocks_x = dfeatures ? blocks(p.N, p.C) : 0;
     f.blocks_w = dweight && p.tw.slices > 1 ? blocks(p.V, p.C) : 0;
     return hip_status(launch_ce_finish(f, d->dtype, s));
+}
+
+// ----------------------------------------------------------------------------------------------------
+// Orthogonalised matrices and the update by them (kernels: lp_ortho.hip)
+// ----------------------------------------------------------------------------------------------------
+namespace {
+
+struct OrthoPlan {
+    std::vector<NsProb> p;
+    std::vector<int> start[4];               // blocks of the launches: elements, pieces, tiles of r x r, of r x c
+    int cfg_sq = 2, cfg_step = 2;
+    size_t o_table = 0, o_norm = 0, bytes = 256;
+    size_t table_words() const { return 4 * (p.size() + 1) + (4 * (p.size() + 1)) % 2 + p.size() * sizeof(NsProb) / 4; }
+    size_t probs_word() const { return 4 * (p.size() + 1) + (4 * (p.size() + 1)) % 2; }
+};
+static_assert(sizeof(NsProb) % 8 == 0, "the table is copied as words, its pointers aligned to eight bytes");
+
+static lp_status ortho_shape(long rows, long cols) {
+    if (rows < 0 || cols < 0 || rows > (1 << 20) || cols > (1 << 20) || std::min(rows, cols) > 16384)
+        return fail(LP_ERR_SHAPE, "a matrix of %ld x %ld: at most 2^20, the shorter side at most 16384", rows, cols);
+    return LP_OK;
+}
+
+// Sizes, launches and workspace from the tensors' shapes alone (rows, cols, plain)
+static lp_status ortho_plan(OrthoPlan& o) {
+    const int n = (int)o.p.size();
+    WsAlloc ws;
+    o.o_table = ws.take(o.table_words() * 4);
+    // the largest tile that leaves every compute unit one
+    long sq[3] = {0, 0, 0}, up[3] = {0, 0, 0};
+    for (int c = 0; c < 3; ++c) {
+        int b;
+        ns_tile_size(c, &b);
+        for (const NsProb& q : o.p)
+            if (!q.plain) {
+                const long r = (std::min(q.rows, q.cols) + b - 1) / b, l = (std::max(q.rows, q.cols) + b - 1) / b;
+                sq[c] += r * r; up[c] += r * l;
+            }
+    }
+    auto pick = [](const long* t) { return t[0] >= 192 ? 0 : t[1] >= 256 ? 1 : 2; };
+    o.cfg_sq = pick(sq); o.cfg_step = pick(up);
+    int bs, bu;
+    ns_tile_size(o.cfg_sq, &bs); ns_tile_size(o.cfg_step, &bu);
+    long total[4] = {0, 0, 0, 0};
+    for (auto& s : o.start) s.assign(n + 1, 0);
+    for (int i = 0; i < n; ++i) {
+        NsProb& q = o.p[i];
+        q.r = std::min(q.rows, q.cols); q.c = std::max(q.rows, q.cols);
+        q.ldr = (q.r + 7) & ~7; q.ldc = (q.c + 7) & ~7;
+        const long here[4] = {((long)q.rows * q.cols + kNsElems - 1) / kNsElems, q.plain ? 0 : (long)div_up(q.rows, 64) * div_up(q.cols, 64),
+                              q.plain ? 0 : (long)div_up(q.r, bs) * div_up(q.r, bs), q.plain ? 0 : (long)div_up(q.r, bu) * div_up(q.c, bu)};
+        for (int k = 0; k < 4; ++k) { o.start[k][i] = (int)total[k]; total[k] += here[k]; }
+        if (!q.plain) {
+            const size_t x = (size_t)q.r * q.ldc * 4, s = (size_t)q.r * q.ldr * 4;
+            q.x0 = (char*)ws.take(x); q.x1 = (char*)ws.take(x); q.s = (char*)ws.take(s); q.b = (char*)ws.take(s);     // offsets, for now
+        }
+    }
+    for (int k = 0; k < 4; ++k) {
+        if (total[k] > (1l << 30)) return fail(LP_ERR_SHAPE, "too many elements in one call");
+        o.start[k][n] = (int)total[k];
+    }
+    o.o_norm = ws.take((size_t)total[0] * sizeof(double));
+    o.bytes = std::max<size_t>(ws.off, 256);
+    return LP_OK;
+}
+
+static lp_status ortho_run(OrthoPlan& o, char* ws, size_t ws_bytes, float momentum, float wd, float rest_lr, int nesterov, int steps, hipStream_t s) {
+    if (!ws || ws_bytes < o.bytes) return fail(LP_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : (size_t)0, o.bytes);
+    if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(LP_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+    const int n = (int)o.p.size();
+    if (o.start[0][n] == 0) return LP_OK;
+    for (NsProb& q : o.p)
+        if (!q.plain) { q.x0 = ws + (size_t)q.x0; q.x1 = ws + (size_t)q.x1; q.s = ws + (size_t)q.s; q.b = ws + (size_t)q.b; }
+    // the table goes to the device in the arguments of small launches: legal under capture, no host memory to keep
+    std::vector<unsigned> words(o.table_words(), 0u);
+    for (int k = 0; k < 4; ++k) memcpy(words.data() + k * (n + 1), o.start[k].data(), (size_t)(n + 1) * 4);
+    memcpy(words.data() + o.probs_word(), o.p.data(), (size_t)n * sizeof(NsProb));
+    hipError_t err = hipSuccess;
+    constexpr int room = (int)(sizeof(NsChunk::w) / 4);
+    for (size_t at = 0; at < words.size() && err == hipSuccess; at += room) {
+        NsChunk c;
+        c.dst = (unsigned*)(ws + o.o_table) + at;
+        c.words = (int)std::min<size_t>(room, words.size() - at);
+        memcpy(c.w, words.data() + at, (size_t)c.words * 4);
+        err = launch_ns_put(c, s);
+    }
+    NsArgs a;
+    memset(&a, 0, sizeof(a));
+    const int* const table = (const int*)(ws + o.o_table);
+    a.p = (const NsProb*)(table + o.probs_word());
+    a.start_norm = table; a.norm = (double*)(ws + o.o_norm); a.n = n;
+    a.momentum = momentum; a.wd = wd; a.rest_lr = rest_lr; a.nesterov = nesterov;
+    auto at = [&](int k) { a.start = table + (size_t)k * (n + 1); a.total = o.start[k][n]; };
+    at(0);
+    if (err == hipSuccess) err = launch_ns_norm(a, s);
+    at(1);
+    if (err == hipSuccess) err = launch_ns_split(a, s);
+    for (int i = 0; i < steps && err == hipSuccess; ++i) {
+        a.odd = i & 1; a.last = i + 1 == steps;
+        at(2);
+        err = launch_ns_gram(a, o.cfg_sq, s);
+        if (err == hipSuccess) err = launch_ns_poly(a, o.cfg_sq, s);
+        at(3);
+        if (err == hipSuccess) err = launch_ns_step(a, o.cfg_step, s);
+    }
+    return hip_status(err);
+}
+
+static lp_status ortho_matrices(int n, const lp_matrix* mats, OrthoPlan& o) {
+    if (n < 0 || n > LP_ORTHO_MAX_MATRICES || (n > 0 && !mats)) return fail(LP_ERR_INVALID_ARG, "%d matrices, or their list is NULL", n);
+    for (int i = 0; i < n; ++i) {
+        const lp_matrix& m = mats[i];
+        lp_status st = ortho_shape(m.rows, m.cols);
+        if (st != LP_OK) return st;
+        for (const int t : {m.dtype_in, m.dtype_out})
+            if (t != LP_F32 && t != LP_BF16) return fail(LP_ERR_DTYPE, "matrix %d: dtype %d is neither LP_F32 nor LP_BF16", i, t);
+        const long ldi = m.ld_in ? m.ld_in : m.cols, ldo = m.ld_out ? m.ld_out : m.cols;
+        if (ldi < m.cols || ldo < m.cols || ldi > (1l << 40) || ldo > (1l << 40)) return fail(LP_ERR_SHAPE, "matrix %d: a row stride of %ld or %ld for %d columns", i, ldi, ldo, m.cols);
+        if (m.rows == 0 || m.cols == 0) continue;
+        NsProb q;
+        memset(&q, 0, sizeof(q));
+        q.rows = m.rows; q.cols = m.cols; q.src = m.in; q.out = m.out; q.ld_src = ldi; q.ld_out = ldo;
+        q.src_low = m.dtype_in == LP_BF16; q.out_low = m.dtype_out == LP_BF16;
+        o.p.push_back(q);
+    }
+    return ortho_plan(o);
+}
+
+// one parameter tensor of an update
+static lp_status muon_tensor(int rows, int cols, int dtype, int orthogonal, void* param, const float* grad, float* vel, float* master, const lp_muon_opts* opts, OrthoPlan& o) {
+    if (rows < 1 || cols < 1) return fail(LP_ERR_INVALID_ARG, "a tensor of %d x %d", rows, cols);
+    if (dtype != LP_F32 && dtype != LP_BF16) return fail(LP_ERR_DTYPE, "dtype %d is neither LP_F32 nor LP_BF16", dtype);
+    if (orthogonal) {
+        const lp_status st = ortho_shape(rows, cols);
+        if (st != LP_OK) return st;
+    }
+    NsProb q;
+    memset(&q, 0, sizeof(q));
+    q.rows = rows; q.cols = cols; q.plain = !orthogonal; q.ld_out = cols; q.out_low = dtype == LP_BF16;
+    q.out = param; q.grad = grad; q.vel = vel; q.master = master;
+    q.vec = !misaligned(grad) && !misaligned(vel);
+    if (opts) {
+        q.lr = (float)(opts->lr * std::sqrt(std::max(1.0, (double)rows / cols)));
+        q.shrink = (float)(1.0 - (double)opts->lr * opts->weight_decay);
+    }
+    o.p.push_back(q);
+    return LP_OK;
+}
+
+static lp_status muon_opts(const lp_muon_opts* opts) {
+    if (!opts) return fail(LP_ERR_INVALID_ARG, "options are NULL");
+    if (opts->steps < 1 || opts->steps > LP_ORTHO_MAX_STEPS) return fail(LP_ERR_INVALID_ARG, "%d steps outside [1, %d]", opts->steps, LP_ORTHO_MAX_STEPS);
+    return LP_OK;
+}
+
+static lp_status muon_tensors(int n, const lp_muon_tensor* t, void* params, const float* grads, float* velocity, float* master, const lp_muon_opts* opts, OrthoPlan& o) {
+    if (n < 0 || n > LP_ORTHO_MAX_MATRICES || (n > 0 && !t)) return fail(LP_ERR_INVALID_ARG, "%d tensors, or their list is NULL", n);
+    for (int i = 0; i < n; ++i) {
+        if (t[i].offset % (t[i].dtype == LP_BF16 ? 2 : 4) || t[i].grad_offset % 4) return fail(LP_ERR_INVALID_ARG, "tensor %d: misaligned offset", i);
+        auto f = [&](const void* p) { return p ? (float*)((char*)p + t[i].grad_offset) : nullptr; };
+        const lp_status st = muon_tensor(t[i].rows, t[i].cols, t[i].dtype, t[i].orthogonal, params ? (char*)params + t[i].offset : nullptr, f(grads), f(velocity), f(master), opts, o);
+        if (st != LP_OK) return st;
+    }
+    return ortho_plan(o);
+}
+
+static lp_status muon_net(const lp_net* net, int aux, uint32_t mask, int head, void* const* params, const float* const* dparams, float* const* velocity,
+                          float* const* master, const lp_muon_opts* opts, OrthoPlan& o) {
+    if (!net) return fail(LP_ERR_INVALID_ARG, "net is NULL");
+    if (aux && net->aux.empty()) return fail(LP_ERR_STATE, "the net was created without an AuxNet");
+    const int n = aux ? (int)net->aux.size() : net->K;
+    if (mask == 0 || (n < 32 && (mask >> n) != 0)) return fail(LP_ERR_INVALID_ARG, "mask 0x%x does not fit %d parameter sets", mask, n);
+    for (int k = 0; k < n; ++k) {
+        if (!((mask >> k) & 1u)) continue;
+        const std::vector<lp_tensor_info>* t; size_t pb, gb;
+        lp_status st = table_of(net, aux, k, &t, &pb, &gb);
+        if (st != LP_OK) return st;
+        void* const w = params ? params[k] : nullptr;
+        const float* const g = dparams ? dparams[k] : nullptr;
+        float* const v = velocity ? velocity[k] : nullptr;
+        float* const m = master ? master[k] : nullptr;
+        if (opts) {
+            if (!w || !g || !v) return fail(LP_ERR_INVALID_ARG, "params[%d], dparams[%d] or velocity[%d] is NULL", k, k, k);
+            if (misaligned(w) || misaligned(g) || misaligned(v) || misaligned(m)) return fail(LP_ERR_INVALID_ARG, "parameter set %d: a buffer is not 16-byte aligned", k);
+        }
+        for (const lp_tensor_info& ti : *t) {
+            const int orth = ti.kind == LP_T_CONV || (head && ti.kind == LP_T_FC_W);
+            auto f = [&](const void* p) { return p ? (float*)((char*)p + ti.grad_offset) : nullptr; };
+            st = muon_tensor(ti.dims[0], (int)(ti.numel / ti.dims[0]), ti.dtype, orth, w ? (char*)w + ti.offset : nullptr, f(g), f(v), f(m), opts, o);
+            if (st != LP_OK) return st;
+        }
+    }
+    return ortho_plan(o);
+}
+
+}  // namespace
+
+lp_status lp_orthogonalize_workspace_bytes(int n, const lp_matrix* mats, size_t* bytes) {
+    if (!bytes) return fail(LP_ERR_INVALID_ARG, "bytes is NULL");
+    return guarded([&] {
+        OrthoPlan o;
+        const lp_status st = ortho_matrices(n, mats, o);
+        if (st == LP_OK) *bytes = o.bytes;
+        return st;
+    });
+}
+
+lp_status lp_orthogonalize(void* stream, int n, const lp_matrix* mats, int steps, void* workspace, size_t workspace_bytes) {
+    if (steps < 1 || steps > LP_ORTHO_MAX_STEPS) return fail(LP_ERR_INVALID_ARG, "%d steps outside [1, %d]", steps, LP_ORTHO_MAX_STEPS);
+    return guarded([&] {
+        OrthoPlan o;
+        const lp_status st = ortho_matrices(n, mats, o);
+        if (st != LP_OK) return st;
+        for (const NsProb& q : o.p) {
+            if (!q.src || !q.out) return fail(LP_ERR_INVALID_ARG, "a matrix of %d x %d without in or out", q.rows, q.cols);
+            if (reinterpret_cast<uintptr_t>(q.src) % (q.src_low ? 2 : 4) || reinterpret_cast<uintptr_t>(q.out) % (q.out_low ? 2 : 4))
+                return fail(LP_ERR_INVALID_ARG, "a matrix is not aligned to its elements");
+        }
+        return ortho_run(o, (char*)workspace, workspace_bytes, 0.f, 0.f, 0.f, 0, steps, (hipStream_t)stream);
+    });
+}
+
+lp_status lp_muon_step_workspace_bytes(int n, const lp_muon_tensor* tensors, size_t* bytes) {
+    if (!bytes) return fail(LP_ERR_INVALID_ARG, "bytes is NULL");
+    return guarded([&] {
+        OrthoPlan o;
+        const lp_status st = muon_tensors(n, tensors, nullptr, nullptr, nullptr, nullptr, nullptr, o);
+        if (st == LP_OK) *bytes = o.bytes;
+        return st;
+    });
+}
+
+lp_status lp_muon_step(void* stream, int n, const lp_muon_tensor* tensors, void* params, const float* grads, float* velocity,
+                       float* master, const lp_muon_opts* opts, void* workspace, size_t workspace_bytes) {
+    const lp_status bad = muon_opts(opts);
+    if (bad != LP_OK) return bad;
+    if (n > 0 && (!params || !grads || !velocity)) return fail(LP_ERR_INVALID_ARG, "params, grads or velocity is NULL");
+    if (misaligned(params) || misaligned(grads) || misaligned(velocity) || misaligned(master)) return fail(LP_ERR_INVALID_ARG, "a buffer is not 16-byte aligned");
+    return guarded([&] {
+        OrthoPlan o;
+        const lp_status st = muon_tensors(n, tensors, params, grads, velocity, master, opts, o);
+        if (st != LP_OK) return st;
+        return ortho_run(o, (char*)workspace, workspace_bytes, opts->momentum, opts->weight_decay, opts->rest_lr, opts->nesterov != 0, opts->steps, (hipStream_t)stream);
+    });
+}
+
+lp_status lp_muon_workspace_bytes(const struct lp_net* net, int aux, uint32_t mask, int head, size_t* bytes) {
+    if (!bytes) return fail(LP_ERR_INVALID_ARG, "bytes is NULL");
+    return guarded([&] {
+        OrthoPlan o;
+        const lp_status st = muon_net(net, aux, mask, head, nullptr, nullptr, nullptr, nullptr, nullptr, o);
+        if (st == LP_OK) *bytes = o.bytes;
+        return st;
+    });
+}
+
+lp_status lp_muon_update(struct lp_net* net, void* stream, int aux, uint32_t mask, int head, void* const* params,
+                         const float* const* dparams, float* const* velocity, float* const* master, const lp_muon_opts* opts,
+                         void* workspace, size_t workspace_bytes) {
+    const lp_status bad = muon_opts(opts);
+    if (bad != LP_OK) return bad;
+    if (!params || !dparams || !velocity) return fail(LP_ERR_INVALID_ARG, "params, dparams or velocity is NULL");
+    return guarded([&] {
+        OrthoPlan o;
+        const lp_status st = muon_net(net, aux, mask, head, params, dparams, velocity, master, opts, o);
+        if (st != LP_OK) return st;
+        return ortho_run(o, (char*)workspace, workspace_bytes, opts->momentum, opts->weight_decay, opts->rest_lr, opts->nesterov != 0, opts->steps, (hipStream_t)stream);
+    });
 }
 
 lp_status lp_aux_variable_update(struct lp_net* net, void* stream, void* const* x, const void* const* y_prev,

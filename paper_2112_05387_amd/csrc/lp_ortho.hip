@@ -1,0 +1,331 @@
+// Orthogonalisation of matrices by Newton-Schulz products, and the parameter update that takes it as its direction (gfx950):
+//
+//   X <- U / |U|;   five times:  S = X X^T,  B = a I + b S + c S S,  X <- B X
+//
+// drives every singular value of U towards one (the odd polynomial a x + b x^3 + c x^5 of each, with the coefficients below, stays
+// within 0.7 .. 1.2 from the fifth step on).  Products with the shorter side r as rows: 2 r^2 (2 c + r) multiplications a step.
+//
+// Precision.  The small singular values grow by a = 3.4 a step, 480 times in five, and so does every rounding in their
+// directions.  In bf16 the result of a random matrix is off by 1 %, of one of low rank by half; with 11 bits (one fp16) by 0.15 %
+// and 6 %.  Here every operand is a sum of two fp16 (22 bits; the entries are bounded by 1.21, S by 1.5, B by 3.5, so powers of
+// two that keep the second part above the subnormal numbers are fixed), and a product takes three of the four: off by 7e-7 and
+// 2e-5 of it, as fp32 arithmetic is (1.5e-6, 3e-5).
+//
+// All tensors of an update go through the same launches: one over the elements (momentum, sums of squares, and the whole update
+// of the tensors that are not matrices), one that scales, splits and turns tall matrices, and three products a step.
+#include "lp_ortho.h"
+
+#include <algorithm>
+
+#include "lp_gemm.h"
+#include "lp_kernels.h"
+
+namespace lp {
+namespace {
+
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr float kScaleX = 16384.f, kScaleS = 8192.f, kScaleB = 4096.f;
+
+// the last tensor whose first block is not beyond `block`
+__device__ __forceinline__ int ns_find(const int* start, int n, int block) {
+    const int lane = threadIdx.x & 63;
+    int found = 0;
+    for (int i = 0; i < n; i += 64) found += __popcll(__ballot(i + lane < n && start[min(i + lane, n)] <= block));
+    return __builtin_amdgcn_readfirstlane(found - 1);
+}
+
+__device__ __forceinline__ unsigned f16_bits(float x) { return __builtin_bit_cast(unsigned short, (_Float16)x); }
+__device__ __forceinline__ float f16_up(unsigned b) { return (float)__builtin_bit_cast(_Float16, (unsigned short)b); }
+
+__global__ __launch_bounds__(256) void ns_put_kernel(const NsChunk c) {
+    for (int i = threadIdx.x; i < c.words; i += 256) c.dst[i] = c.w[i];
+}
+
+__device__ __forceinline__ float load_low(const void* p, int low, size_t e) {
+    return low ? bf16_bits_to_float(reinterpret_cast<const unsigned short*>(p)[e]) : reinterpret_cast<const float*>(p)[e];
+}
+__device__ __forceinline__ void store_low(void* p, int low, size_t e, float x) {
+    if (low) reinterpret_cast<unsigned short*>(p)[e] = float_to_bf16_bits(x);
+    else reinterpret_cast<float*>(p)[e] = x;
+}
+
+// Elements: momentum of the matrices and their sums of squares; the whole update of the other tensors
+__global__ __launch_bounds__(256) void ns_norm_kernel(const NsArgs a) {
+    const int pi = ns_find(a.start, a.n, blockIdx.x);
+    const NsProb& P = a.p[pi];
+    const size_t numel = (size_t)P.rows * P.cols, base = (size_t)(blockIdx.x - a.start[pi]) * kNsElems;
+    const int tid = threadIdx.x;
+    double sum = 0.0;
+    auto element = [&](size_t e, float g, float v, float w) __attribute__((always_inline)) {       // returns through vel / out
+        if (P.plain) {
+            v = fmaf(a.momentum, v, fmaf(a.wd, w, g));
+            w = fmaf(-a.rest_lr, v, w);
+            P.vel[e] = v;
+            if (P.master) P.master[e] = w;
+            store_low(P.out, P.out_low, e, w);
+        } else {
+            v = fmaf(a.momentum, v, g);
+            P.vel[e] = v;
+            const float u = a.nesterov ? fmaf(a.momentum, v, g) : v;
+            sum += (double)u * u;
+        }
+    };
+    if (P.src) {
+        for (int i = tid; i < kNsElems; i += 256) {
+            const size_t e = base + i;
+            if (e >= numel) break;
+            const size_t row = e / P.cols;
+            const float u = load_low(P.src, P.src_low, row * P.ld_src + (e - row * P.cols));
+            sum += (double)u * u;
+        }
+    } else if (P.vec && !P.plain && base + kNsElems <= numel) {
+#pragma unroll
+        for (int i = 0; i < kNsElems / 1024; ++i) {
+            const size_t e = base + (size_t)(i * 256 + tid) * 4;
+            const f32x4 g = *reinterpret_cast<const f32x4*>(P.grad + e);
+            f32x4 v = *reinterpret_cast<const f32x4*>(P.vel + e);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                v[q] = fmaf(a.momentum, v[q], g[q]);
+                const float u = a.nesterov ? fmaf(a.momentum, v[q], g[q]) : v[q];
+                sum += (double)u * u;
+            }
+            *reinterpret_cast<f32x4*>(P.vel + e) = v;
+        }
+    } else {
+        for (int i = tid; i < kNsElems; i += 256) {
+            const size_t e = base + i;
+            if (e >= numel) break;
+            element(e, P.grad[e], P.vel[e], P.plain ? (P.master ? P.master[e] : load_low(P.out, P.out_low, e)) : 0.f);
+        }
+    }
+    __shared__ double s[4];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    if ((tid & 63) == 0) s[tid >> 6] = sum;
+    __syncthreads();
+    if (tid == 0) a.norm[blockIdx.x] = (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+// 64 x 64 pieces of U / |U| into the planes of X, turned where the matrix is tall
+__global__ __launch_bounds__(256) void ns_split_kernel(const NsArgs a) {
+    __shared__ float t[64][65];
+    __shared__ double s[4];
+    const int pi = ns_find(a.start, a.n, blockIdx.x);
+    const NsProb& P = a.p[pi];
+    const int tid = threadIdx.x;
+    const int b0 = a.start_norm[pi], b1 = a.start_norm[pi + 1];
+    double sum = 0.0;
+    for (int b = b0 + tid; b < b1; b += 256) sum += a.norm[b];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    if ((tid & 63) == 0) s[tid >> 6] = sum;
+    const int local = blockIdx.x - a.start[pi], pc = (P.cols + 63) >> 6;
+    const int r0 = local / pc * 64, c0 = (local - local / pc * pc) * 64;
+    const int col = tid & 63, c = c0 + col;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const int row = (tid >> 6) + 4 * k, rr = r0 + row;
+        float u = 0.f;
+        if (rr < P.rows && c < P.cols) {
+            if (P.src) u = load_low(P.src, P.src_low, (size_t)rr * P.ld_src + c);
+            else {
+                const size_t e = (size_t)rr * P.cols + c;
+                u = P.vel[e];
+                if (a.nesterov) u = fmaf(a.momentum, u, P.grad[e]);
+            }
+        }
+        t[row][col] = u;
+    }
+    __syncthreads();
+    const double norm = sqrt((s[0] + s[1]) + (s[2] + s[3]));
+    const float inv = (float)((double)kScaleX / (norm < 1e-7 ? 1e-7 : norm));
+    const bool tall = P.rows > P.cols;
+    // the piece as rows of X: row x0 + i, columns y0 + 2 j, y0 + 2 j + 1
+    const int x0 = tall ? c0 : r0, y0 = tall ? r0 : c0;
+    unsigned* const hi = reinterpret_cast<unsigned*>(P.x0);
+    unsigned* const lo = hi + ((size_t)P.r * P.ldc >> 1);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int i = (tid >> 5) + 8 * k, j = 2 * (tid & 31);
+        if (x0 + i < P.r && y0 + j < P.ldc) {
+            const float u0 = (tall ? t[j][i] : t[i][j]) * inv, u1 = (tall ? t[j + 1][i] : t[i][j + 1]) * inv;
+            const unsigned h0 = f16_bits(u0), h1 = f16_bits(u1);
+            const size_t at = ((size_t)(x0 + i) * P.ldc + y0 + j) >> 1;
+            hi[at] = h0 | (h1 << 16);
+            lo[at] = f16_bits(u0 - f16_up(h0)) | (f16_bits(u1 - f16_up(h1)) << 16);
+        }
+    }
+}
+
+enum NsMode { NS_GRAM, NS_POLY, NS_STEP, NS_LAST };
+
+// A 32 x 32 piece E[j][i] of O, i from i0 along the longer side: stored, or taken as the step of the parameters
+__device__ __forceinline__ void ns_answer(const NsProb& P, const float* E, bool tall, int i0, int j0, int lane) {
+    const int l = lane & 31, m0 = lane >> 5;
+    const int col = tall ? j0 + l : i0 + l, row0 = tall ? i0 : j0;
+    const int step = tall ? 1 : 33, at = tall ? l * 33 : l;
+    if (col >= P.cols) return;
+#pragma unroll 4
+    for (int m = m0; m < 32; m += 2) {
+        if (row0 + m >= P.rows) break;
+        const float o = E[at + m * step];
+        const size_t e = (size_t)(row0 + m) * P.ld_out + col;
+        if (P.src) store_low(P.out, P.out_low, e, o);
+        else {
+            const float old = P.master ? P.master[e] : load_low(P.out, P.out_low, e);
+            const float w = fmaf(-P.lr, o, old * P.shrink);
+            if (P.master) P.master[e] = w;
+            store_low(P.out, P.out_low, e, w);
+        }
+    }
+}
+
+template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm_kernel(const NsArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const int x = blockIdx.x & 7, per = a.total >> 3, rem = a.total & 7;
+    const int t = x * per + (x < rem ? x : rem) + (blockIdx.x >> 3);       // consecutive tiles to one XCD
+    const int pi = ns_find(a.start, a.n, t);
+    const NsProb& P = a.p[pi];
+    const int local = t - a.start[pi], r = P.r, ldr = P.ldr, ldc = P.ldc;
+    constexpr bool STEP = MODE == NS_STEP || MODE == NS_LAST;
+    const int ni = STEP ? P.c : r, ti_n = (ni + T::BI - 1) / T::BI, tj_n = (r + T::BJ - 1) / T::BJ;
+    const int band = min(8, tj_n), full = band * ti_n, bd = local / full, w = min(band, tj_n - bd * band), in = local - bd * full;
+    const int ti = in / w, tj = bd * band + in - ti * w;
+    const int i0 = ti * T::BI, j0 = tj * T::BJ;
+    char* const X = a.odd ? P.x1 : P.x0;
+    const size_t xplane = (size_t)r * ldc * 2, splane = (size_t)r * ldr * 2;
+    const GemmOperand ox = {X, xplane, ldc, STEP ? ldc : r}, os = {P.s, splane, ldr, r}, ob = {P.b, splane, ldr, r};
+    const GemmPairs three = {3, 0x100, 0x010};
+    typename T::Acc acc;
+#pragma unroll
+    for (int i = 0; i < T::TI / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < T::TJ / 32; ++j)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+    if constexpr (MODE == NS_GRAM) T::run(ox, ox, three, i0, j0, 0, ldc, (GemmMask)nullptr, smem, acc);
+    else if constexpr (MODE == NS_POLY) T::run(os, os, three, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
+    else T::run(ox, ob, three, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wi = wave / (T::BJ / T::TJ), wj = wave % (T::BJ / T::TJ);
+    const int lr = lane & 31, h = lane >> 5;
+    const int ib = i0 + wi * T::TI, jb = j0 + wj * T::TJ;
+    constexpr int FI = T::TI / 32, FJ = T::TJ / 32;
+
+    if constexpr (MODE == NS_LAST) {
+        // the answer: micro-tiles through LDS, so that both orientations go out along rows
+        float* const E = reinterpret_cast<float*>(smem) + wave * (32 * 33);
+        const bool tall = P.rows > P.cols;
+        constexpr float back = 1.f / (kScaleB * kScaleX);
+#pragma unroll
+        for (int j = 0; j < FJ; ++j)
+#pragma unroll
+            for (int i = 0; i < FI; ++i) {
+#pragma unroll
+                for (int q = 0; q < 16; ++q) E[lr * 33 + T::row(q, lane)] = acc[i][j][q] * back;
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_s_waitcnt(0xc07f);
+                ns_answer(P, E, tall, ib + i * 32, jb + j * 32, lane);
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                __builtin_amdgcn_s_waitcnt(0xc07f);
+            }
+        return;
+    }
+    // planes of the result, 32 rows of the wave at a time through LDS, out as 16-byte pieces of rows
+    constexpr int PITCH = T::TI * 2 + 16, EP = 32 * PITCH, CPR = T::TI / 8, RPL = 64 / CPR;
+    constexpr float scale = MODE == NS_GRAM ? kScaleS / (kScaleX * kScaleX) : MODE == NS_POLY ? kC * kScaleB / (kScaleS * kScaleS) : 1.f / kScaleB;
+    char* const out = MODE == NS_GRAM ? P.s : MODE == NS_POLY ? P.b : (a.odd ? P.x0 : P.x1);
+    const size_t oplane = MODE == NS_STEP ? xplane : splane;
+    const int ldo = MODE == NS_STEP ? ldc : ldr;
+    unsigned char* const E = smem + wave * (2 * EP);
+    const int c = lane % CPR, jr = lane / CPR;
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) {
+        const int jj = jb + j * 32 + lr;
+#pragma unroll
+        for (int i = 0; i < FI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int ii = ib + i * 32 + 8 * q + 4 * h;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e] * scale;
+                if constexpr (MODE == NS_POLY) {
+                    if (jj < r && ii < ldr) {
+                        const char* const sp = P.s + ((size_t)jj * ldr + ii) * 2;
+                        const u32x2 s0 = *reinterpret_cast<const u32x2*>(sp), s1 = *reinterpret_cast<const u32x2*>(sp + splane);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float sv = f16_up(s0[e >> 1] >> (16 * (e & 1))) + f16_up(s1[e >> 1] >> (16 * (e & 1)));
+                            v[e] = fmaf(kB * (kScaleB / kScaleS), sv, v[e]);
+                            if (ii + e == jj) v[e] += kA * kScaleB;
+                        }
+                    }
+                }
+                unsigned hb[4], lb[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { hb[e] = f16_bits(v[e]); lb[e] = f16_bits(v[e] - f16_up(hb[e])); }
+                unsigned char* const d = E + lr * PITCH + (i * 32 + 8 * q + 4 * h) * 2;
+                *reinterpret_cast<u32x2*>(d) = u32x2{hb[0] | (hb[1] << 16), hb[2] | (hb[3] << 16)};
+                *reinterpret_cast<u32x2*>(d + EP) = u32x2{lb[0] | (lb[1] << 16), lb[2] | (lb[3] << 16)};
+            }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+#pragma unroll
+        for (int q = 0; q < 32 / RPL; ++q) {
+            const int row = q * RPL + jr, jo = jb + j * 32 + row, ii = ib + c * 8;
+            if (jo < r && ii < ldo) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    *reinterpret_cast<u32x4*>(out + k * oplane + ((size_t)jo * ldo + ii) * 2) = *reinterpret_cast<const u32x4*>(E + k * EP + row * PITCH + c * 16);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+    }
+}
+
+template <bool AKR> using NBig = GemmTile<f16_t, AKR, false, 2, 4, 4, 2, 2>;
+template <bool AKR> using NMid = GemmTile<f16_t, AKR, false, 2, 2, 2, 2, 2>;
+template <bool AKR> using NSmall = GemmTile<f16_t, AKR, false, 2, 2, 1, 1, 4>;
+
+template <class T, int MODE> hipError_t launch_gemm(const NsArgs& a, hipStream_t s) {
+    static OncePerDevice once;
+    constexpr int lds = std::max(T::LDS, T::NW * 2 * 32 * (T::TI * 2 + 16));
+    auto k = ns_gemm_kernel<T, MODE>;
+    if (const hipError_t e = raise_lds_limit(once, {(const void*)k}, lds); e != hipSuccess) return e;
+    hipLaunchKernelGGL(k, dim3(a.total), dim3(T::NT), lds, s, a);
+    return hipGetLastError();
+}
+template <bool AKR, int MODE> hipError_t launch_mode(const NsArgs& a, int cfg, hipStream_t s) {
+    if (a.total <= 0) return hipSuccess;
+    if (cfg == 0) return launch_gemm<NBig<AKR>, MODE>(a, s);
+    if (cfg == 1) return launch_gemm<NMid<AKR>, MODE>(a, s);
+    return launch_gemm<NSmall<AKR>, MODE>(a, s);
+}
+
+}  // namespace
+
+void ns_tile_size(int cfg, int* b) { *b = cfg == 0 ? 256 : cfg == 1 ? 128 : 64; }
+
+hipError_t launch_ns_put(const NsChunk& c, hipStream_t s) {
+    hipLaunchKernelGGL(ns_put_kernel, dim3(1), dim3(256), 0, s, c);
+    return hipGetLastError();
+}
+hipError_t launch_ns_norm(const NsArgs& a, hipStream_t s) {
+    if (a.total <= 0) return hipSuccess;
+    hipLaunchKernelGGL(ns_norm_kernel, dim3(a.total), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+hipError_t launch_ns_split(const NsArgs& a, hipStream_t s) {
+    if (a.total <= 0) return hipSuccess;
+    hipLaunchKernelGGL(ns_split_kernel, dim3(a.total), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+hipError_t launch_ns_gram(const NsArgs& a, int cfg, hipStream_t s) { return launch_mode<false, NS_GRAM>(a, cfg, s); }
+hipError_t launch_ns_poly(const NsArgs& a, int cfg, hipStream_t s) { return launch_mode<false, NS_POLY>(a, cfg, s); }
+hipError_t launch_ns_step(const NsArgs& a, int cfg, hipStream_t s) { return a.last ? launch_mode<true, NS_LAST>(a, cfg, s) : launch_mode<true, NS_STEP>(a, cfg, s); }
+
+}  // namespace lp

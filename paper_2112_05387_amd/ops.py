@@ -4,6 +4,9 @@ Every call enqueues its work on the current stream of the tensors' device and re
 torch's allocator on that stream, so calls on several streams, and calls captured into HIP graphs, do not share any.  As with
 any torch operator, a tensor that another stream produced has to be waited for by the caller.
 """
+import functools
+import math
+
 import torch
 
 from . import binding as B
@@ -93,3 +96,65 @@ def linear_ce_backward(features, weight, labels, lse, bias=None, scale=1.0):
         B.lp_linear_ce_backward(d, torch.cuda.current_stream().cuda_stream, features.data_ptr(), weight.data_ptr(), _ptr(bias), labels.data_ptr(),
                                 lse.data_ptr(), scale, dx.data_ptr(), dw.data_ptr(), _ptr(db), ws.data_ptr(), size)
     return dx, dw, db
+
+
+def orthogonalize(matrices, steps=5, out_dtype=None):
+    """The matrices with their singular values taken towards one by Newton-Schulz products (lp_orthogonalize): a list of new
+    tensors, each of its matrix's type (or `out_dtype`).  float32 or bfloat16, any sizes and row strides, all in the same launches."""
+    matrices = list(matrices)
+    dev = _device(*matrices)
+    mats = (B.lp_matrix * len(matrices))()
+    outs, keep = [], []
+    for i, m in enumerate(matrices):
+        o = out_dtype or m.dtype
+        if m.dim() != 2 or m.dtype not in _DTYPES or o not in _DTYPES:
+            raise ValueError(f"matrix {i}: expected a float32 or bfloat16 matrix, got {m.dtype} {tuple(m.shape)}, result {o}")
+        if m.numel() and ((m.shape[1] > 1 and m.stride(1) != 1) or (m.shape[0] > 1 and m.stride(0) < m.shape[1])):
+            m = m.clone(memory_format=torch.contiguous_format)
+            keep.append(m)
+        out = torch.empty(m.shape, dtype=o, device=dev)
+        outs.append(out)
+        mats[i] = B.lp_matrix(m.shape[0], m.shape[1], _DTYPES[m.dtype], _DTYPES[o], m.data_ptr(), out.data_ptr(), _ld(m), 0)
+    if dev is None:
+        return outs
+    with torch.cuda.device(dev):
+        size = B.lp_orthogonalize_workspace_bytes(mats)
+        ws = torch.empty(size, dtype=torch.uint8, device=dev)
+        B.lp_orthogonalize(torch.cuda.current_stream().cuda_stream, mats, steps, ws.data_ptr(), size)
+    return outs
+
+
+@functools.lru_cache(maxsize=64)
+def _muon_table(table):
+    """(tensors of a packed set as the library reads them, workspace they need, bytes of the parameters and of the fp32 buffers)"""
+    arr = (B.lp_muon_tensor * len(table))()
+    end = gend = 0
+    for i, (shape, dtype, orthogonal, offset, grad_offset) in enumerate(table):
+        n = math.prod(shape)
+        rows = shape[0] if len(shape) > 1 else 1
+        if dtype not in ("f32", "bf16") or n < 1:
+            raise ValueError(f"tensor {i}: {dtype} {shape}")
+        arr[i] = B.lp_muon_tensor(rows, n // rows, B.LP_BF16 if dtype == "bf16" else B.LP_F32, int(orthogonal), offset, grad_offset)
+        end, gend = max(end, offset + n * (2 if dtype == "bf16" else 4)), max(gend, grad_offset + 4 * n)
+    return arr, B.lp_muon_step_workspace_bytes(arr), end, gend
+
+
+def muon_update(table, params, grads, velocity, master=None, *, lr, momentum=0.95, nesterov=True, weight_decay=0.0, rest_lr=None, steps=5):
+    """Parameter update by orthogonalised momentum of a packed set of tensors, in place (lp_muon_step).
+
+    table: a tuple of (shape, "f32" or "bf16", orthogonal, byte offset in params, byte offset in the fp32 buffers), the layout
+    lp_net_tensor_info describes; a tensor of several dimensions is read as a matrix of shape[0] rows.  params: uint8; grads,
+    velocity, master: float32, one-dimensional, contiguous.  rest_lr (default lr): learning rate of the tensors that are not
+    orthogonalised."""
+    arr, size, end, gend = _muon_table(tuple(table))
+    dev = _device(params, grads, velocity, master)
+    if params.dtype != torch.uint8 or not params.is_contiguous() or params.numel() < end:
+        raise ValueError(f"params: expected {end} bytes (uint8, contiguous), got {params.dtype} {tuple(params.shape)}")
+    for name, t in (("grads", grads), ("velocity", velocity), ("master", master)):
+        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or 4 * t.numel() < gend):
+            raise ValueError(f"{name}: expected {gend // 4} float32, contiguous, got {t.dtype} {tuple(t.shape)}")
+    opts = B.lp_muon_opts(lr, momentum, weight_decay, lr if rest_lr is None else rest_lr, int(nesterov), steps)
+    with torch.cuda.device(dev):
+        ws = torch.empty(size, dtype=torch.uint8, device=dev)
+        B.lp_muon_step(torch.cuda.current_stream().cuda_stream, arr, params.data_ptr(), grads.data_ptr(), velocity.data_ptr(), _ptr(master),
+                       opts, ws.data_ptr(), size)

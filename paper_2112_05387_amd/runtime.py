@@ -224,6 +224,19 @@ class LocalStep:
                         None if velocity is None else self._p(velocity), None if master is None else self._p(master),
                         lr, momentum, weight_decay)
 
+    def muon_update(self, lr, velocity, momentum=0.95, nesterov=True, weight_decay=0.0, rest_lr=None, steps=5, master=None,
+                    mask=None, head=False, aux=False):
+        """Update by orthogonalised momentum (lp_muon_update) of the modules in `mask` (default all), or of the AuxNets: filters
+        orthogonalised, batch-norm tensors and the head (its weight too unless `head`) by momentum with rest_lr (default lr).
+        velocity, master: lists of tensors laid out like the gradients.  The workspace is torch's, on the current stream."""
+        m = ((1 << (self.K - 1)) - 1 if aux else self._mask(None)) if mask is None else mask
+        opts = B.lp_muon_opts(lr, momentum, weight_decay, lr if rest_lr is None else rest_lr, int(nesterov), steps)
+        size = B.lp_muon_workspace_bytes(self.net, aux, m, head)
+        ws = torch.empty(size, dtype=torch.uint8, device=self.dev)
+        B.lp_muon_update(self.net, self._stream(), aux, m, head, self._p(self.aux_params if aux else self.params),
+                         self._p(self.daux_params if aux else self.dparams), self._p(velocity),
+                         None if master is None else self._p(master), opts, ws.data_ptr(), size)
+
     def set_fused_update(self, on, lr=0.0, momentum=0.0, weight_decay=0.0, velocity=None, master=None):
         """Parameter update inside the backward pass (in the epilogues of the filter-gradient kernels); `velocity` and
         `master` are lists of K device tensors laid out like the gradients and must stay alive while it is on."""
