@@ -3496,7 +3496,7 @@ static lp_status ortho_plan(OrthoPlan& o) {
         for (const NsProb& q : o.p)
             if (!q.plain) {
                 const long r = (std::min(q.rows, q.cols) + b - 1) / b, l = (std::max(q.rows, q.cols) + b - 1) / b;
-                sq[c] += r * r; up[c] += r * l;
+                sq[c] += r * (r + 1) / 2; up[c] += r * l;
             }
     }
     auto pick = [](const long* t) { return t[0] >= 192 ? 0 : t[1] >= 256 ? 1 : 2; };
@@ -3508,12 +3508,12 @@ static lp_status ortho_plan(OrthoPlan& o) {
     for (int i = 0; i < n; ++i) {
         NsProb& q = o.p[i];
         q.r = std::min(q.rows, q.cols); q.c = std::max(q.rows, q.cols);
-        q.ldr = (q.r + 7) & ~7; q.ldc = (q.c + 7) & ~7;
+        q.ldr = div_up(q.r, 32) * 64; q.ldc = div_up(q.c, 32) * 64;
         const long here[4] = {((long)q.rows * q.cols + kNsElems - 1) / kNsElems, q.plain ? 0 : (long)div_up(q.rows, 64) * div_up(q.cols, 64),
-                              q.plain ? 0 : (long)div_up(q.r, bs) * div_up(q.r, bs), q.plain ? 0 : (long)div_up(q.r, bu) * div_up(q.c, bu)};
+                              q.plain ? 0 : (long)div_up(q.r, bs) * (div_up(q.r, bs) + 1) / 2, q.plain ? 0 : (long)div_up(q.r, bu) * div_up(q.c, bu)};
         for (int k = 0; k < 4; ++k) { o.start[k][i] = (int)total[k]; total[k] += here[k]; }
         if (!q.plain) {
-            const size_t x = (size_t)q.r * q.ldc * 4, s = (size_t)q.r * q.ldr * 4;
+            const size_t x = (size_t)q.r * q.ldc * 2, s = (size_t)q.r * q.ldr * 2;
             q.x0 = (char*)ws.take(x); q.x1 = (char*)ws.take(x); q.s = (char*)ws.take(s); q.b = (char*)ws.take(s);     // offsets, for now
         }
     }
@@ -3583,6 +3583,8 @@ static lp_status ortho_matrices(int n, const lp_matrix* mats, OrthoPlan& o) {
         memset(&q, 0, sizeof(q));
         q.rows = m.rows; q.cols = m.cols; q.src = m.in; q.out = m.out; q.ld_src = ldi; q.ld_out = ldo;
         q.src_low = m.dtype_in == LP_BF16; q.out_low = m.dtype_out == LP_BF16;
+        q.vec = ldi == m.cols && !misaligned(m.in);
+        q.vec_out = m.cols % 4 == 0 && ldo % 4 == 0 && !misaligned(m.out);
         o.p.push_back(q);
     }
     return ortho_plan(o);
@@ -3601,6 +3603,7 @@ static lp_status muon_tensor(int rows, int cols, int dtype, int orthogonal, void
     q.rows = rows; q.cols = cols; q.plain = !orthogonal; q.ld_out = cols; q.out_low = dtype == LP_BF16;
     q.out = param; q.grad = grad; q.vel = vel; q.master = master;
     q.vec = !misaligned(grad) && !misaligned(vel);
+    q.vec_out = cols % 4 == 0 && !misaligned(param) && !misaligned(master);
     if (opts) {
         q.lr = (float)(opts->lr * std::sqrt(std::max(1.0, (double)rows / cols)));
         q.shrink = (float)(1.0 - (double)opts->lr * opts->weight_decay);

@@ -11,6 +11,10 @@
 // v_mfma_f32_32x32x16: the former by 16-byte reads, the latter by transposing reads (ds_read_b64_tr_b16: 16 lanes read four
 // k of 16 rows and get four k of one row each).  So no operand is ever laid out anew for the other direction of a product.
 //
+// DUAL: both operands are sums of two planes that lie beside each other, 32 k of the first and the same 32 of the second in 128
+// bytes, and a k-tile of 64 elements is 32 k of either.  From the fragments of two planes come three products (the
+// fourth, of the two rests, is below the precision): half as much again for the same loads and LDS reads.
+//
 // LDS bandwidth (128 bytes a clock) and the latency of loads bound such a loop.  The tile of a wave is as large as the registers
 // allow, a k-tile is 64 long (128-byte rows: whole cache lines), the loads of a k-tile are spread between the products of the
 // one before it, and one barrier a k-tile, ahead of the products of its last 16 k, both frees its stage and shows the next.
@@ -20,6 +24,8 @@
 // Ragged edges, tails of k and rows that are to count as zero are out-of-range buffer offsets, which read as zeros.
 #pragma once
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "lp_mma.h"
 
@@ -47,12 +53,13 @@ typedef __attribute__((address_space(3))) void* gemm_lds_t;
 typedef const __attribute__((address_space(4))) unsigned long long* GemmMask;      // read by scalar loads
 typedef __attribute__((ext_vector_type(4))) short gemm_s16x4;
 
-template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGES, bool MASKED = false> struct GemmTile {
+template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGES, bool MASKED = false, bool DUAL = false> struct GemmTile {
     static constexpr int BK = 64, NW = WI * WJ, NT = NW * 64;
     static constexpr int TI = FI * 32, TJ = FJ * 32, BI = WI * TI, BJ = WJ * TJ;
     static constexpr int A_BYTES = BI * BK * 2, STAGE = (BI + BJ) * BK * 2, LDS = STAGES * STAGE;
     static constexpr int NSA = BI / 8 / NW, NSB = BJ / 8 / NW, NL = NSA + NSB;      // wave-loads of a k-tile
     static constexpr int KS = BK / 16;
+    static constexpr int PL = DUAL ? 2 : 1, KT = BK / PL;           // planes beside each other; k of a k-tile
     static_assert(NW % 2 == 0 && NSA * NW * 8 == BI && NSB * NW * 8 == BJ, "every wave loads the same number of slabs");
     typedef f32x16 Acc[FI][FJ];
 
@@ -64,9 +71,12 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, 0x7fffffff, 0x00020000);
     }
 
+    // KR: the places of a row's 32-byte pairs
+    template <int B> __device__ static __forceinline__ int swap(int k) { return B * PL >= 128 ? (k & 3) << 1 : B * PL == 64 ? ((k >> 1) & 1) << 1 : 0; }
+
     // One operand's loads: lane's offset in a slab, and what it has to compare with at the edges.
     template <bool KR, int B, int NS> struct Loader {
-        static constexpr int RB = B * 2, RPS = KR ? 1024 / RB : 8;      // KR: bytes of a row of the stage; rows of a slab
+        static constexpr int RB = B * PL * 2, RPS = KR ? 1024 / RB : 8; // KR: bytes of a row of the stage; rows of a slab
         const char* base; size_t plane; int ldb;        // bytes of a row of the operand
         unsigned voff; int row, chunk, last;            // row: this lane's in slab 0; last: rows that exist from row 0 of the tile on
         int step;                                       // bytes between the slabs of a wave
@@ -84,8 +94,8 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 constexpr int CPR = RB / 16;
                 const int sub = lane / CPR, pos = lane % CPR;
                 row = wave * RPS + sub;
-                const int f = B >= 128 ? (row & 3) << 1 : B == 64 ? ((row >> 1) & 1) << 1 : 0;
-                const int col = x0 + (((pos >> 1) ^ f) << 4) + (pos & 1) * 8;
+                const int f = swap<B>(row);
+                const int col = x0 * PL + (((pos >> 1) ^ f) << 4) + (pos & 1) * 8;
                 base = o.base; chunk = 0; last = 0;
                 voff = col < o.extent ? (unsigned)(row * ldb + col * 2) : kOOB;
             }
@@ -93,7 +103,7 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         }
         // load i of the k-tile that starts at k (krem: k that are left), of the plane at `p`
         __device__ __forceinline__ unsigned offset(int i, int krem, unsigned long long mask) const {
-            if constexpr (!KR) return row + i * (NW * RPS) < last && chunk * 8 < krem ? voff : kOOB;
+            if constexpr (!KR) return row + i * (NW * RPS) < last && (DUAL ? 0 : chunk * 8) < krem ? voff : kOOB;
             else {
                 const int k = row + i * (NW * RPS);
                 bool ok = k < krem;
@@ -102,7 +112,7 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
             }
         }
         __device__ __forceinline__ const char* at(int p, int k) const {
-            return base + (size_t)p * plane + (KR ? (size_t)k * ldb : (size_t)k * 2);
+            return base + (size_t)p * plane + (KR ? (size_t)k * ldb : (size_t)k * 2 * PL);
         }
     };
 
@@ -110,10 +120,10 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
     // waits for every load to LDS that is under way.  Nothing may touch a fragment between read() and arrived(), which is
     // where its value becomes usable; no fragment is under way where control flow joins.
     template <bool KR, int B, int F> struct Reader {
-        static constexpr int RB = B * 2;
+        static constexpr int RB = B * PL * 2;
         unsigned addr[KR ? F : KS];
-        u32x4 whole[2][KR ? 1 : F];
-        u32x2 half[2][KR ? F : 1][2];
+        u32x4 whole[2 * PL][KR ? 1 : F];               // DUAL: [k-step][plane]
+        u32x2 half[2 * PL][KR ? F : 1][2];
 
         __device__ __forceinline__ void init(int w, int lane, unsigned lds0) {
             if constexpr (!KR) {
@@ -122,18 +132,21 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 for (int ks = 0; ks < KS; ++ks) addr[ks] = lds0 + (w * F * 32 + r) * (BK * 2) + (((2 * ks + (lane >> 5)) ^ sw) << 4);
             } else {
                 const int lq = lane & 15, k = 8 * (lane >> 5) + (lq >> 2);
-                const int f = B >= 128 ? (k & 3) << 1 : B == 64 ? ((k >> 1) & 1) << 1 : 0;
+                const int f = swap<B>(k);
 #pragma unroll
-                for (int m = 0; m < F; ++m) addr[m] = lds0 + k * RB + (((2 * (w * F + m) + ((lane >> 4) & 1)) ^ f) << 5) + 8 * (lq & 3);
+                for (int m = 0; m < F; ++m) addr[m] = lds0 + k * RB + (((2 * PL * (w * F + m) + ((lane >> 4) & 1)) ^ f) << 5) + 8 * (lq & 3);
             }
         }
-        // the fragments of k-step S of the stage that starts at byte `st`
+        // the fragments of k-step S of the stage that starts at byte `st` (DUAL: S = 2 * plane + k-step of the k-tile's two)
         template <int S, int M = 0> __device__ __forceinline__ void read(unsigned st) {
+            constexpr int slot = DUAL ? 2 * (S & 1) + (S >> 1) : S & 1;
             if constexpr (M < F) {
-                if constexpr (!KR) asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(whole[S & 1][M]) : "v"(addr[S] + st), "i"(M * 32 * BK * 2));
+                if constexpr (!KR) asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(whole[slot][M]) : "v"(addr[S] + st), "i"(M * 32 * BK * 2));
                 else {
-                    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(half[S & 1][M][0]) : "v"(addr[M] + st), "i"(S * 16 * RB));
-                    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(half[S & 1][M][1]) : "v"(addr[M] + st), "i"(S * 16 * RB + 4 * RB));
+                    constexpr int off = (DUAL ? S & 1 : S) * 16 * RB;
+                    const unsigned a = (DUAL && S >= 2 ? addr[M] ^ 64u : addr[M]) + st;      // the second plane: two pairs on
+                    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(half[slot][M][0]) : "v"(a), "i"(off));
+                    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(half[slot][M][1]) : "v"(a), "i"(off + 4 * RB));
                 }
                 read<S, M + 1>(st);
             }
@@ -151,12 +164,13 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         }
     };
 
-    // Adds to acc the products of rows i0.. of A and j0.. of B over k in [kb, ke), kb a multiple of 64.  mask (MASKED): bit k & 63
+    // Adds to acc the products of rows i0.. of A and j0.. of B over k in [kb, ke), kb a multiple of 64.  (DUAL: one pair, and operands
+    // with k contiguous are zero behind ke up to a multiple of 32.)  mask (MASKED): bit k & 63
     // of word k >> 6 is set where A's row k counts.  Ends with every load landed and all waves past their last LDS read.
     __device__ static __forceinline__ void run(const GemmOperand& A, const GemmOperand& B, const GemmPairs& pairs, int i0, int j0, int kb, int ke,
                                                GemmMask mask, unsigned char* smem, Acc& acc) {
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const int nkt = (ke - kb + BK - 1) / BK, total = ke > kb ? nkt * pairs.n : 0;
+        const int nkt = (ke - kb + KT - 1) / KT, total = ke > kb ? nkt * pairs.n : 0;
         if (total <= 0) return;
         Loader<AKR, BI, NSA> la;
         Loader<BKR, BJ, NSB> lb;
@@ -174,7 +188,7 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         unsigned char* t_dst = smem;
         // the k-tile that is loaded next; past the end nothing is left of k and everything reads as zero
         auto tile_begin = [&](int st) __attribute__((always_inline)) {
-            const int k = kb + kt * BK;
+            const int k = kb + kt * KT;
             t_krem = issued < total ? ke - k : 0;
             pa = la.at((pairs.a >> (4 * seg)) & 15, k);
             pb = lb.at((pairs.b >> (4 * seg)) & 15, k);
@@ -192,23 +206,30 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         };
         auto arrived = [&](int slot) __attribute__((always_inline)) {
             __builtin_amdgcn_s_waitcnt(0xc07f);                // lgkmcnt(0)
-            ra.arrived(slot);
-            rb.arrived(slot);
+#pragma unroll
+            for (int p = 0; p < PL; ++p) {
+                ra.arrived(PL * slot + p);
+                rb.arrived(PL * slot + p);
+            }
         };
-        constexpr int NM = FI * FJ;                            // products of a k-step = places for loads
-        constexpr int PER = (NL + 2 * NM - 1) / (2 * NM);      // loads at a place: a k-tile's are issued within two k-steps
+        constexpr int NM = FI * FJ, NP = DUAL ? 3 * NM : NM;   // products of a k-step = places for loads
+        constexpr int PER = (NL + 2 * NP - 1) / (2 * NP);      // loads at a place: a k-tile's are issued within two k-steps
+        // DUAL: the small terms first
         auto products = [&](int slot, int first, bool issue) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < FI; ++i)
+            for (int p = 0; p < NP / NM; ++p)
 #pragma unroll
-                for (int j = 0; j < FJ; ++j) {
-                    Mma<E, 32>::run(ra.get(slot, i), rb.get(slot, j), acc[i][j]);
-                    if (issue) {
+                for (int i = 0; i < FI; ++i)
 #pragma unroll
-                        for (int q = 0; q < PER; ++q) issue_one((first + i * FJ + j) * PER + q);
+                    for (int j = 0; j < FJ; ++j) {
+                        if constexpr (DUAL) Mma<E, 32>::run(ra.get(2 * slot + (p == 0), i), rb.get(2 * slot + (p == 1), j), acc[i][j]);
+                        else Mma<E, 32>::run(ra.get(slot, i), rb.get(slot, j), acc[i][j]);
+                        if (issue) {
+#pragma unroll
+                            for (int q = 0; q < PER; ++q) issue_one((first + p * NM + i * FJ + j) * PER + q);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
                     }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
         };
 #pragma unroll
         for (int s = 0; s < STAGES; ++s) {
@@ -220,24 +241,35 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        ra.template read<0>(0); rb.template read<0>(0);
+        auto read = [&](auto k, unsigned stage) __attribute__((always_inline)) {
+            constexpr int S = decltype(k)::value;
+            ra.template read<S>(stage); rb.template read<S>(stage);
+            if constexpr (DUAL) { ra.template read<S + 2>(stage); rb.template read<S + 2>(stage); }
+        };
+        const std::integral_constant<int, 0> k0;
+        const std::integral_constant<int, 1> k1;
+        const std::integral_constant<int, 2> k2;
+        const std::integral_constant<int, 3> k3;
+        read(k0, 0);
         arrived(0);
         unsigned st = 0;
         int sn = 0;
         for (int t = 0; t < total; ++t) {
-            ra.template read<1>(st); rb.template read<1>(st);
+            read(k1, st);
             __builtin_amdgcn_sched_barrier(0);
             // the loads that are left of the k-tile begun under the last k-step of the iteration before (none in the first)
-            products(0, NM, t > 0);
+            products(0, NP, t > 0);
             arrived(1);
-            ra.template read<2>(st); rb.template read<2>(st);
-            __builtin_amdgcn_sched_barrier(0);
-            products(1, 0, false);
-            arrived(0);
-            ra.template read<3>(st); rb.template read<3>(st);
-            __builtin_amdgcn_sched_barrier(0);
-            products(0, 0, false);
-            arrived(1);                                        // this wave has read all of its stage
+            if constexpr (!DUAL) {
+                read(k2, st);
+                __builtin_amdgcn_sched_barrier(0);
+                products(1, 0, false);
+                arrived(0);
+                read(k3, st);
+                __builtin_amdgcn_sched_barrier(0);
+                products(0, 0, false);
+                arrived(1);
+            }                                                  // this wave has read all of its stage
             wait_vmcnt<(STAGES - 2) * NL>();                   // k-tile t + 1 landed (this wave's share)
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_barrier();
@@ -245,14 +277,14 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
             const int freed = sn;
             if (++sn == STAGES) sn = 0;
             st = (unsigned)(sn * STAGE);
-            ra.template read<0>(st); rb.template read<0>(st);  // (behind the last k-tile: zeros, not used)
+            read(k0, st);                                      // (behind the last k-tile: zeros, not used)
             tile_begin(freed);
             __builtin_amdgcn_sched_barrier(0);
             products(1, 0, true);
             arrived(0);
         }
 #pragma unroll
-        for (int i = NM * PER; i < NL; ++i) issue_one(i);      // what would have been issued under the next iteration: zeros
+        for (int i = NP * PER; i < NL; ++i) issue_one(i);      // what would have been issued under the next iteration: zeros
         wait_vmcnt<0>();
         asm volatile("" ::: "memory");
         __syncthreads();

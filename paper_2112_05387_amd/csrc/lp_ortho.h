@@ -12,13 +12,13 @@ struct NsProb {
     void* out;                          // orthogonalised matrix (src != null), or the parameters
     const float* grad; float *vel, *master;
     long ld_src, ld_out;
-    char *x0, *x1, *s, *b;              // planes: X before and after a step, X X^T, the polynomial in it
-    int rows, cols, r, c, ldr, ldc;     // as stored; shorter and longer side, and those rounded up to eight
+    char *x0, *x1, *s, *b;              // X before and after a step, X X^T, the polynomial in it
+    int rows, cols, r, c, ldr, ldc;     // as stored; shorter and longer side; elements of a row of S, B and of X: 32 of the first
+                                        // plane, the same 32 of the second, and so on, zeros behind the last
     int src_low, out_low;               // bf16
     int plain;                          // updated without orthogonalisation
     float lr, shrink;                   // the step taken, what is left of the parameters (1 - lr * weight decay)
-    int vec;                            // 16-byte accesses to the fp32 tensors
-    int pad_;
+    int vec, vec_out;                   // 16-byte accesses to what is read (grad, vel or src), to rows of out and master
 };
 
 // First block of every tensor in the launches over elements, over 64 x 64 pieces, over tiles of r x r and of r x c; behind

@@ -70,27 +70,53 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(const NsArgs a) {
             sum += (double)u * u;
         }
     };
-    if (P.src) {
+    constexpr int U = kNsElems / 1024;
+    if (P.vec && !P.plain) {
+        // four elements a thread and trip, all loads first
+        f32x4 g[U], v[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const size_t e = base + (size_t)(i * 256 + tid) * 4;
+            g[i] = f32x4{0.f, 0.f, 0.f, 0.f}; v[i] = g[i];
+            if (e + 4 > numel) continue;
+            if (P.src) {
+                if (P.src_low) {
+                    const u32x2 w = *reinterpret_cast<const u32x2*>(reinterpret_cast<const unsigned short*>(P.src) + e);
+                    g[i] = f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
+                } else g[i] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(P.src) + e);
+            } else {
+                g[i] = *reinterpret_cast<const f32x4*>(P.grad + e);
+                v[i] = *reinterpret_cast<const f32x4*>(P.vel + e);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const size_t e = base + (size_t)(i * 256 + tid) * 4;
+            if (e + 4 <= numel) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float u = g[i][q];
+                    if (!P.src) {
+                        v[i][q] = fmaf(a.momentum, v[i][q], g[i][q]);
+                        u = a.nesterov ? fmaf(a.momentum, v[i][q], g[i][q]) : v[i][q];
+                    }
+                    sum += (double)u * u;
+                }
+                if (!P.src) *reinterpret_cast<f32x4*>(P.vel + e) = v[i];
+            } else {
+                for (size_t t = e; t < numel; ++t) {
+                    if (P.src) { const float u = load_low(P.src, P.src_low, t); sum += (double)u * u; }
+                    else element(t, P.grad[t], P.vel[t], 0.f);
+                }
+            }
+        }
+    } else if (P.src) {
         for (int i = tid; i < kNsElems; i += 256) {
             const size_t e = base + i;
             if (e >= numel) break;
             const size_t row = e / P.cols;
             const float u = load_low(P.src, P.src_low, row * P.ld_src + (e - row * P.cols));
             sum += (double)u * u;
-        }
-    } else if (P.vec && !P.plain && base + kNsElems <= numel) {
-#pragma unroll
-        for (int i = 0; i < kNsElems / 1024; ++i) {
-            const size_t e = base + (size_t)(i * 256 + tid) * 4;
-            const f32x4 g = *reinterpret_cast<const f32x4*>(P.grad + e);
-            f32x4 v = *reinterpret_cast<const f32x4*>(P.vel + e);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                v[q] = fmaf(a.momentum, v[q], g[q]);
-                const float u = a.nesterov ? fmaf(a.momentum, v[q], g[q]) : v[q];
-                sum += (double)u * u;
-            }
-            *reinterpret_cast<f32x4*>(P.vel + e) = v;
         }
     } else {
         for (int i = tid; i < kNsElems; i += 256) {
@@ -143,17 +169,16 @@ __global__ __launch_bounds__(256) void ns_split_kernel(const NsArgs a) {
     const bool tall = P.rows > P.cols;
     // the piece as rows of X: row x0 + i, columns y0 + 2 j, y0 + 2 j + 1
     const int x0 = tall ? c0 : r0, y0 = tall ? r0 : c0;
-    unsigned* const hi = reinterpret_cast<unsigned*>(P.x0);
-    unsigned* const lo = hi + ((size_t)P.r * P.ldc >> 1);
+    unsigned* const out = reinterpret_cast<unsigned*>(P.x0);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int i = (tid >> 5) + 8 * k, j = 2 * (tid & 31);
-        if (x0 + i < P.r && y0 + j < P.ldc) {
+        if (x0 + i < P.r && 2 * (y0 + j) < P.ldc) {
             const float u0 = (tall ? t[j][i] : t[i][j]) * inv, u1 = (tall ? t[j + 1][i] : t[i][j + 1]) * inv;
             const unsigned h0 = f16_bits(u0), h1 = f16_bits(u1);
-            const size_t at = ((size_t)(x0 + i) * P.ldc + y0 + j) >> 1;
-            hi[at] = h0 | (h1 << 16);
-            lo[at] = f16_bits(u0 - f16_up(h0)) | (f16_bits(u1 - f16_up(h1)) << 16);
+            const size_t at = ((size_t)(x0 + i) * P.ldc + (y0 + j) / 32 * 64 + (j & 31)) >> 1;
+            out[at] = h0 | (h1 << 16);
+            out[at + 16] = f16_bits(u0 - f16_up(h0)) | (f16_bits(u1 - f16_up(h1)) << 16);
         }
     }
 }
@@ -162,14 +187,48 @@ enum NsMode { NS_GRAM, NS_POLY, NS_STEP, NS_LAST };
 
 // A 32 x 32 piece E[j][i] of O, i from i0 along the longer side: stored, or taken as the step of the parameters
 __device__ __forceinline__ void ns_answer(const NsProb& P, const float* E, bool tall, int i0, int j0, int lane) {
-    const int l = lane & 31, m0 = lane >> 5;
-    const int col = tall ? j0 + l : i0 + l, row0 = tall ? i0 : j0;
-    const int step = tall ? 1 : 33, at = tall ? l * 33 : l;
+    const int col0 = tall ? j0 : i0, row0 = tall ? i0 : j0;
+    const int step = tall ? 1 : 33, next = tall ? 33 : 1;         // from a row of the piece to the next, from a column
+    if (P.vec_out) {
+        const int col = col0 + 4 * (lane & 7), m0 = lane >> 3;
+        if (col >= P.cols) return;
+        f32x4 w[4];
+        u32x2 low[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {                             // all loads first
+            const int row = min(row0 + m0 + 8 * k, P.rows - 1);
+            const size_t e = (size_t)row * P.ld_out + col;
+            if (P.src) continue;
+            if (P.master) w[k] = *reinterpret_cast<const f32x4*>(P.master + e);
+            else if (P.out_low) low[k] = *reinterpret_cast<const u32x2*>(reinterpret_cast<const unsigned short*>(P.out) + e);
+            else w[k] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(P.out) + e);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int m = m0 + 8 * k;
+            f32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = E[m * step + (4 * (lane & 7) + e) * next];
+            if (!P.src) {
+                if (!P.master && P.out_low) w[k] = f32x4{__uint_as_float(low[k][0] << 16), __uint_as_float(low[k][0] & 0xffff0000u),
+                                                         __uint_as_float(low[k][1] << 16), __uint_as_float(low[k][1] & 0xffff0000u)};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(-P.lr, o[e], w[k][e] * P.shrink);
+            }
+            if (row0 + m >= P.rows) continue;
+            const size_t e = (size_t)(row0 + m) * P.ld_out + col;
+            if (P.master) *reinterpret_cast<f32x4*>(P.master + e) = o;
+            if (P.out_low) *reinterpret_cast<u32x2*>(reinterpret_cast<unsigned short*>(P.out) + e) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+            else *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(P.out) + e) = o;
+        }
+        return;
+    }
+    const int l = lane & 31, m0 = lane >> 5, col = col0 + l;
     if (col >= P.cols) return;
 #pragma unroll 4
     for (int m = m0; m < 32; m += 2) {
         if (row0 + m >= P.rows) break;
-        const float o = E[at + m * step];
+        const float o = E[m * step + l * next];
         const size_t e = (size_t)(row0 + m) * P.ld_out + col;
         if (P.src) store_low(P.out, P.out_low, e, o);
         else {
@@ -181,6 +240,19 @@ __device__ __forceinline__ void ns_answer(const NsProb& P, const float* E, bool 
     }
 }
 
+// a 32 x 32 piece in LDS, rows of 32 first and 32 second parts (128 bytes, a pitch of 144), to rows row0.. of `out`
+constexpr int kPiecePitch = 144, kPiece = 32 * kPiecePitch;
+__device__ __forceinline__ void ns_piece_out(const unsigned char* E, char* out, int ld, int row0, int rows, int col0, int lane) {
+    if (2 * col0 >= ld) return;
+    const int m0 = lane >> 3, c = lane & 7;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int m = m0 + 8 * k;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(E + m * kPiecePitch + c * 16);
+        if (row0 + m < rows) *reinterpret_cast<u32x4*>(out + ((size_t)(row0 + m) * ld + 2 * col0) * 2 + c * 16) = v;
+    }
+}
+
 template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm_kernel(const NsArgs a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const int x = blockIdx.x & 7, per = a.total >> 3, rem = a.total & 7;
@@ -189,14 +261,21 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
     const NsProb& P = a.p[pi];
     const int local = t - a.start[pi], r = P.r, ldr = P.ldr, ldc = P.ldc;
     constexpr bool STEP = MODE == NS_STEP || MODE == NS_LAST;
-    const int ni = STEP ? P.c : r, ti_n = (ni + T::BI - 1) / T::BI, tj_n = (r + T::BJ - 1) / T::BJ;
-    const int band = min(8, tj_n), full = band * ti_n, bd = local / full, w = min(band, tj_n - bd * band), in = local - bd * full;
-    const int ti = in / w, tj = bd * band + in - ti * w;
+    int ti, tj;
+    if constexpr (STEP) {
+        const int ti_n = (P.c + T::BI - 1) / T::BI, tj_n = (r + T::BJ - 1) / T::BJ;
+        const int band = min(8, tj_n), full = band * ti_n, bd = local / full, w = min(band, tj_n - bd * band), in = local - bd * full;
+        ti = in / w; tj = bd * band + in - ti * w;
+    } else {                                                      // symmetric: the tiles with ti <= tj, and what they mirror
+        tj = (int)((sqrtf(8.f * (float)local + 1.f) - 1.f) * 0.5f);
+        while (tj * (tj + 1) / 2 > local) --tj;
+        while ((tj + 1) * (tj + 2) / 2 <= local) ++tj;
+        ti = local - tj * (tj + 1) / 2;
+    }
     const int i0 = ti * T::BI, j0 = tj * T::BJ;
     char* const X = a.odd ? P.x1 : P.x0;
-    const size_t xplane = (size_t)r * ldc * 2, splane = (size_t)r * ldr * 2;
-    const GemmOperand ox = {X, xplane, ldc, STEP ? ldc : r}, os = {P.s, splane, ldr, r}, ob = {P.b, splane, ldr, r};
-    const GemmPairs three = {3, 0x100, 0x010};
+    const GemmOperand ox = {X, 0, ldc, STEP ? ldc : r}, os = {P.s, 0, ldr, r}, ob = {P.b, 0, ldr, r};
+    const GemmPairs one = {1, 0, 0};
     typename T::Acc acc;
 #pragma unroll
     for (int i = 0; i < T::TI / 32; ++i)
@@ -204,9 +283,9 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
         for (int j = 0; j < T::TJ / 32; ++j)
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
-    if constexpr (MODE == NS_GRAM) T::run(ox, ox, three, i0, j0, 0, ldc, (GemmMask)nullptr, smem, acc);
-    else if constexpr (MODE == NS_POLY) T::run(os, os, three, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
-    else T::run(ox, ob, three, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
+    if constexpr (MODE == NS_GRAM) T::run(ox, ox, one, i0, j0, 0, P.c, (GemmMask)nullptr, smem, acc);
+    else if constexpr (MODE == NS_POLY) T::run(os, os, one, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
+    else T::run(ox, ob, one, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / (T::BJ / T::TJ), wj = wave % (T::BJ / T::TJ);
@@ -233,67 +312,67 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
             }
         return;
     }
-    // planes of the result, 32 rows of the wave at a time through LDS, out as 16-byte pieces of rows
-    constexpr int PITCH = T::TI * 2 + 16, EP = 32 * PITCH, CPR = T::TI / 8, RPL = 64 / CPR;
+    // the two parts of the result, 32 x 32 at a time through LDS, from where they go out as whole cache lines
     constexpr float scale = MODE == NS_GRAM ? kScaleS / (kScaleX * kScaleX) : MODE == NS_POLY ? kC * kScaleB / (kScaleS * kScaleS) : 1.f / kScaleB;
     char* const out = MODE == NS_GRAM ? P.s : MODE == NS_POLY ? P.b : (a.odd ? P.x0 : P.x1);
-    const size_t oplane = MODE == NS_STEP ? xplane : splane;
-    const int ldo = MODE == NS_STEP ? ldc : ldr;
-    unsigned char* const E = smem + wave * (2 * EP);
-    const int c = lane % CPR, jr = lane / CPR;
+    const int ldo = STEP ? ldc : ldr;
+    unsigned char* const E = smem + wave * kPiece;
 #pragma unroll
-    for (int j = 0; j < FJ; ++j) {
-        const int jj = jb + j * 32 + lr;
+    for (int j = 0; j < FJ; ++j)
 #pragma unroll
-        for (int i = 0; i < FI; ++i)
+        for (int i = 0; i < FI; ++i) {
+            const int jj = jb + j * 32 + lr, jp = jb + j * 32, ip = ib + i * 32;
+            unsigned hb[16], lb[16];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int ii = ib + i * 32 + 8 * q + 4 * h;
+                const int ii = ip + 8 * q + 4 * h;
                 float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e] * scale;
                 if constexpr (MODE == NS_POLY) {
-                    if (jj < r && ii < ldr) {
-                        const char* const sp = P.s + ((size_t)jj * ldr + ii) * 2;
-                        const u32x2 s0 = *reinterpret_cast<const u32x2*>(sp), s1 = *reinterpret_cast<const u32x2*>(sp + splane);
+                    if (jj < r && 2 * ip < ldr) {
+                        const char* const sp = P.s + ((size_t)jj * ldr + 2 * ip + (ii - ip)) * 2;
+                        const u32x2 s0 = *reinterpret_cast<const u32x2*>(sp), s1 = *reinterpret_cast<const u32x2*>(sp + 64);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float sv = f16_up(s0[e >> 1] >> (16 * (e & 1))) + f16_up(s1[e >> 1] >> (16 * (e & 1)));
+                            const float sv = f16_up((s0[e >> 1] >> (16 * (e & 1))) & 0xffffu) + f16_up((s1[e >> 1] >> (16 * (e & 1))) & 0xffffu);
                             v[e] = fmaf(kB * (kScaleB / kScaleS), sv, v[e]);
                             if (ii + e == jj) v[e] += kA * kScaleB;
                         }
                     }
                 }
-                unsigned hb[4], lb[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { hb[e] = f16_bits(v[e]); lb[e] = f16_bits(v[e] - f16_up(hb[e])); }
-                unsigned char* const d = E + lr * PITCH + (i * 32 + 8 * q + 4 * h) * 2;
-                *reinterpret_cast<u32x2*>(d) = u32x2{hb[0] | (hb[1] << 16), hb[2] | (hb[3] << 16)};
-                *reinterpret_cast<u32x2*>(d + EP) = u32x2{lb[0] | (lb[1] << 16), lb[2] | (lb[3] << 16)};
+                for (int e = 0; e < 4; ++e) { hb[4 * q + e] = f16_bits(v[e]); lb[4 * q + e] = f16_bits(v[e] - f16_up(hb[4 * q + e])); }
+                unsigned char* const d = E + lr * kPiecePitch + (8 * q + 4 * h) * 2;
+                *reinterpret_cast<u32x2*>(d) = u32x2{hb[4 * q] | (hb[4 * q + 1] << 16), hb[4 * q + 2] | (hb[4 * q + 3] << 16)};
+                *reinterpret_cast<u32x2*>(d + 64) = u32x2{lb[4 * q] | (lb[4 * q + 1] << 16), lb[4 * q + 2] | (lb[4 * q + 3] << 16)};
             }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_s_waitcnt(0xc07f);
+            auto visible = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_s_waitcnt(0xc07f); };
+            visible();
+            ns_piece_out(E, out, ldo, jp, r, ip, lane);
+            visible();
+            if (!STEP && ti != tj) {
 #pragma unroll
-        for (int q = 0; q < 32 / RPL; ++q) {
-            const int row = q * RPL + jr, jo = jb + j * 32 + row, ii = ib + c * 8;
-            if (jo < r && ii < ldo) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    *reinterpret_cast<u32x4*>(out + k * oplane + ((size_t)jo * ldo + ii) * 2) = *reinterpret_cast<const u32x4*>(E + k * EP + row * PITCH + c * 16);
+                for (int q = 0; q < 16; ++q) {
+                    unsigned short* const d = reinterpret_cast<unsigned short*>(E + T::row(q, lane) * kPiecePitch + lr * 2);
+                    d[0] = (unsigned short)hb[q];
+                    d[32] = (unsigned short)lb[q];
+                }
+                visible();
+                ns_piece_out(E, out, ldo, ip, r, jp, lane);
+                visible();
             }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        __builtin_amdgcn_s_waitcnt(0xc07f);
-    }
 }
 
-template <bool AKR> using NBig = GemmTile<f16_t, AKR, false, 2, 4, 4, 2, 2>;
-template <bool AKR> using NMid = GemmTile<f16_t, AKR, false, 2, 2, 2, 2, 2>;
-template <bool AKR> using NSmall = GemmTile<f16_t, AKR, false, 2, 2, 1, 1, 4>;
+template <bool AKR> using NBig = GemmTile<f16_t, AKR, false, 2, 4, 4, 2, 2, false, true>;
+template <bool AKR> using NMid = GemmTile<f16_t, AKR, false, 2, 2, 2, 2, 2, false, true>;
+template <bool AKR> using NSmall = GemmTile<f16_t, AKR, false, 2, 2, 1, 1, 4, false, true>;
 
 template <class T, int MODE> hipError_t launch_gemm(const NsArgs& a, hipStream_t s) {
     static OncePerDevice once;
-    constexpr int lds = std::max(T::LDS, T::NW * 2 * 32 * (T::TI * 2 + 16));
+    constexpr int lds = T::LDS;
+    static_assert(T::NW * kPiece <= lds, "the way out fits into the stages");
     auto k = ns_gemm_kernel<T, MODE>;
     if (const hipError_t e = raise_lds_limit(once, {(const void*)k}, lds); e != hipSuccess) return e;
     hipLaunchKernelGGL(k, dim3(a.total), dim3(T::NT), lds, s, a);
