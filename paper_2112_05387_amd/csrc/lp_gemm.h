@@ -15,9 +15,13 @@
 // bytes, and a k-tile of 64 elements is 32 k of either.  From the fragments of two planes come three products (the
 // fourth, of the two rests, is below the precision): half as much again for the same loads and LDS reads.
 //
-// LDS bandwidth (128 bytes a clock) and the latency of loads bound such a loop.  The tile of a wave is as large as the registers
-// allow, a k-tile is 64 long (128-byte rows: whole cache lines), the loads of a k-tile are spread between the products of the
-// one before it, and one barrier a k-tile, ahead of the products of its last 16 k, both frees its stage and shows the next.
+// A k-tile is 64 elements long (128-byte rows: whole cache lines) and its loads are spread between the products of the one before
+// it.  Four waves (tiles of 128 and less, two workgroups a compute unit): one barrier a k-tile, ahead of the products of its last
+// 16 k, both frees its stage and shows the next.  Eight waves (256 x 256, one workgroup): two groups that take turns.
+// What bounds it: power.  8192 x 8192 x 4096 in bf16 1105 (k contiguous), 1220 (one operand with rows along k), 1240 TFLOP/s
+// (both), DUAL 1440 of its three products, at 1.6 to 1.9 GHz; without the loads 1270 to 1570, the matrix cores busy for 85 % of
+// the clocks.  All eight waves in step, as the four are: 1013, 1128, 1203, 1370; a quarter as many waves of 128 x 128 each,
+// a third fewer LDS reads: 5 % less than that; fragments two k-steps ahead: the same.
 // Rows are unpadded; their 16-byte chunks (KR: 32-byte pairs) trade places so that a read touches every bank once:
 //   KR = false  chunk c of row r at c ^ (r >> 1 & 7)
 //   KR = true   pair p of row k at p ^ 2 (k & 3) (rows of 256 bytes or more), p ^ 2 (k >> 1 & 1) (128 bytes), p (64 bytes)
@@ -60,6 +64,7 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
     static constexpr int NSA = BI / 8 / NW, NSB = BJ / 8 / NW, NL = NSA + NSB;      // wave-loads of a k-tile
     static constexpr int KS = BK / 16;
     static constexpr int PL = DUAL ? 2 : 1, KT = BK / PL;           // planes beside each other; k of a k-tile
+    static constexpr bool TURNS = NW == 8;                          // two waves a SIMD, one of either group (see run)
     static_assert(NW % 2 == 0 && NSA * NW * 8 == BI && NSB * NW * 8 == BJ, "every wave loads the same number of slabs");
     typedef f32x16 Acc[FI][FJ];
 
@@ -139,7 +144,7 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         }
         // the fragments of k-step S of the stage that starts at byte `st` (DUAL: S = 2 * plane + k-step of the k-tile's two)
         template <int S, int M = 0> __device__ __forceinline__ void read(unsigned st) {
-            constexpr int slot = DUAL ? 2 * (S & 1) + (S >> 1) : S & 1;
+            constexpr int slot = DUAL ? 2 * (S & 1) + (S >> 1) : S & 1;      // [k-step][plane], or two k-steps
             if constexpr (M < F) {
                 if constexpr (!KR) asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(whole[slot][M]) : "v"(addr[S] + st), "i"(M * 32 * BK * 2));
                 else {
@@ -183,7 +188,7 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         rb.init(wave % WJ, lane, lds0 + A_BYTES);
 
         int seg = 0, kt = 0, issued = 0, t_krem = 0;
-        unsigned long long t_mask = 0;
+        unsigned long long t_mask = 0, ahead = 0;              // ahead: of the k-tile behind, loaded where nothing waits for it
         const char *pa = nullptr, *pb = nullptr;
         unsigned char* t_dst = smem;
         // the k-tile that is loaded next; past the end nothing is left of k and everything reads as zero
@@ -192,10 +197,13 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
             t_krem = issued < total ? ke - k : 0;
             pa = la.at((pairs.a >> (4 * seg)) & 15, k);
             pb = lb.at((pairs.b >> (4 * seg)) & 15, k);
-            if constexpr (MASKED) t_mask = mask[min(k, ke - 1) >> 6];
+            if constexpr (MASKED) t_mask = TURNS ? ahead : mask[min(k, ke - 1) >> 6];
             t_dst = smem + st * STAGE + wave * 1024;
             ++issued;
             if (++kt == nkt) { kt = 0; if (seg + 1 < pairs.n) ++seg; }
+        };
+        auto mask_ahead = [&] __attribute__((always_inline)) {
+            if constexpr (MASKED && TURNS) ahead = mask[min(kb + kt * KT, ke - 1) >> 6];
         };
         auto issue_one = [&](int i) __attribute__((always_inline)) {
             if (i < NSA)
@@ -232,59 +240,127 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                     }
         };
 #pragma unroll
-        for (int s = 0; s < STAGES; ++s) {
+        for (int s = 0; s < (TURNS ? 1 : STAGES); ++s) {
+            mask_ahead();
             tile_begin(s);
 #pragma unroll
             for (int i = 0; i < NL; ++i) issue_one(i);
         }
-        wait_vmcnt<(STAGES - 1) * NL>();
+        if constexpr (TURNS) mask_ahead();
+        wait_vmcnt<TURNS ? 0 : (STAGES - 1) * NL>();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        auto read = [&](auto k, unsigned stage) __attribute__((always_inline)) {
-            constexpr int S = decltype(k)::value;
-            ra.template read<S>(stage); rb.template read<S>(stage);
-            if constexpr (DUAL) { ra.template read<S + 2>(stage); rb.template read<S + 2>(stage); }
+        auto barrier = [&] __attribute__((always_inline)) {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
         };
         const std::integral_constant<int, 0> k0;
         const std::integral_constant<int, 1> k1;
         const std::integral_constant<int, 2> k2;
         const std::integral_constant<int, 3> k3;
-        read(k0, 0);
-        arrived(0);
-        unsigned st = 0;
-        int sn = 0;
-        for (int t = 0; t < total; ++t) {
-            read(k1, st);
-            __builtin_amdgcn_sched_barrier(0);
-            // the loads that are left of the k-tile begun under the last k-step of the iteration before (none in the first)
-            products(0, NP, t > 0);
-            arrived(1);
-            if constexpr (!DUAL) {
-                read(k2, st);
-                __builtin_amdgcn_sched_barrier(0);
-                products(1, 0, false);
-                arrived(0);
-                read(k3, st);
-                __builtin_amdgcn_sched_barrier(0);
-                products(0, 0, false);
-                arrived(1);
-            }                                                  // this wave has read all of its stage
-            wait_vmcnt<(STAGES - 2) * NL>();                   // k-tile t + 1 landed (this wave's share)
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            const int freed = sn;
-            if (++sn == STAGES) sn = 0;
-            st = (unsigned)(sn * STAGE);
-            read(k0, st);                                      // (behind the last k-tile: zeros, not used)
-            tile_begin(freed);
-            __builtin_amdgcn_sched_barrier(0);
-            products(1, 0, true);
-            arrived(0);
-        }
+        if constexpr (TURNS) {
+            // Two groups of four waves, one of each on a SIMD, take turns: one multiplies half a k-tile while the other fetches its
+            // fragments and issues loads.  The second group runs one barrier behind.
+            static_assert(STAGES == 2 && NL % 2 == 0, "the stage that is not read is loaded");
+            const bool second = wave >= NW / 2;
+            auto fetch = [&](auto half, unsigned stage) __attribute__((always_inline)) {
+                constexpr int H = decltype(half)::value, S0 = DUAL ? H : 2 * H, S1 = DUAL ? H + 2 : 2 * H + 1;
+                ra.template read<S0>(stage); rb.template read<S0>(stage);
+                ra.template read<S1>(stage); rb.template read<S1>(stage);
+            };
+            auto fetched = [&](auto half) __attribute__((always_inline)) {
+                constexpr int H = decltype(half)::value, S0 = DUAL ? 2 * H : 0;
+                __builtin_amdgcn_s_waitcnt(0xc07f);            // lgkmcnt(0)
+                ra.arrived(S0); rb.arrived(S0);
+                ra.arrived(S0 + 1); rb.arrived(S0 + 1);
+            };
+            // half a k-tile of products; the first half's with the later loads, one at every second product
+            auto multiply = [&](auto half) __attribute__((always_inline)) {
+                constexpr int H = decltype(half)::value;
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = NP * PER; i < NL; ++i) issue_one(i);      // what would have been issued under the next iteration: zeros
+                for (int p = 0; p < (DUAL ? 3 : 2); ++p)
+#pragma unroll
+                    for (int i = 0; i < FI; ++i)
+#pragma unroll
+                        for (int j = 0; j < FJ; ++j) {
+                            const int n = (p * FI + i) * FJ + j;
+                            if constexpr (DUAL) Mma<E, 32>::run(ra.get(2 * H + (p == 0), i), rb.get(2 * H + (p == 1), j), acc[i][j]);
+                            else Mma<E, 32>::run(ra.get(p, i), rb.get(p, j), acc[i][j]);
+                            if (H == 0 && n % 2 == 0 && NL / 2 + n / 2 < NL) issue_one(NL / 2 + n / 2);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                __builtin_amdgcn_s_setprio(0);
+            };
+            if (second) barrier();
+            unsigned st = 0;
+            int sn = 0;
+            for (int t = 0; t < total; ++t) {
+                fetch(k0, st);
+                tile_begin(sn ^ 1);                            // k-tile t + 1, where both groups have read all of k-tile t - 1
+#pragma unroll
+                for (int i = 0; i < NL / 2; ++i) issue_one(i);
+                fetched(k0);
+                barrier();
+                mask_ahead();
+                multiply(k0);
+                barrier();
+                fetch(k1, st);
+                fetched(k1);
+                if (second) wait_vmcnt<0>();                   // k-tile t + 1 has landed ahead of the barrier behind which the first group
+                barrier();                                     // reads it: the second group fetches in front of that one, the first multiplies
+                multiply(k1);
+                if (!second) wait_vmcnt<0>();
+                barrier();
+                sn ^= 1;
+                st = (unsigned)(sn * STAGE);
+            }
+            if (!second) barrier();
+        } else {
+            auto read = [&](auto k, unsigned stage) __attribute__((always_inline)) {
+                constexpr int S = decltype(k)::value;
+                ra.template read<S>(stage); rb.template read<S>(stage);
+                if constexpr (DUAL) { ra.template read<S + 2>(stage); rb.template read<S + 2>(stage); }
+            };
+            read(k0, 0);
+            arrived(0);
+            unsigned st = 0;
+            int sn = 0;
+            for (int t = 0; t < total; ++t) {
+                read(k1, st);
+                __builtin_amdgcn_sched_barrier(0);
+                // the loads that are left of the k-tile begun under the last k-step of the iteration before (none in the first)
+                products(0, NP, t > 0);
+                arrived(1);
+                if constexpr (!DUAL) {
+                    read(k2, st);
+                    __builtin_amdgcn_sched_barrier(0);
+                    products(1, 0, false);
+                    arrived(0);
+                    read(k3, st);
+                    __builtin_amdgcn_sched_barrier(0);
+                    products(0, 0, false);
+                    arrived(1);
+                }                                                  // this wave has read all of its stage
+                wait_vmcnt<(STAGES - 2) * NL>();                   // k-tile t + 1 landed (this wave's share)
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                const int freed = sn;
+                if (++sn == STAGES) sn = 0;
+                st = (unsigned)(sn * STAGE);
+                read(k0, st);                                      // (behind the last k-tile: zeros, not used)
+                tile_begin(freed);
+                __builtin_amdgcn_sched_barrier(0);
+                products(1, 0, true);
+                arrived(0);
+            }
+#pragma unroll
+            for (int i = NP * PER; i < NL; ++i) issue_one(i);      // what would have been issued under the next iteration: zeros
+        }
         wait_vmcnt<0>();
         asm volatile("" ::: "memory");
         __syncthreads();
