@@ -3470,7 +3470,7 @@ namespace {
 struct OrthoPlan {
     std::vector<NsProb> p;
     std::vector<int> start[4];               // blocks of the launches: elements, pieces, tiles of r x r, of r x c
-    int cfg_sq = 2, cfg_step = 2;
+    int cfg_sq = NT_64, cfg_step = NT_64;
     size_t o_table = 0, o_norm = 0, bytes = 256;
     size_t table_words() const { return 4 * (p.size() + 1) + (4 * (p.size() + 1)) % 2 + p.size() * sizeof(NsProb) / 4; }
     size_t probs_word() const { return 4 * (p.size() + 1) + (4 * (p.size() + 1)) % 2; }
@@ -3488,21 +3488,24 @@ static lp_status ortho_plan(OrthoPlan& o) {
     const int n = (int)o.p.size();
     WsAlloc ws;
     o.o_table = ws.take(o.table_words() * 4);
-    // the largest tile that leaves every compute unit one
-    long sq[3] = {0, 0, 0}, up[3] = {0, 0, 0};
-    for (int c = 0; c < 3; ++c) {
-        int b;
-        ns_tile_size(c, &b);
+    // the tile that is fastest for all of them together: time goes with the length of the reduction as well, so that the longest count
+    double best_sq = 1e300, best_step = 1e300;
+    for (int c = 0; c < NT_COUNT; ++c) {
+        int bi, bj;
+        ns_tile_size(c, &bi, &bj);
+        long sq = 0, step = 0;
         for (const NsProb& q : o.p)
             if (!q.plain) {
-                const long r = (std::min(q.rows, q.cols) + b - 1) / b, l = (std::max(q.rows, q.cols) + b - 1) / b;
-                sq[c] += r * (r + 1) / 2; up[c] += r * l;
+                const int r = std::min(q.rows, q.cols), l = std::max(q.rows, q.cols);
+                sq += (long)div_up(r, bj) * (div_up(r, bj) + 1) / 2;
+                step += (long)div_up(r, bj) * div_up(l, bi);
             }
+        const double tq = ns_tile_time(c, sq), ts = ns_tile_time(c, step);
+        if (bi == bj && tq < best_sq) { best_sq = tq; o.cfg_sq = c; }
+        if (ts < best_step) { best_step = ts; o.cfg_step = c; }
     }
-    auto pick = [](const long* t) { return t[0] >= 192 ? 0 : t[1] >= 256 ? 1 : 2; };
-    o.cfg_sq = pick(sq); o.cfg_step = pick(up);
-    int bs, bu;
-    ns_tile_size(o.cfg_sq, &bs); ns_tile_size(o.cfg_step, &bu);
+    int bs, bi, bj;
+    ns_tile_size(o.cfg_sq, &bs, &bs); ns_tile_size(o.cfg_step, &bi, &bj);
     long total[4] = {0, 0, 0, 0};
     for (auto& s : o.start) s.assign(n + 1, 0);
     for (int i = 0; i < n; ++i) {
@@ -3510,7 +3513,7 @@ static lp_status ortho_plan(OrthoPlan& o) {
         q.r = std::min(q.rows, q.cols); q.c = std::max(q.rows, q.cols);
         q.ldr = div_up(q.r, 32) * 64; q.ldc = div_up(q.c, 32) * 64;
         const long here[4] = {((long)q.rows * q.cols + kNsElems - 1) / kNsElems, q.plain ? 0 : (long)div_up(q.rows, 64) * div_up(q.cols, 64),
-                              q.plain ? 0 : (long)div_up(q.r, bs) * (div_up(q.r, bs) + 1) / 2, q.plain ? 0 : (long)div_up(q.r, bu) * div_up(q.c, bu)};
+                              q.plain ? 0 : (long)div_up(q.r, bs) * (div_up(q.r, bs) + 1) / 2, q.plain ? 0 : (long)div_up(q.r, bj) * div_up(q.c, bi)};
         for (int k = 0; k < 4; ++k) { o.start[k][i] = (int)total[k]; total[k] += here[k]; }
         if (!q.plain) {
             const size_t x = (size_t)q.r * q.ldc * 2, s = (size_t)q.r * q.ldr * 2;

@@ -125,6 +125,7 @@ template <class T, int MODE, int NP, int WAVES> __global__ __launch_bounds__(T::
     const int kb = blockIdx.y * a.kchunk;
     T::run(a.w, a.x, a.pairs, i0, j0, kb, min(a.K, kb + a.kchunk), (GemmMask)nullptr, smem, acc);
 
+    if (T::idle()) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / (T::BJ / T::TJ), wj = wave % (T::BJ / T::TJ);
     const int lr = lane & 31, h = lane >> 5;
@@ -392,6 +393,7 @@ template <class T, int WAVES> __global__ __launch_bounds__(T::NT, WAVES) void ce
     const int kb = blockIdx.y * a.kchunk;
     T::run(a.a, a.b, a.pairs, i0, j0, kb, min(a.K, kb + a.kchunk), (GemmMask)a.mask, smem, acc);
 
+    if (T::idle()) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / (T::BJ / T::TJ), wj = wave % (T::BJ / T::TJ);
     const int lr = lane & 31, h = lane >> 5;
@@ -475,11 +477,11 @@ __global__ __launch_bounds__(256) void ce_zero_kernel(float* p, size_t n) {
     for (size_t t = (size_t)blockIdx.x * 256 + threadIdx.x; t < n; t += (size_t)gridDim.x * 256) p[t] = 0.f;
 }
 
-// tiles: big (one workgroup a compute unit), middle (two), small (many), few samples
+// tiles: big and middle (one workgroup a compute unit), small (two), few samples
 template <bool AKR, bool BKR, bool M> using TBig = GemmTile<bf16_t, AKR, BKR, 2, 4, 4, 2, 2, M>;
-template <bool AKR, bool BKR, bool M> using TMid = GemmTile<bf16_t, AKR, BKR, 2, 2, 2, 2, 2, M>;
-template <bool AKR, bool BKR, bool M> using TSmall = GemmTile<bf16_t, AKR, BKR, 2, 2, 1, 1, 4, M>;
-template <bool AKR, bool BKR, bool M> using TFew = GemmTile<bf16_t, AKR, BKR, 4, 1, 1, 1, 3, M>;
+template <bool AKR, bool BKR, bool M> using TMid = GemmTile<bf16_t, AKR, BKR, 2, 2, 2, 2, 4, M, false, true>;
+template <bool AKR, bool BKR, bool M> using TSmall = GemmTile<bf16_t, AKR, BKR, 2, 2, 1, 1, 4, M, false, true>;
+template <bool AKR, bool BKR, bool M> using TFew = GemmTile<bf16_t, AKR, BKR, 4, 1, 1, 1, 3, M, false, true>;
 
 template <class K, class A> hipError_t launch(K kernel, OncePerDevice& once, dim3 grid, int threads, int lds, hipStream_t s, const A& args) {
     if (const hipError_t e = raise_lds_limit(once, {(const void*)kernel}, lds); e != hipSuccess) return e;

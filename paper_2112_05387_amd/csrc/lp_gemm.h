@@ -57,8 +57,8 @@ typedef __attribute__((address_space(3))) void* gemm_lds_t;
 typedef const __attribute__((address_space(4))) unsigned long long* GemmMask;      // read by scalar loads
 typedef __attribute__((ext_vector_type(4))) short gemm_s16x4;
 
-template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGES, bool MASKED = false, bool DUAL = false> struct GemmTile {
-    static constexpr int BK = 64, NW = WI * WJ, NT = NW * 64;
+template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGES, bool MASKED = false, bool DUAL = false, bool LOADERS = false> struct GemmTile {
+    static constexpr int BK = 64, NW = WI * WJ, NT = NW * 64 * (LOADERS ? 2 : 1);
     static constexpr int TI = FI * 32, TJ = FJ * 32, BI = WI * TI, BJ = WJ * TJ;
     static constexpr int A_BYTES = BI * BK * 2, STAGE = (BI + BJ) * BK * 2, LDS = STAGES * STAGE;
     static constexpr int NSA = BI / 8 / NW, NSB = BJ / 8 / NW, NL = NSA + NSB;      // wave-loads of a k-tile
@@ -169,12 +169,17 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         }
     };
 
+    // waves that have no share of the result
+    __device__ static __forceinline__ bool idle() { return LOADERS && (int)threadIdx.x >= NW * 64; }
+
     // Adds to acc the products of rows i0.. of A and j0.. of B over k in [kb, ke), kb a multiple of 64.  (DUAL: one pair, and operands
     // with k contiguous are zero behind ke up to a multiple of 32.)  mask (MASKED): bit k & 63
     // of word k >> 6 is set where A's row k counts.  Ends with every load landed and all waves past their last LDS read.
     __device__ static __forceinline__ void run(const GemmOperand& A, const GemmOperand& B, const GemmPairs& pairs, int i0, int j0, int kb, int ke,
                                                GemmMask mask, unsigned char* smem, Acc& acc) {
-        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int tid = threadIdx.x, lane = tid & 63, number = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const bool loader = LOADERS && number >= NW;
+        const int wave = loader ? number - NW : number;
         const int nkt = (ke - kb + KT - 1) / KT, total = ke > kb ? nkt * pairs.n : 0;
         if (total <= 0) return;
         Loader<AKR, BI, NSA> la;
@@ -220,8 +225,10 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 rb.arrived(PL * slot + p);
             }
         };
-        constexpr int NM = FI * FJ, NP = DUAL ? 3 * NM : NM;   // products of a k-step = places for loads
-        constexpr int PER = (NL + 2 * NP - 1) / (2 * NP);      // loads at a place: a k-tile's are issued within two k-steps
+        constexpr int NM = FI * FJ, NP = DUAL ? 3 * NM : NM;   // products of a phase (a k-step) = places for loads
+        // The loads of a k-tile are issued between the products behind the barrier that frees its stage.  Two stages: as early as
+        // they go, one or more a place, as they have to land within the k-tile; more stages: evenly over a whole k-tile.
+        constexpr int PHASES = DUAL ? 2 : KS, PLACES = STAGES == 2 ? (NL < 2 * NP ? NL : 2 * NP) : PHASES * NP;
         // DUAL: the small terms first
         auto products = [&](int slot, int first, bool issue) __attribute__((always_inline)) {
 #pragma unroll
@@ -234,20 +241,23 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                         else Mma<E, 32>::run(ra.get(slot, i), rb.get(slot, j), acc[i][j]);
                         if (issue) {
 #pragma unroll
-                            for (int q = 0; q < PER; ++q) issue_one((first + p * NM + i * FJ + j) * PER + q);
+                            for (int q = 0; q < NL; ++q)
+                                if (q * PLACES / NL == first + p * NM + i * FJ + j) issue_one(q);
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
         };
+        if (!LOADERS || loader) {
 #pragma unroll
-        for (int s = 0; s < (TURNS ? 1 : STAGES); ++s) {
-            mask_ahead();
-            tile_begin(s);
+            for (int s = 0; s < (TURNS ? 1 : STAGES); ++s) {
+                mask_ahead();
+                tile_begin(s);
 #pragma unroll
-            for (int i = 0; i < NL; ++i) issue_one(i);
+                for (int i = 0; i < NL; ++i) issue_one(i);
+            }
+            if constexpr (TURNS) mask_ahead();
+            wait_vmcnt<TURNS ? 0 : (STAGES - 1) * NL>();
         }
-        if constexpr (TURNS) mask_ahead();
-        wait_vmcnt<TURNS ? 0 : (STAGES - 1) * NL>();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -264,7 +274,7 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         if constexpr (TURNS) {
             // Two groups of four waves, one of each on a SIMD, take turns: one multiplies half a k-tile while the other fetches its
             // fragments and issues loads.  The second group runs one barrier behind.
-            static_assert(STAGES == 2 && NL % 2 == 0, "the stage that is not read is loaded");
+            static_assert(STAGES == 2 && NL - NL / 2 <= (DUAL ? 3 : 2) * NM / 2, "the stage that is not read is loaded");
             const bool second = wave >= NW / 2;
             auto fetch = [&](auto half, unsigned stage) __attribute__((always_inline)) {
                 constexpr int H = decltype(half)::value, S0 = DUAL ? H : 2 * H, S1 = DUAL ? H + 2 : 2 * H + 1;
@@ -319,6 +329,18 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 st = (unsigned)(sn * STAGE);
             }
             if (!second) barrier();
+        } else if (loader) {
+            // A wave that issues a load stands still for some 30 clocks, and where it is the only one of its SIMD the matrix core does so
+            // too: here the loads have waves of their own.
+            int sn = 0;
+            for (int t = 0; t < total; ++t) {
+                wait_vmcnt<(STAGES - 2) * NL>();               // k-tile t + 1 landed
+                barrier();                                     // ... and k-tile t is read
+                tile_begin(sn);
+#pragma unroll
+                for (int i = 0; i < NL; ++i) issue_one(i);
+                if (++sn == STAGES) sn = 0;
+            }
         } else {
             auto read = [&](auto k, unsigned stage) __attribute__((always_inline)) {
                 constexpr int S = decltype(k)::value;
@@ -332,20 +354,20 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
             for (int t = 0; t < total; ++t) {
                 read(k1, st);
                 __builtin_amdgcn_sched_barrier(0);
-                // the loads that are left of the k-tile begun under the last k-step of the iteration before (none in the first)
-                products(0, NP, t > 0);
+                // (in the first iteration all of the stages' loads are under way)
+                products(0, NP, !LOADERS && t > 0);
                 arrived(1);
                 if constexpr (!DUAL) {
                     read(k2, st);
                     __builtin_amdgcn_sched_barrier(0);
-                    products(1, 0, false);
+                    products(1, 2 * NP, !LOADERS && t > 0);
                     arrived(0);
                     read(k3, st);
                     __builtin_amdgcn_sched_barrier(0);
-                    products(0, 0, false);
+                    products(0, 3 * NP, !LOADERS && t > 0);
                     arrived(1);
-                }                                                  // this wave has read all of its stage
-                wait_vmcnt<(STAGES - 2) * NL>();                   // k-tile t + 1 landed (this wave's share)
+                }                                              // this wave has read all of its stage
+                if constexpr (!LOADERS) wait_vmcnt<(STAGES - 2) * NL>();      // k-tile t + 1 landed (this wave's share)
                 asm volatile("" ::: "memory");
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
@@ -353,13 +375,14 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 if (++sn == STAGES) sn = 0;
                 st = (unsigned)(sn * STAGE);
                 read(k0, st);                                      // (behind the last k-tile: zeros, not used)
-                tile_begin(freed);
+                if constexpr (!LOADERS) tile_begin(freed);
                 __builtin_amdgcn_sched_barrier(0);
-                products(1, 0, true);
+                products(1, 0, !LOADERS);
                 arrived(0);
             }
 #pragma unroll
-            for (int i = NP * PER; i < NL; ++i) issue_one(i);      // what would have been issued under the next iteration: zeros
+            for (int q = 0; q < NL; ++q)                       // what would have been issued in the next iteration: zeros
+                if (!LOADERS && q * PLACES / NL >= NP) issue_one(q);
         }
         wait_vmcnt<0>();
         asm volatile("" ::: "memory");

@@ -36,9 +36,12 @@ struct NsArgs {
 
 struct NsChunk { unsigned* dst; int words; unsigned w[960]; };
 
-constexpr int kNsElems = 8192;          // elements of a block of the launch over elements
+constexpr int kNsElems = 4096;          // elements of a block of the launch over elements
 
-void ns_tile_size(int cfg, int* b);     // 0: 256, 1: 128, 2: 64
+// Tiles of a step (i: longer side, j: shorter side) and of the symmetric products, and the tile that is fastest for `tiles(cfg)` of them
+enum NsTile { NT_256 = 0, NT_256x320, NT_128, NT_64, NT_COUNT };
+void ns_tile_size(int cfg, int* bi, int* bj);
+double ns_tile_time(int cfg, long tiles);
 hipError_t launch_ns_put(const NsChunk& c, hipStream_t s);
 hipError_t launch_ns_norm(const NsArgs& a, hipStream_t s);
 hipError_t launch_ns_split(const NsArgs& a, hipStream_t s);

@@ -185,24 +185,25 @@ __global__ __launch_bounds__(256) void ns_split_kernel(const NsArgs a) {
 
 enum NsMode { NS_GRAM, NS_POLY, NS_STEP, NS_LAST };
 
-// A 32 x 32 piece E[j][i] of O, i from i0 along the longer side: stored, or taken as the step of the parameters
-__device__ __forceinline__ void ns_answer(const NsProb& P, const float* E, bool tall, int i0, int j0, int lane) {
-    const int col0 = tall ? j0 : i0, row0 = tall ? i0 : j0;
+// A 32 x 32 piece of O, i from i0 along the longer side: what it is the step of is requested before its values lie in LDS.
+struct NsOld { f32x4 w[4]; u32x2 low[4]; };
+__device__ __forceinline__ void ns_request(const NsProb& P, NsOld& old, int row0, int col0, int lane) {
+    if (P.src || !P.vec_out) return;
+    const int col = min(col0 + 4 * (lane & 7), P.cols - 4);       // (rows and columns beyond the last: read, not used)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const size_t e = (size_t)min(row0 + (lane >> 3) + 8 * k, P.rows - 1) * P.ld_out + col;
+        if (P.master) old.w[k] = *reinterpret_cast<const f32x4*>(P.master + e);
+        else if (P.out_low) old.low[k] = *reinterpret_cast<const u32x2*>(reinterpret_cast<const unsigned short*>(P.out) + e);
+        else old.w[k] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(P.out) + e);
+    }
+}
+// ... E[j][i] in LDS: stored, or taken as the step of the parameters
+__device__ __forceinline__ void ns_answer(const NsProb& P, const NsOld& old, const float* E, bool tall, int row0, int col0, int lane) {
     const int step = tall ? 1 : 33, next = tall ? 33 : 1;         // from a row of the piece to the next, from a column
     if (P.vec_out) {
         const int col = col0 + 4 * (lane & 7), m0 = lane >> 3;
         if (col >= P.cols) return;
-        f32x4 w[4];
-        u32x2 low[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {                             // all loads first
-            const int row = min(row0 + m0 + 8 * k, P.rows - 1);
-            const size_t e = (size_t)row * P.ld_out + col;
-            if (P.src) continue;
-            if (P.master) w[k] = *reinterpret_cast<const f32x4*>(P.master + e);
-            else if (P.out_low) low[k] = *reinterpret_cast<const u32x2*>(reinterpret_cast<const unsigned short*>(P.out) + e);
-            else w[k] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(P.out) + e);
-        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int m = m0 + 8 * k;
@@ -210,10 +211,11 @@ __device__ __forceinline__ void ns_answer(const NsProb& P, const float* E, bool 
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = E[m * step + (4 * (lane & 7) + e) * next];
             if (!P.src) {
-                if (!P.master && P.out_low) w[k] = f32x4{__uint_as_float(low[k][0] << 16), __uint_as_float(low[k][0] & 0xffff0000u),
-                                                         __uint_as_float(low[k][1] << 16), __uint_as_float(low[k][1] & 0xffff0000u)};
+                f32x4 w = old.w[k];
+                if (!P.master && P.out_low) w = f32x4{__uint_as_float(old.low[k][0] << 16), __uint_as_float(old.low[k][0] & 0xffff0000u),
+                                                      __uint_as_float(old.low[k][1] << 16), __uint_as_float(old.low[k][1] & 0xffff0000u)};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = fmaf(-P.lr, o[e], w[k][e] * P.shrink);
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(-P.lr, o[e], w[e] * P.shrink);
             }
             if (row0 + m >= P.rows) continue;
             const size_t e = (size_t)(row0 + m) * P.ld_out + col;
@@ -232,8 +234,8 @@ __device__ __forceinline__ void ns_answer(const NsProb& P, const float* E, bool 
         const size_t e = (size_t)(row0 + m) * P.ld_out + col;
         if (P.src) store_low(P.out, P.out_low, e, o);
         else {
-            const float old = P.master ? P.master[e] : load_low(P.out, P.out_low, e);
-            const float w = fmaf(-P.lr, o, old * P.shrink);
+            const float was = P.master ? P.master[e] : load_low(P.out, P.out_low, e);
+            const float w = fmaf(-P.lr, o, was * P.shrink);
             if (P.master) P.master[e] = w;
             store_low(P.out, P.out_low, e, w);
         }
@@ -287,6 +289,7 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
     else if constexpr (MODE == NS_POLY) T::run(os, os, one, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
     else T::run(ox, ob, one, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
 
+    if (T::idle()) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / (T::BJ / T::TJ), wj = wave % (T::BJ / T::TJ);
     const int lr = lane & 31, h = lane >> 5;
@@ -298,18 +301,29 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
         float* const E = reinterpret_cast<float*>(smem) + wave * (32 * 33);
         const bool tall = P.rows > P.cols;
         constexpr float back = 1.f / (kScaleB * kScaleX);
+        auto place = [&](int n, int& row0, int& col0) __attribute__((always_inline)) {
+            const int ip = ib + (n % FI) * 32, jp = jb + (n / FI) * 32;
+            row0 = tall ? ip : jp; col0 = tall ? jp : ip;
+        };
+        NsOld old[2];
+        int row0, col0;
+        place(0, row0, col0);
+        ns_request(P, old[0], row0, col0, lane);
 #pragma unroll
-        for (int j = 0; j < FJ; ++j)
-#pragma unroll
-            for (int i = 0; i < FI; ++i) {
-#pragma unroll
-                for (int q = 0; q < 16; ++q) E[lr * 33 + T::row(q, lane)] = acc[i][j][q] * back;
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                __builtin_amdgcn_s_waitcnt(0xc07f);
-                ns_answer(P, E, tall, ib + i * 32, jb + j * 32, lane);
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                __builtin_amdgcn_s_waitcnt(0xc07f);
+        for (int n = 0; n < FI * FJ; ++n) {
+            if (n + 1 < FI * FJ) {
+                place(n + 1, row0, col0);
+                ns_request(P, old[(n + 1) & 1], row0, col0, lane);
             }
+#pragma unroll
+            for (int q = 0; q < 16; ++q) E[lr * 33 + T::row(q, lane)] = acc[n % FI][n / FI][q] * back;
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            place(n, row0, col0);
+            ns_answer(P, old[n & 1], E, tall, row0, col0, lane);
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+        }
         return;
     }
     // the two parts of the result, 32 x 32 at a time through LDS, from where they go out as whole cache lines
@@ -366,8 +380,9 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
 }
 
 template <bool AKR> using NBig = GemmTile<f16_t, AKR, false, 2, 4, 4, 2, 2, false, true>;
-template <bool AKR> using NMid = GemmTile<f16_t, AKR, false, 2, 2, 2, 2, 2, false, true>;
-template <bool AKR> using NSmall = GemmTile<f16_t, AKR, false, 2, 2, 1, 1, 4, false, true>;
+template <bool AKR> using NWide = GemmTile<f16_t, AKR, false, 4, 2, 2, 5, 2, false, true>;
+template <bool AKR> using NMid = GemmTile<f16_t, AKR, false, 2, 2, 2, 2, 4, false, true, true>;
+template <bool AKR> using NSmall = GemmTile<f16_t, AKR, false, 2, 2, 1, 1, 4, false, true, true>;
 
 template <class T, int MODE> hipError_t launch_gemm(const NsArgs& a, hipStream_t s) {
     static OncePerDevice once;
@@ -380,14 +395,29 @@ template <class T, int MODE> hipError_t launch_gemm(const NsArgs& a, hipStream_t
 }
 template <bool AKR, int MODE> hipError_t launch_mode(const NsArgs& a, int cfg, hipStream_t s) {
     if (a.total <= 0) return hipSuccess;
-    if (cfg == 0) return launch_gemm<NBig<AKR>, MODE>(a, s);
-    if (cfg == 1) return launch_gemm<NMid<AKR>, MODE>(a, s);
-    return launch_gemm<NSmall<AKR>, MODE>(a, s);
+    if constexpr (AKR)
+        if (cfg == NT_256x320) return launch_gemm<NWide<AKR>, MODE>(a, s);
+    switch (cfg) {
+        case NT_256: return launch_gemm<NBig<AKR>, MODE>(a, s);
+        case NT_128: return launch_gemm<NMid<AKR>, MODE>(a, s);
+        default: return launch_gemm<NSmall<AKR>, MODE>(a, s);
+    }
 }
 
 }  // namespace
 
-void ns_tile_size(int cfg, int* b) { *b = cfg == 0 ? 256 : cfg == 1 ? 128 : 64; }
+void ns_tile_size(int cfg, int* bi, int* bj) {
+    static const int d[NT_COUNT][2] = {{256, 256}, {256, 320}, {128, 128}, {64, 64}};
+    *bi = d[cfg][0]; *bj = d[cfg][1];
+}
+
+// Time of `tiles` tiles, in microseconds at 8192 k: the rounds that fill the chip (`slots` workgroups at once), and the last one by how
+// full it is.  Measured: 256 x 256 430 a round, 256 x 320 530, 128 x 128 118 (64 tiles) to 173, 64 x 64 67 (256 tiles) to 227 (1024).
+double ns_tile_time(int cfg, long tiles) {
+    static const struct { int slots; double some, full; } t[NT_COUNT] = {{256, 330, 430}, {256, 410, 530}, {256, 100, 173}, {512, 30, 115}};
+    const long rounds = tiles / t[cfg].slots, rest = tiles - rounds * t[cfg].slots;
+    return (double)rounds * t[cfg].full + (rest ? t[cfg].some + (t[cfg].full - t[cfg].some) * (double)rest / t[cfg].slots : 0.0);
+}
 
 hipError_t launch_ns_put(const NsChunk& c, hipStream_t s) {
     hipLaunchKernelGGL(ns_put_kernel, dim3(1), dim3(256), 0, s, c);
