@@ -3204,21 +3204,25 @@ static TilePlan tile_plan(int cfg, int I, int J, int K, int slices) {
     t.slices = std::max(1, div_up(K, t.kchunk));
     return t;
 }
-// Largest tile that still gives the chip's 256 compute units something to do.
-static int tile_cfg(int I, int J, bool big) {
-    const long t256 = (long)div_up(I, 256) * div_up(J, 256), t128 = (long)div_up(I, 128) * div_up(J, 128);
-    if (J <= 32) return 3;
-    if (big && t256 >= 192) return 0;
-    return t128 >= 256 ? 1 : 2;
-}
-// A gradient product: cut along the reduction where its tiles are few, in pieces of at least four k-tiles.
-static TilePlan grad_plan(int I, int J, int K, int pairs, bool few_cols, bool may_cut) {
-    int cfg = tile_cfg(I, J, true);
-    if (cfg == 3 && !few_cols) cfg = 2;
-    TilePlan t = tile_plan(cfg, I, J, K, 1);
-    const int want = cfg == 2 || cfg == 3 ? 768 : 512, tiles = t.ti * t.tj;
-    if (may_cut && tiles * 2 <= want) t = tile_plan(cfg, I, J, K, std::max(1, std::min(want / tiles, div_up(K, 64) * pairs / 4)));
-    return t;
+// The fastest way to cut a product: tile (from `first` on; few: the one for up to 32 columns too) and pieces of the reduction, whose
+// partial results are written and read once more.
+static TilePlan best_plan(int I, int J, int K, int pairs, int first, bool few, bool may_cut, double* time = nullptr) {
+    TilePlan best = tile_plan(2, I, J, K, 1);
+    double least = 1e300;
+    for (int cfg = first; cfg < 4; ++cfg) {
+        if (cfg == 3 && !few) continue;
+        int want = 1;
+        for (int n = 1; n <= 1024; n = std::max(n + 1, n * 5 / 4)) {
+            if (n < want) continue;
+            const TilePlan t = tile_plan(cfg, I, J, K, n);
+            want = t.slices + 1;
+            const double ms = ce_tile_time(cfg, (long)t.ti * t.tj * t.slices, t.kchunk / 64 * pairs) + (t.slices > 1 ? 1.0 + (double)t.slices * I * J * 8 / 4e6 : 0.0);
+            if (ms < least) { least = ms; best = t; }
+            if (!may_cut || t.slices * 64 >= K || (long)t.ti * t.tj * t.slices > 4096) break;
+        }
+    }
+    if (time) *time = least;
+    return best;
 }
 
 struct CePlan {
@@ -3228,7 +3232,7 @@ struct CePlan {
     GemmPairs logits, dx, dw;
     TilePlan tl, tx, tw;
     int piece, pieces, ldv;                  // classes of a piece of the probabilities
-    size_t o_x, o_w, o_partial, o_slices, o_bsum, o_bcnt, o_ticket, o_mask, o_count, o_prob, o_dx, o_dw, o_colsum, bytes;
+    size_t o_x, o_w, o_partial, o_slices, o_bsum, o_bcnt, o_mask, o_count, o_prob, o_dx, o_dw, o_colsum, bytes;
     int parts, colparts;
 };
 
@@ -3252,13 +3256,15 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     const GemmPairs one{1, 0, 0}, six{6, 0x201100, 0x021010};
     p.logits = low ? one : six; p.dx = p.logits; p.dw = low ? GemmPairs{2, 0, 0x10} : six;
 
-    int cfg = tile_cfg(p.V, p.N, true);
-    if (cfg == 0 && !low && backward) cfg = 1;                   // three planes of a 256 x 256 tile do not fit into LDS
-    p.tl = tile_plan(cfg, p.V, std::max(1, p.N), p.K, 1);
+    // logits: by tiles that finish their rows, or cut along the channels, with the softmax as a pass of its own (some 8 us).  Three
+    // planes of a 256 x 256 tile do not fit into LDS.
+    double whole, cut;
+    const int N1 = std::max(1, p.N), first = low || !backward ? 0 : 1;
+    p.tl = best_plan(p.V, N1, p.K, p.logits.n, first, p.N <= 32, false, &whole);
+    const TilePlan tc = best_plan(p.V, N1, p.K, p.logits.n, 2, p.N <= 32, true, &cut);
+    p.cut = cut + 8.0 < whole && (size_t)tc.slices * N1 * p.V <= ((size_t)8 << 20);
+    if (p.cut) p.tl = tc;
     if ((long)p.tl.ti * p.tl.tj > (1l << 30)) return fail(LP_ERR_SHAPE, "%d rows x %d classes in one call", p.N, p.V);
-    const int tiles = p.tl.ti * p.tl.tj;
-    p.cut = cfg >= 2 && tiles < 128;
-    if (p.cut) p.tl = tile_plan(cfg, p.V, std::max(1, p.N), p.K, std::max(1, std::min(512 / tiles, div_up(p.K, 64) * p.logits.n / 4)));
     int bi, bj, wi, wj;
     ce_tile_size(p.tl.cfg, &bi, &bj, &wi, &wj);
     p.parts = p.tl.ti * wi;
@@ -3280,12 +3286,11 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     p.o_slices = p.cut ? ws.take((size_t)p.tl.slices * N * V8 * 4) : 0;
     if (!backward) {
         p.o_partial = p.cut ? 0 : ws.take(N * p.parts * sizeof(float2));
-        p.o_bsum = ws.take((N + 3) / 4 * 4);
-        p.o_bcnt = ws.take((N + 3) / 4 * 4);
-        p.o_ticket = ws.take(4);
+        p.o_bsum = ws.take(N * 4);
+        p.o_bcnt = ws.take(N * 4);
     } else {
-        p.tx = grad_plan(p.C, std::max(1, p.N), p.piece, p.dx.n, true, true);
-        p.tw = grad_plan(p.C, p.piece, std::max(1, p.N), p.dw.n, false, p.pieces == 1);
+        p.tx = best_plan(p.C, N1, p.piece, p.dx.n, 0, p.N <= 32, true);
+        p.tw = best_plan(p.C, p.piece, N1, p.dw.n, 0, false, p.pieces == 1);
         p.o_mask = ws.take((N + 63) / 64 * 8);
         p.o_count = ws.take(4);
         p.o_prob = ws.take((size_t)p.nprob * 2 * N * p.ldv);
@@ -3362,7 +3367,6 @@ lp_status lp_linear_ce_forward(const lp_linear_ce_desc* d, void* stream, const v
     GemmOperand X, W;
     if ((st = ce_operands(p, d->dtype, features, weight, ws, X, W, s)) != LP_OK) return st;
     CeLogits a = ce_logits(p, X, W, bias, 0, p.V);
-    a.ticket = (int*)(ws + p.o_ticket);
     CeRows r;
     memset(&r, 0, sizeof(r));
     if (p.cut) {
@@ -3377,7 +3381,7 @@ lp_status lp_linear_ce_forward(const lp_linear_ce_desc* d, void* stream, const v
     if (st != LP_OK) return st;
     r.N = p.N; r.V = p.V; r.K = p.K; r.labels = labels; r.bias = bias; r.w = W; r.x = X; r.pairs = p.logits;
     r.lse = lse; r.row_loss = row_loss; r.loss = loss;
-    r.bsum = (float*)(ws + p.o_bsum); r.bcnt = (int*)(ws + p.o_bcnt); r.ticket = (int*)(ws + p.o_ticket);
+    r.bsum = (float*)(ws + p.o_bsum); r.bcnt = (int*)(ws + p.o_bcnt);
     return hip_status(launch_ce_rows(r, s));
 }
 
@@ -3402,7 +3406,6 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
     if ((st = ce_operands(p, d->dtype, features, weight, ws, X, W, s)) != LP_OK) return st;
     unsigned long long* const mask = (unsigned long long*)(ws + p.o_mask);
     int* const count = (int*)(ws + p.o_count);
-    if ((st = hip_status(launch_ce_labels(labels, p.N, p.V, mask, count, s))) != LP_OK) return st;
     char* const prob = ws + p.o_prob;
     const size_t pplane = (size_t)p.N * p.ldv * 2;
     GemmOperand P{prob, pplane, p.ldv, 0};
@@ -3415,13 +3418,13 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
     for (int v0 = 0, piece = 0; piece < p.pieces; ++piece, v0 += p.piece) {
         const int V = std::min(p.piece, p.V - v0);
         CeLogits a = ce_logits(p, X, W, bias, v0, V);
-        a.lse = lse; a.labels = labels; a.prob = prob; a.pplane = pplane; a.ldv = p.ldv;
+        a.lse = lse; a.labels = labels; a.mask = mask; a.count = count; a.prob = prob; a.pplane = pplane; a.ldv = p.ldv;
         if (p.cut) {
             a.slices = (float*)(ws + p.o_slices); a.slice = (size_t)p.N * a.ldv;
             CeRows r;
             memset(&r, 0, sizeof(r));
             r.N = p.N; r.V = p.V; r.labels = labels; r.bias = bias; r.slices = a.slices; r.slice = a.slice; r.nslices = p.tl.slices; r.ldv = a.ldv;
-            r.lse = const_cast<float*>(lse);
+            r.lse = const_cast<float*>(lse); r.mask = mask; r.count = count;
             st = hip_status(launch_ce_slices(a, p.tl.slices, p.tl.cfg, s));
             if (st == LP_OK) st = hip_status(launch_ce_prob(r, (unsigned short*)prob, pplane, p.nprob, s));
         } else {
@@ -3452,7 +3455,7 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
             if ((st = hip_status(launch_ce_dx(g, t.slices, t.cfg, s))) != LP_OK) return st;
         }
         // the bias of this piece: with the last one beside the other sums
-        f.blocks_b = dbias ? div_up(V, 64) : 0; f.V = V; f.dbias = dbias ? dbias + v0 : nullptr;
+        f.blocks_b = dbias ? div_up(V, 32) : 0; f.V = V; f.dbias = dbias ? dbias + v0 : nullptr;
         if (piece + 1 < p.pieces && (st = hip_status(launch_ce_finish(f, d->dtype, s))) != LP_OK) return st;
     }
     f.x = CeSum{(float*)(ws + p.o_dx), (size_t)p.N * p.K, p.tx.slices, p.K, dfeatures, (size_t)p.lddx, p.N, p.C};

@@ -14,7 +14,7 @@ struct CeLogits {
     int V, N, v0, V_all;
     int tiles_i, tiles_j, band;
     const float* bias;                  // of the piece, or null
-    int* ticket;                        // set to zero for the kernel behind this one, or null
+    unsigned long long* mask; int* count;    // probabilities: which rows count, and how many do, are found beside them
     float2* partial; int parts;         // statistics: [N][parts] (maximum, sum), base 2
     float* slices; size_t slice;        // partial logits: [slices][N][ldv]
     int ldv;                            // row length of slices / prob, a multiple of 8
@@ -30,7 +30,8 @@ struct CeRows {
     const float* slices; size_t slice; int nslices, ldv;
     GemmOperand w, x; GemmPairs pairs;
     float *lse, *row_loss, *loss;
-    float* bsum; int* bcnt; int* ticket;
+    float* bsum; int* bcnt;             // of every workgroup
+    unsigned long long* mask; int* count;
 };
 // out[j][i] (+)= sum_k a[k][i] * b[..]; i channels, j samples or classes
 struct CeGrad {
@@ -56,8 +57,8 @@ struct CeFinish {
 
 // tiles: 0 256 x 256, 1 128 x 128, 2 64 x 64, 3 128 x 32 (few samples); waves along either side
 void ce_tile_size(int cfg, int* bi, int* bj, int* wi, int* wj);
+double ce_tile_time(int cfg, long blocks, int ktiles);
 hipError_t launch_ce_pack(const void* src, long ld_src, int rows, int cols, int dtype, void* dst, size_t plane, int ld, hipStream_t s);
-hipError_t launch_ce_labels(const int* labels, int N, int V, unsigned long long* mask, int* count, hipStream_t s);
 hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s);
 hipError_t launch_ce_prob_tiles(const CeLogits& a, int planes, int cfg, hipStream_t s);
 hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t s);

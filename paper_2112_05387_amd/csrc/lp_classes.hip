@@ -83,12 +83,11 @@ template <class T, int NP> __global__ __launch_bounds__(256) void ce_pack_kernel
 
 __device__ __forceinline__ bool is_class(int y, int V) { return (unsigned)y < (unsigned)V; }
 
-// bit n & 63 of word n >> 6: row n counts; and how many do.  One workgroup.
-__global__ __launch_bounds__(1024) void ce_labels_kernel(const int* __restrict__ labels, int N, int V, unsigned long long* __restrict__ mask, int* __restrict__ count) {
-    __shared__ int s[16];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+// bit n & 63 of word n >> 6: row n counts; and how many do.  By one workgroup, beside those that form the probabilities.
+__device__ __forceinline__ void ce_labels(const int* __restrict__ labels, int N, int V, unsigned long long* __restrict__ mask, int* __restrict__ count, int* s) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, nw = blockDim.x >> 6;
     int c = 0;
-    for (int n0 = wave * 64; n0 < N; n0 += 1024) {
+    for (int n0 = wave * 64; n0 < N; n0 += 64 * nw) {
         const int n = n0 + lane;
         const unsigned long long m = __ballot(n < N && is_class(labels[n < N ? n : 0], V));
         c += __popcll(m);
@@ -98,7 +97,7 @@ __global__ __launch_bounds__(1024) void ce_labels_kernel(const int* __restrict__
     __syncthreads();
     if (threadIdx.x == 0) {
         int t = 0;
-        for (int i = 0; i < 16; ++i) t += s[i];
+        for (int i = 0; i < nw; ++i) t += s[i];
         *count = t;
     }
 }
@@ -111,7 +110,8 @@ enum LogitsMode { LM_STATS, LM_PROB, LM_SLICE };
 
 template <class T, int MODE, int NP, int WAVES> __global__ __launch_bounds__(T::NT, WAVES) void ce_logits_kernel(const CeLogits a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0 && a.ticket) *a.ticket = 0;
+    if constexpr (MODE == LM_PROB)
+        if ((int)blockIdx.x == a.tiles_i * a.tiles_j) { ce_labels(a.labels, a.N, a.V_all, a.mask, a.count, reinterpret_cast<int*>(smem)); return; }
     int ti, tj;
     gemm_tile_of(blockIdx.x, a.tiles_i * a.tiles_j, a.tiles_i, a.tiles_j, a.band, ti, tj);
     const int i0 = ti * T::BI, j0 = tj * T::BJ;
@@ -261,8 +261,9 @@ template <class T, int MODE, int NP, int WAVES> __global__ __launch_bounds__(T::
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// The end of the forward pass: a wave a row.  (m, s) of the tiles (or the partial logits themselves) to lse, the label's logit, the
-// row's loss; the last workgroup to arrive adds up what all of them left, in the order of the rows.
+// The end of the forward pass.  (m, s) of the tiles (or the partial logits themselves) to lse, the label's logit, the row's loss and
+// every workgroup's sum of them; a last small kernel (or the only workgroup) adds those up.  WPR waves a row: one, or four where rows
+// are few or their logits come in slices.
 // ---------------------------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     const float t = fmaxf(m, m2), t0 = t == -kInf ? 0.f : t;
@@ -270,34 +271,78 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     m = t;
 }
 
-template <bool SLICES> __global__ __launch_bounds__(256) void ce_rows_kernel(const CeRows a) {
-    __shared__ float s_loss[4];
+// sums of the slices of two logits, eight slices requested at once
+__device__ __forceinline__ float2 sliced(const float* p, size_t slice, int n) {
+    float2 l = make_float2(0.f, 0.f);
+    int k = 0;
+    for (; k + 8 <= n; k += 8) {
+        float2 t[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) t[q] = *reinterpret_cast<const float2*>(p + (k + q) * slice);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) { l.x += t[q].x; l.y += t[q].y; }
+    }
+    for (; k < n; ++k) { const float2 t = *reinterpret_cast<const float2*>(p + k * slice); l.x += t.x; l.y += t.y; }
+    return l;
+}
+
+// sum of n losses and number of rows, by a workgroup of 256
+__device__ __forceinline__ void ce_total(const float* sums, const int* counts, int n, float* loss) {
+    __shared__ double s_t[4];
+    __shared__ int s_c[4];
+    const int tid = threadIdx.x;
+    double t = 0.0;
+    int c = 0;
+    for (int b = tid; b < n; b += 256) { t += sums[b]; c += counts[b]; }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { t += __shfl_xor(t, o); c += __shfl_xor(c, o); }
+    if ((tid & 63) == 0) { s_t[tid >> 6] = t; s_c[tid >> 6] = c; }
+    __syncthreads();
+    if (tid == 0) {
+        const int all = s_c[0] + s_c[1] + s_c[2] + s_c[3];
+        *loss = (float)(((s_t[0] + s_t[1]) + (s_t[2] + s_t[3])) / (double)(all > 1 ? all : 1));
+    }
+}
+__global__ __launch_bounds__(256) void ce_total_kernel(const float* sums, const int* counts, int n, float* loss) { ce_total(sums, counts, n, loss); }
+
+template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_kernel(const CeRows a) {
+    __shared__ float s_m[4], s_s[4], s_own[4], s_loss[4];
     __shared__ int s_cnt[4];
-    __shared__ int s_last;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.x * 4 + wave;
-    float loss = 0.f;
-    int counts = 0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.x * (4 / WPR) + wave / WPR;
+    const int part = wave % WPR, l0 = part * 64 + lane;
+    constexpr int STEP = 64 * WPR;
+    float loss = 0.f, m = -kInf, s = 0.f, own = 0.f;
+    int y = -1;
+    bool valid = false;
     if (n < a.N) {
-        const int y = a.labels[n];
-        const bool valid = is_class(y, a.V);
-        float m = -kInf, s = 0.f, own = 0.f;
+        y = a.labels[n];
+        valid = is_class(y, a.V);
         if constexpr (SLICES) {
             const float* const row = a.slices + (size_t)n * a.ldv;
-            for (int v = lane; v < a.V; v += 64) {
-                float l = row[v];
-                for (int k = 1; k < a.nslices; ++k) l += row[k * a.slice + v];
-                if (a.bias) l += a.bias[v];
-                if (v == y) own = l;
-                join(m, s, l * kLog2e, 1.f);
+            for (int v = 2 * l0; v < a.V; v += 2 * STEP) {
+                float2 l = sliced(row + v, a.slice, a.nslices);
+                if (a.bias) { l.x += a.bias[v]; l.y += v + 1 < a.V ? a.bias[v + 1] : 0.f; }
+                if (v == y) own = l.x;
+                if (v + 1 == y) own = l.y;
+                join(m, s, l.x * kLog2e, 1.f);
+                if (v + 1 < a.V) join(m, s, l.y * kLog2e, 1.f);
             }
         } else {
             const float2* const row = a.partial + (size_t)n * a.parts;
-            for (int t = lane; t < a.parts; t += 64) { const float2 v = row[t]; join(m, s, v.x, v.y); }
+            int t = l0;
+            for (; t + 3 * STEP < a.parts; t += 4 * STEP) {
+                float2 v[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] = row[t + q * STEP];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) join(m, s, v[q].x, v[q].y);
+            }
+            for (; t < a.parts; t += STEP) { const float2 v = row[t]; join(m, s, v.x, v.y); }
             if (valid)
                 for (int p = 0; p < a.pairs.n; ++p) {
                     const unsigned short* const x = reinterpret_cast<const unsigned short*>(a.x.base + ((a.pairs.b >> (4 * p)) & 15) * a.x.plane) + (size_t)n * a.x.ld;
                     const unsigned short* const w = reinterpret_cast<const unsigned short*>(a.w.base + ((a.pairs.a >> (4 * p)) & 15) * a.w.plane) + (size_t)y * a.w.ld;
-                    for (int c = lane * 8; c < a.K; c += 512) {
+                    for (int c = l0 * 8; c < a.K; c += 8 * STEP) {
                         const u32x4 xv = *reinterpret_cast<const u32x4*>(x + c), wv = *reinterpret_cast<const u32x4*>(w + c);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
@@ -313,59 +358,54 @@ template <bool SLICES> __global__ __launch_bounds__(256) void ce_rows_kernel(con
             join(m, s, m2, s2);
             own += __shfl_xor(own, o);
         }
+    }
+    if constexpr (WPR == 4) {
+        if (lane == 0) { s_m[wave] = m; s_s[wave] = s; s_own[wave] = own; }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if (w == 0) { m = s_m[0]; s = s_s[0]; own = s_own[0]; }
+            else { join(m, s, s_m[w], s_s[w]); own += s_own[w]; }
+        }
+    }
+    if (n < a.N && part == 0) {
         const float lse = (m + __builtin_amdgcn_logf(s)) * kLn2;       // log2
         if (!SLICES && valid && a.bias) own += a.bias[y];
         loss = valid ? lse - own : 0.f;
-        counts = valid ? 1 : 0;
         if (lane == 0) {
             a.lse[n] = lse;
             if (a.row_loss) a.row_loss[n] = loss;
         }
     }
-    if (lane == 0) { s_loss[wave] = loss; s_cnt[wave] = counts; }
+    if (lane == 0) { s_loss[wave] = loss; s_cnt[wave] = part == 0 && valid ? 1 : 0; }
     __syncthreads();
     if (tid == 0) {
-        // device scope: the sums are read by a workgroup of another XCD
-        __hip_atomic_store(a.bsum + blockIdx.x, (s_loss[0] + s_loss[1]) + (s_loss[2] + s_loss[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(a.bcnt + blockIdx.x, s_cnt[0] + s_cnt[1] + s_cnt[2] + s_cnt[3], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = __hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+        a.bsum[blockIdx.x] = (s_loss[0] + s_loss[1]) + (s_loss[2] + s_loss[3]);
+        a.bcnt[blockIdx.x] = s_cnt[0] + s_cnt[1] + s_cnt[2] + s_cnt[3];
     }
-    __syncthreads();
-    if (!s_last) return;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-    double t = 0.0;
-    int c = 0;
-    for (int b = tid; b < (int)gridDim.x; b += 256) {
-        t += __hip_atomic_load(a.bsum + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        c += __hip_atomic_load(a.bcnt + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __shared__ double s_t[4];
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { t += __shfl_xor(t, o); c += __shfl_xor(c, o); }
-    if (lane == 0) { s_t[wave] = t; s_cnt[wave] = c; }
-    __syncthreads();
-    if (tid == 0) {
-        const int all = s_cnt[0] + s_cnt[1] + s_cnt[2] + s_cnt[3];
-        *a.loss = (float)(((s_t[0] + s_t[1]) + (s_t[2] + s_t[3])) / (double)(all > 1 ? all : 1));
+    if (gridDim.x == 1) {
+        __syncthreads();
+        ce_total(a.bsum, a.bcnt, 1, a.loss);
     }
 }
 
 // Probabilities from partial logits (few tiles): a workgroup a row
 template <int NP> __global__ __launch_bounds__(256) void ce_prob_kernel(const CeRows a, unsigned short* __restrict__ prob, size_t pplane) {
-    const int n = blockIdx.x, y = a.labels[n];
+    __shared__ int s_cnt[4];
+    const int n = blockIdx.x;
+    if (n == a.N) { ce_labels(a.labels, a.N, a.V, a.mask, a.count, s_cnt); return; }
+    const int y = a.labels[n];
     const bool valid = is_class(y, a.V);
     const float shift = a.lse[n] * kLog2e;
     const float* const row = a.slices + (size_t)n * a.ldv;
     for (int v = threadIdx.x * 2; v < a.ldv; v += 512) {
         unsigned b[2][NP];
+        const float2 l = sliced(row + v, a.slice, a.nslices);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             float p = 0.f;
             if (valid && v + e < a.V) {
-                float l = row[v + e];
-                for (int k = 1; k < a.nslices; ++k) l += row[k * a.slice + v + e];
-                if (a.bias) l += a.bias[v + e];
-                p = __builtin_amdgcn_exp2f(fmaf(l, kLog2e, -shift));
+                p = __builtin_amdgcn_exp2f(fmaf((e ? l.y : l.x) + (a.bias ? a.bias[v + e] : 0.f), kLog2e, -shift));
                 if (v + e == y) p -= 1.f;
             }
             split_bf16<NP>(p, b[e]);
@@ -456,21 +496,26 @@ template <class T> __global__ __launch_bounds__(256) void ce_finish_kernel(const
         }
         return;
     }
-    // bias: 64 classes a workgroup, its four waves a quarter of the parts each
-    __shared__ float s_b[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, v = (b - a.blocks_x - a.blocks_w) * 64 + lane;
+    // bias: 32 classes a workgroup, eight groups of threads a part of the rows each
+    __shared__ float s_b[8][32];
+    const int col = threadIdx.x & 31, grp = threadIdx.x >> 5, v = (b - a.blocks_x - a.blocks_w) * 32 + col;
     float t = 0.f;
     if (v < a.V) {
         if (a.colsum) {
-            for (int k = wave; k < a.parts; k += 4) t += a.colsum[(size_t)k * a.ld_colsum + v];
+#pragma unroll 8
+            for (int k = grp; k < a.parts; k += 8) t += a.colsum[(size_t)k * a.ld_colsum + v];
         } else {
-            for (int n = wave; n < a.N; n += 4)
+#pragma unroll 8
+            for (int n = grp; n < a.N; n += 8)
                 for (int p = 0; p < a.nplanes; ++p) t += bf16_up(a.prob[p * (a.pplane / 2) + (size_t)n * a.ldv + v]);
         }
     }
-    s_b[wave][lane] = t;
+    s_b[grp][col] = t;
     __syncthreads();
-    if (wave == 0 && v < a.V) a.dbias[v] = ((s_b[0][lane] + s_b[1][lane]) + (s_b[2][lane] + s_b[3][lane])) * g;
+    if (grp == 0 && v < a.V) {
+        for (int k = 1; k < 8; ++k) t += s_b[k][col];
+        a.dbias[v] = t * g;
+    }
 }
 
 __global__ __launch_bounds__(256) void ce_zero_kernel(float* p, size_t n) {
@@ -492,7 +537,7 @@ template <class K, class A> hipError_t launch(K kernel, OncePerDevice& once, dim
 template <class T, int MODE, int NP, int WAVES> hipError_t launch_logits_t(const CeLogits& a, int slices, hipStream_t s) {
     static OncePerDevice once;
     constexpr int EP = MODE == LM_PROB ? T::NW * NP * 32 * (T::TI * 2 + 16) : 0;
-    return launch(ce_logits_kernel<T, MODE, NP, WAVES>, once, dim3(a.tiles_i * a.tiles_j, slices), T::NT, std::max(T::LDS, EP), s, a);
+    return launch(ce_logits_kernel<T, MODE, NP, WAVES>, once, dim3(a.tiles_i * a.tiles_j + (MODE == LM_PROB ? 1 : 0), slices), T::NT, std::max(T::LDS, EP), s, a);
 }
 template <class T, int WAVES> hipError_t launch_grad_t(const CeGrad& a, int slices, hipStream_t s) {
     static OncePerDevice once;
@@ -500,6 +545,16 @@ template <class T, int WAVES> hipError_t launch_grad_t(const CeGrad& a, int slic
 }
 
 }  // namespace
+
+// Time of a product cut into `blocks` workgroups of `ktiles` k-tiles each, microseconds: rounds of as many as run at once, a k-tile of a
+// full chip and of a nearly empty one as measured (256 x 256 1.95 and 1.4 us, 128 x 128 0.52 and 0.36, 64 x 64 0.43 and 0.27), and what a
+// workgroup does besides.
+double ce_tile_time(int cfg, long blocks, int ktiles) {
+    static const struct { int slots; double some, full, rest; } t[4] = {{256, 1.4, 1.95, 6.0}, {256, 0.36, 0.52, 4.0}, {512, 0.27, 0.43, 3.0}, {512, 0.25, 0.40, 3.0}};
+    const long rounds = blocks / t[cfg].slots, over = blocks - rounds * t[cfg].slots;
+    const double last = t[cfg].some + (t[cfg].full - t[cfg].some) * (double)over / t[cfg].slots;
+    return (double)rounds * (t[cfg].rest + ktiles * t[cfg].full) + (over ? t[cfg].rest + ktiles * last : 0.0);
+}
 
 void ce_tile_size(int cfg, int* bi, int* bj, int* wi, int* wj) {
     static const int d[4][4] = {{256, 256, 2, 4}, {128, 128, 2, 2}, {64, 64, 2, 2}, {128, 32, 4, 1}};
@@ -512,10 +567,6 @@ hipError_t launch_ce_pack(const void* src, long ld_src, int rows, int cols, int 
     const dim3 grid((unsigned)std::min<size_t>((n + 255) / 256, 1u << 16));
     if (dtype == 1) hipLaunchKernelGGL((ce_pack_kernel<bf16_t, 1>), grid, dim3(256), 0, s, (const bf16_t*)src, ld_src, rows, cols, (unsigned short*)dst, plane / 2, ld);
     else hipLaunchKernelGGL((ce_pack_kernel<float, 3>), grid, dim3(256), 0, s, (const float*)src, ld_src, rows, cols, (unsigned short*)dst, plane / 2, ld);
-    return hipGetLastError();
-}
-hipError_t launch_ce_labels(const int* labels, int N, int V, unsigned long long* mask, int* count, hipStream_t s) {
-    hipLaunchKernelGGL(ce_labels_kernel, dim3(1), dim3(1024), 0, s, labels, N, V, mask, count);
     return hipGetLastError();
 }
 hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s) {
@@ -544,14 +595,18 @@ hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t 
     return launch_logits_t<TFew<false, false, false>, LM_SLICE, 1, 2>(a, slices, s);
 }
 hipError_t launch_ce_rows(const CeRows& a, hipStream_t s) {
-    const dim3 grid((a.N + 3) / 4);
-    if (a.slices) hipLaunchKernelGGL(ce_rows_kernel<true>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(ce_rows_kernel<false>, grid, dim3(256), 0, s, a);
+    // (8192 rows of 256 parts: a wave a row 11 us, four 14; 1000 rows 6 and 5)
+    const bool wide = a.slices || a.N < 2048;
+    const int blocks = wide ? a.N : (a.N + 3) / 4;
+    if (a.slices) hipLaunchKernelGGL((ce_rows_kernel<true, 4>), dim3(blocks), dim3(256), 0, s, a);
+    else if (wide) hipLaunchKernelGGL((ce_rows_kernel<false, 4>), dim3(blocks), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((ce_rows_kernel<false, 1>), dim3(blocks), dim3(256), 0, s, a);
+    if (blocks > 1) hipLaunchKernelGGL(ce_total_kernel, dim3(1), dim3(256), 0, s, a.bsum, a.bcnt, blocks, a.loss);
     return hipGetLastError();
 }
 hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int planes, hipStream_t s) {
-    if (planes == 2) hipLaunchKernelGGL(ce_prob_kernel<2>, dim3(a.N), dim3(256), 0, s, a, prob, pplane);
-    else hipLaunchKernelGGL(ce_prob_kernel<3>, dim3(a.N), dim3(256), 0, s, a, prob, pplane);
+    if (planes == 2) hipLaunchKernelGGL(ce_prob_kernel<2>, dim3(a.N + 1), dim3(256), 0, s, a, prob, pplane);
+    else hipLaunchKernelGGL(ce_prob_kernel<3>, dim3(a.N + 1), dim3(256), 0, s, a, prob, pplane);
     return hipGetLastError();
 }
 hipError_t launch_ce_dx(const CeGrad& a, int slices, int cfg, hipStream_t s) {
