@@ -3472,11 +3472,11 @@ namespace {
 
 struct OrthoPlan {
     std::vector<NsProb> p;
-    std::vector<int> start[4];               // blocks of the launches: elements, pieces, tiles of r x r, of r x c
+    std::vector<int> start[kNsLaunches];     // blocks of the launches: small, elements, pieces, tiles of r x r, of r x c
     int cfg_sq = NT_64, cfg_step = NT_64;
-    size_t o_table = 0, o_norm = 0, bytes = 256;
-    size_t table_words() const { return 4 * (p.size() + 1) + (4 * (p.size() + 1)) % 2 + p.size() * sizeof(NsProb) / 4; }
-    size_t probs_word() const { return 4 * (p.size() + 1) + (4 * (p.size() + 1)) % 2; }
+    size_t o_table = 0, o_norm = 0, lds = 0, bytes = 256;
+    size_t probs_word() const { return (kNsLaunches * (p.size() + 1) + 1) / 2 * 2; }
+    size_t table_words() const { return probs_word() + p.size() * sizeof(NsProb) / 4; }
 };
 static_assert(sizeof(NsProb) % 8 == 0, "the table is copied as words, its pointers aligned to eight bytes");
 
@@ -3491,17 +3491,18 @@ static lp_status ortho_plan(OrthoPlan& o) {
     const int n = (int)o.p.size();
     WsAlloc ws;
     o.o_table = ws.take(o.table_words() * 4);
-    // the tile that is fastest for all of them together: time goes with the length of the reduction as well, so that the longest count
+    auto large = [](const NsProb& q) { return !(q.flags & NS_PLAIN) && ns_small_lds(q.rows, q.cols) == 0; };
+    // the tile that is fastest for all of them together
     double best_sq = 1e300, best_step = 1e300;
     for (int c = 0; c < NT_COUNT; ++c) {
         int bi, bj;
         ns_tile_size(c, &bi, &bj);
         long sq = 0, step = 0;
         for (const NsProb& q : o.p)
-            if (!q.plain) {
-                const int r = std::min(q.rows, q.cols), l = std::max(q.rows, q.cols);
-                sq += (long)div_up(r, bj) * (div_up(r, bj) + 1) / 2;
-                step += (long)div_up(r, bj) * div_up(l, bi);
+            if (large(q)) {
+                const NsWork w(q.rows, q.cols);
+                sq += (long)div_up(w.r, bj) * (div_up(w.r, bj) + 1) / 2;
+                step += (long)div_up(w.r, bj) * div_up(w.c, bi);
             }
         const double tq = ns_tile_time(c, sq), ts = ns_tile_time(c, step);
         if (bi == bj && tq < best_sq) { best_sq = tq; o.cfg_sq = c; }
@@ -3509,25 +3510,27 @@ static lp_status ortho_plan(OrthoPlan& o) {
     }
     int bs, bi, bj;
     ns_tile_size(o.cfg_sq, &bs, &bs); ns_tile_size(o.cfg_step, &bi, &bj);
-    long total[4] = {0, 0, 0, 0};
+    long total[kNsLaunches] = {0, 0, 0, 0, 0};
     for (auto& s : o.start) s.assign(n + 1, 0);
     for (int i = 0; i < n; ++i) {
         NsProb& q = o.p[i];
-        q.r = std::min(q.rows, q.cols); q.c = std::max(q.rows, q.cols);
-        q.ldr = div_up(q.r, 32) * 64; q.ldc = div_up(q.c, 32) * 64;
-        const long here[4] = {((long)q.rows * q.cols + kNsElems - 1) / kNsElems, q.plain ? 0 : (long)div_up(q.rows, 64) * div_up(q.cols, 64),
-                              q.plain ? 0 : (long)div_up(q.r, bs) * (div_up(q.r, bs) + 1) / 2, q.plain ? 0 : (long)div_up(q.r, bj) * div_up(q.c, bi)};
-        for (int k = 0; k < 4; ++k) { o.start[k][i] = (int)total[k]; total[k] += here[k]; }
-        if (!q.plain) {
-            const size_t x = (size_t)q.r * q.ldc * 2, s = (size_t)q.r * q.ldr * 2;
-            q.x0 = (char*)ws.take(x); q.x1 = (char*)ws.take(x); q.s = (char*)ws.take(s); q.b = (char*)ws.take(s);     // offsets, for now
+        const NsWork w(q.rows, q.cols);
+        const long chunks = ((long)q.rows * q.cols + kNsElems - 1) / kNsElems;
+        long here[kNsLaunches] = {0, 0, 0, 0, 0};
+        if (q.flags & NS_PLAIN) here[0] = chunks;
+        else if (!large(q)) { here[0] = 1; o.lds = std::max(o.lds, ns_small_lds(q.rows, q.cols)); }
+        else {
+            here[1] = chunks; here[2] = (long)div_up(q.rows, 64) * div_up(q.cols, 64);
+            here[3] = (long)div_up(w.r, bs) * (div_up(w.r, bs) + 1) / 2; here[4] = (long)div_up(w.r, bj) * div_up(w.c, bi);
+            q.work = (char*)ws.take(w.bytes());       // an offset, for now
         }
+        for (int k = 0; k < kNsLaunches; ++k) { o.start[k][i] = (int)total[k]; total[k] += here[k]; }
     }
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < kNsLaunches; ++k) {
         if (total[k] > (1l << 30)) return fail(LP_ERR_SHAPE, "too many elements in one call");
         o.start[k][n] = (int)total[k];
     }
-    o.o_norm = ws.take((size_t)total[0] * sizeof(double));
+    o.o_norm = ws.take((size_t)total[1] * sizeof(double));
     o.bytes = std::max<size_t>(ws.off, 256);
     return LP_OK;
 }
@@ -3536,12 +3539,11 @@ static lp_status ortho_run(OrthoPlan& o, char* ws, size_t ws_bytes, float moment
     if (!ws || ws_bytes < o.bytes) return fail(LP_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : (size_t)0, o.bytes);
     if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(LP_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
     const int n = (int)o.p.size();
-    if (o.start[0][n] == 0) return LP_OK;
-    for (NsProb& q : o.p)
-        if (!q.plain) { q.x0 = ws + (size_t)q.x0; q.x1 = ws + (size_t)q.x1; q.s = ws + (size_t)q.s; q.b = ws + (size_t)q.b; }
+    if (n == 0) return LP_OK;
+    for (NsProb& q : o.p) q.work = ws + (size_t)q.work;
     // the table goes to the device in the arguments of small launches: legal under capture, no host memory to keep
     std::vector<unsigned> words(o.table_words(), 0u);
-    for (int k = 0; k < 4; ++k) memcpy(words.data() + k * (n + 1), o.start[k].data(), (size_t)(n + 1) * 4);
+    for (int k = 0; k < kNsLaunches; ++k) memcpy(words.data() + k * (n + 1), o.start[k].data(), (size_t)(n + 1) * 4);
     memcpy(words.data() + o.probs_word(), o.p.data(), (size_t)n * sizeof(NsProb));
     hipError_t err = hipSuccess;
     constexpr int room = (int)(sizeof(NsChunk::w) / 4);
@@ -3556,19 +3558,22 @@ static lp_status ortho_run(OrthoPlan& o, char* ws, size_t ws_bytes, float moment
     memset(&a, 0, sizeof(a));
     const int* const table = (const int*)(ws + o.o_table);
     a.p = (const NsProb*)(table + o.probs_word());
-    a.start_norm = table; a.norm = (double*)(ws + o.o_norm); a.n = n;
+    a.start_norm = table + (n + 1); a.norm = (double*)(ws + o.o_norm); a.n = n;
     a.momentum = momentum; a.wd = wd; a.rest_lr = rest_lr; a.nesterov = nesterov;
     auto at = [&](int k) { a.start = table + (size_t)k * (n + 1); a.total = o.start[k][n]; };
     at(0);
-    if (err == hipSuccess) err = launch_ns_norm(a, s);
+    if (err == hipSuccess) err = launch_ns_small(a, steps, o.lds, s);
+    if (o.start[1][n] == 0) return hip_status(err);
     at(1);
+    if (err == hipSuccess) err = launch_ns_norm(a, s);
+    at(2);
     if (err == hipSuccess) err = launch_ns_split(a, s);
     for (int i = 0; i < steps && err == hipSuccess; ++i) {
         a.odd = i & 1; a.last = i + 1 == steps;
-        at(2);
+        at(3);
         err = launch_ns_gram(a, o.cfg_sq, s);
         if (err == hipSuccess) err = launch_ns_poly(a, o.cfg_sq, s);
-        at(3);
+        at(4);
         if (err == hipSuccess) err = launch_ns_step(a, o.cfg_step, s);
     }
     return hip_status(err);
@@ -3588,9 +3593,8 @@ static lp_status ortho_matrices(int n, const lp_matrix* mats, OrthoPlan& o) {
         NsProb q;
         memset(&q, 0, sizeof(q));
         q.rows = m.rows; q.cols = m.cols; q.src = m.in; q.out = m.out; q.ld_src = ldi; q.ld_out = ldo;
-        q.src_low = m.dtype_in == LP_BF16; q.out_low = m.dtype_out == LP_BF16;
-        q.vec = ldi == m.cols && !misaligned(m.in);
-        q.vec_out = m.cols % 4 == 0 && ldo % 4 == 0 && !misaligned(m.out);
+        q.flags = (m.dtype_in == LP_BF16 ? NS_SRC_LOW : 0) | (m.dtype_out == LP_BF16 ? NS_OUT_LOW : 0) | (ldi == m.cols && !misaligned(m.in) ? NS_VEC : 0) |
+                  (m.cols % 4 == 0 && ldo % 4 == 0 && !misaligned(m.out) ? NS_VEC_OUT : 0);
         o.p.push_back(q);
     }
     return ortho_plan(o);
@@ -3606,10 +3610,10 @@ static lp_status muon_tensor(int rows, int cols, int dtype, int orthogonal, void
     }
     NsProb q;
     memset(&q, 0, sizeof(q));
-    q.rows = rows; q.cols = cols; q.plain = !orthogonal; q.ld_out = cols; q.out_low = dtype == LP_BF16;
+    q.rows = rows; q.cols = cols; q.ld_out = cols;
     q.out = param; q.grad = grad; q.vel = vel; q.master = master;
-    q.vec = !misaligned(grad) && !misaligned(vel);
-    q.vec_out = cols % 4 == 0 && !misaligned(param) && !misaligned(master);
+    q.flags = (dtype == LP_BF16 ? NS_OUT_LOW : 0) | (orthogonal ? 0 : NS_PLAIN) | (!misaligned(grad) && !misaligned(vel) ? NS_VEC : 0) |
+              (cols % 4 == 0 && !misaligned(param) && !misaligned(master) ? NS_VEC_OUT : 0);
     if (opts) {
         q.lr = (float)(opts->lr * std::sqrt(std::max(1.0, (double)rows / cols)));
         q.shrink = (float)(1.0 - (double)opts->lr * opts->weight_decay);
@@ -3684,7 +3688,7 @@ lp_status lp_orthogonalize(void* stream, int n, const lp_matrix* mats, int steps
         if (st != LP_OK) return st;
         for (const NsProb& q : o.p) {
             if (!q.src || !q.out) return fail(LP_ERR_INVALID_ARG, "a matrix of %d x %d without in or out", q.rows, q.cols);
-            if (reinterpret_cast<uintptr_t>(q.src) % (q.src_low ? 2 : 4) || reinterpret_cast<uintptr_t>(q.out) % (q.out_low ? 2 : 4))
+            if (reinterpret_cast<uintptr_t>(q.src) % (q.flags & NS_SRC_LOW ? 2 : 4) || reinterpret_cast<uintptr_t>(q.out) % (q.flags & NS_OUT_LOW ? 2 : 4))
                 return fail(LP_ERR_INVALID_ARG, "a matrix is not aligned to its elements");
         }
         return ortho_run(o, (char*)workspace, workspace_bytes, 0.f, 0.f, 0.f, 0, steps, (hipStream_t)stream);

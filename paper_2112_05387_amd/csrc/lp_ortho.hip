@@ -19,59 +19,31 @@
 
 #include "lp_gemm.h"
 #include "lp_kernels.h"
+#include "lp_ortho_dev.h"
 
 namespace lp {
 namespace {
-
-constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
-constexpr float kScaleX = 16384.f, kScaleS = 8192.f, kScaleB = 4096.f;
-
-// the last tensor whose first block is not beyond `block`
-__device__ __forceinline__ int ns_find(const int* start, int n, int block) {
-    const int lane = threadIdx.x & 63;
-    int found = 0;
-    for (int i = 0; i < n; i += 64) found += __popcll(__ballot(i + lane < n && start[min(i + lane, n)] <= block));
-    return __builtin_amdgcn_readfirstlane(found - 1);
-}
-
-__device__ __forceinline__ unsigned f16_bits(float x) { return __builtin_bit_cast(unsigned short, (_Float16)x); }
-__device__ __forceinline__ float f16_up(unsigned b) { return (float)__builtin_bit_cast(_Float16, (unsigned short)b); }
 
 __global__ __launch_bounds__(256) void ns_put_kernel(const NsChunk c) {
     for (int i = threadIdx.x; i < c.words; i += 256) c.dst[i] = c.w[i];
 }
 
-__device__ __forceinline__ float load_low(const void* p, int low, size_t e) {
-    return low ? bf16_bits_to_float(reinterpret_cast<const unsigned short*>(p)[e]) : reinterpret_cast<const float*>(p)[e];
-}
-__device__ __forceinline__ void store_low(void* p, int low, size_t e, float x) {
-    if (low) reinterpret_cast<unsigned short*>(p)[e] = float_to_bf16_bits(x);
-    else reinterpret_cast<float*>(p)[e] = x;
-}
-
-// Elements: momentum of the matrices and their sums of squares; the whole update of the other tensors
+// Elements: momentum of the matrices and their sums of squares
 __global__ __launch_bounds__(256) void ns_norm_kernel(const NsArgs a) {
     const int pi = ns_find(a.start, a.n, blockIdx.x);
     const NsProb& P = a.p[pi];
     const size_t numel = (size_t)P.rows * P.cols, base = (size_t)(blockIdx.x - a.start[pi]) * kNsElems;
     const int tid = threadIdx.x;
     double sum = 0.0;
-    auto element = [&](size_t e, float g, float v, float w) __attribute__((always_inline)) {       // returns through vel / out
-        if (P.plain) {
-            v = fmaf(a.momentum, v, fmaf(a.wd, w, g));
-            w = fmaf(-a.rest_lr, v, w);
-            P.vel[e] = v;
-            if (P.master) P.master[e] = w;
-            store_low(P.out, P.out_low, e, w);
-        } else {
-            v = fmaf(a.momentum, v, g);
-            P.vel[e] = v;
-            const float u = a.nesterov ? fmaf(a.momentum, v, g) : v;
-            sum += (double)u * u;
-        }
+    auto element = [&](size_t e, float g, float v) __attribute__((always_inline)) {
+        v = fmaf(a.momentum, v, g);
+        P.vel[e] = v;
+        const float u = a.nesterov ? fmaf(a.momentum, v, g) : v;
+        sum += (double)u * u;
     };
     constexpr int U = kNsElems / 1024;
-    if (P.vec && !P.plain) {
+    const int src_low = P.flags & NS_SRC_LOW;
+    if (P.flags & NS_VEC) {
         // four elements a thread and trip, all loads first
         f32x4 g[U], v[U];
 #pragma unroll
@@ -80,7 +52,7 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(const NsArgs a) {
             g[i] = f32x4{0.f, 0.f, 0.f, 0.f}; v[i] = g[i];
             if (e + 4 > numel) continue;
             if (P.src) {
-                if (P.src_low) {
+                if (src_low) {
                     const u32x2 w = *reinterpret_cast<const u32x2*>(reinterpret_cast<const unsigned short*>(P.src) + e);
                     g[i] = f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
                 } else g[i] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(P.src) + e);
@@ -105,8 +77,8 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(const NsArgs a) {
                 if (!P.src) *reinterpret_cast<f32x4*>(P.vel + e) = v[i];
             } else {
                 for (size_t t = e; t < numel; ++t) {
-                    if (P.src) { const float u = load_low(P.src, P.src_low, t); sum += (double)u * u; }
-                    else element(t, P.grad[t], P.vel[t], 0.f);
+                    if (P.src) { const float u = load_low(P.src, src_low, t); sum += (double)u * u; }
+                    else element(t, P.grad[t], P.vel[t]);
                 }
             }
         }
@@ -115,14 +87,14 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(const NsArgs a) {
             const size_t e = base + i;
             if (e >= numel) break;
             const size_t row = e / P.cols;
-            const float u = load_low(P.src, P.src_low, row * P.ld_src + (e - row * P.cols));
+            const float u = load_low(P.src, src_low, row * P.ld_src + (e - row * P.cols));
             sum += (double)u * u;
         }
     } else {
         for (int i = tid; i < kNsElems; i += 256) {
             const size_t e = base + i;
             if (e >= numel) break;
-            element(e, P.grad[e], P.vel[e], P.plain ? (P.master ? P.master[e] : load_low(P.out, P.out_low, e)) : 0.f);
+            element(e, P.grad[e], P.vel[e]);
         }
     }
     __shared__ double s[4];
@@ -154,7 +126,7 @@ __global__ __launch_bounds__(256) void ns_split_kernel(const NsArgs a) {
         const int row = (tid >> 6) + 4 * k, rr = r0 + row;
         float u = 0.f;
         if (rr < P.rows && c < P.cols) {
-            if (P.src) u = load_low(P.src, P.src_low, (size_t)rr * P.ld_src + c);
+            if (P.src) u = load_low(P.src, P.flags & NS_SRC_LOW, (size_t)rr * P.ld_src + c);
             else {
                 const size_t e = (size_t)rr * P.cols + c;
                 u = P.vel[e];
@@ -169,16 +141,15 @@ __global__ __launch_bounds__(256) void ns_split_kernel(const NsArgs a) {
     const bool tall = P.rows > P.cols;
     // the piece as rows of X: row x0 + i, columns y0 + 2 j, y0 + 2 j + 1
     const int x0 = tall ? c0 : r0, y0 = tall ? r0 : c0;
-    unsigned* const out = reinterpret_cast<unsigned*>(P.x0);
+    const NsWork W(P.rows, P.cols);
+    unsigned* const out = reinterpret_cast<unsigned*>(P.work);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int i = (tid >> 5) + 8 * k, j = 2 * (tid & 31);
-        if (x0 + i < P.r && 2 * (y0 + j) < P.ldc) {
+        if (x0 + i < W.r && 2 * (y0 + j) < W.ldc) {
             const float u0 = (tall ? t[j][i] : t[i][j]) * inv, u1 = (tall ? t[j + 1][i] : t[i][j + 1]) * inv;
-            const unsigned h0 = f16_bits(u0), h1 = f16_bits(u1);
-            const size_t at = ((size_t)(x0 + i) * P.ldc + (y0 + j) / 32 * 64 + (j & 31)) >> 1;
-            out[at] = h0 | (h1 << 16);
-            out[at + 16] = f16_bits(u0 - f16_up(h0)) | (f16_bits(u1 - f16_up(h1)) << 16);
+            const size_t at = ((size_t)(x0 + i) * W.ldc + (y0 + j) / 32 * 64 + (j & 31)) >> 1;
+            split_f16x2(u0, u1, out[at], out[at + 16]);
         }
     }
 }
@@ -188,20 +159,21 @@ enum NsMode { NS_GRAM, NS_POLY, NS_STEP, NS_LAST };
 // A 32 x 32 piece of O, i from i0 along the longer side: what it is the step of is requested before its values lie in LDS.
 struct NsOld { f32x4 w[4]; u32x2 low[4]; };
 __device__ __forceinline__ void ns_request(const NsProb& P, NsOld& old, int row0, int col0, int lane) {
-    if (P.src || !P.vec_out) return;
+    if (P.src || !(P.flags & NS_VEC_OUT)) return;
     const int col = min(col0 + 4 * (lane & 7), P.cols - 4);       // (rows and columns beyond the last: read, not used)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const size_t e = (size_t)min(row0 + (lane >> 3) + 8 * k, P.rows - 1) * P.ld_out + col;
         if (P.master) old.w[k] = *reinterpret_cast<const f32x4*>(P.master + e);
-        else if (P.out_low) old.low[k] = *reinterpret_cast<const u32x2*>(reinterpret_cast<const unsigned short*>(P.out) + e);
+        else if (P.flags & NS_OUT_LOW) old.low[k] = *reinterpret_cast<const u32x2*>(reinterpret_cast<const unsigned short*>(P.out) + e);
         else old.w[k] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(P.out) + e);
     }
 }
 // ... E[j][i] in LDS: stored, or taken as the step of the parameters
 __device__ __forceinline__ void ns_answer(const NsProb& P, const NsOld& old, const float* E, bool tall, int row0, int col0, int lane) {
     const int step = tall ? 1 : 33, next = tall ? 33 : 1;         // from a row of the piece to the next, from a column
-    if (P.vec_out) {
+    const int out_low = P.flags & NS_OUT_LOW;
+    if (P.flags & NS_VEC_OUT) {
         const int col = col0 + 4 * (lane & 7), m0 = lane >> 3;
         if (col >= P.cols) return;
 #pragma unroll
@@ -212,7 +184,7 @@ __device__ __forceinline__ void ns_answer(const NsProb& P, const NsOld& old, con
             for (int e = 0; e < 4; ++e) o[e] = E[m * step + (4 * (lane & 7) + e) * next];
             if (!P.src) {
                 f32x4 w = old.w[k];
-                if (!P.master && P.out_low) w = f32x4{__uint_as_float(old.low[k][0] << 16), __uint_as_float(old.low[k][0] & 0xffff0000u),
+                if (!P.master && out_low) w = f32x4{__uint_as_float(old.low[k][0] << 16), __uint_as_float(old.low[k][0] & 0xffff0000u),
                                                       __uint_as_float(old.low[k][1] << 16), __uint_as_float(old.low[k][1] & 0xffff0000u)};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(-P.lr, o[e], w[e] * P.shrink);
@@ -220,7 +192,7 @@ __device__ __forceinline__ void ns_answer(const NsProb& P, const NsOld& old, con
             if (row0 + m >= P.rows) continue;
             const size_t e = (size_t)(row0 + m) * P.ld_out + col;
             if (P.master) *reinterpret_cast<f32x4*>(P.master + e) = o;
-            if (P.out_low) *reinterpret_cast<u32x2*>(reinterpret_cast<unsigned short*>(P.out) + e) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+            if (out_low) *reinterpret_cast<u32x2*>(reinterpret_cast<unsigned short*>(P.out) + e) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
             else *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(P.out) + e) = o;
         }
         return;
@@ -232,12 +204,12 @@ __device__ __forceinline__ void ns_answer(const NsProb& P, const NsOld& old, con
         if (row0 + m >= P.rows) break;
         const float o = E[m * step + l * next];
         const size_t e = (size_t)(row0 + m) * P.ld_out + col;
-        if (P.src) store_low(P.out, P.out_low, e, o);
+        if (P.src) store_low(P.out, out_low, e, o);
         else {
-            const float was = P.master ? P.master[e] : load_low(P.out, P.out_low, e);
+            const float was = P.master ? P.master[e] : load_low(P.out, out_low, e);
             const float w = fmaf(-P.lr, o, was * P.shrink);
             if (P.master) P.master[e] = w;
-            store_low(P.out, P.out_low, e, w);
+            store_low(P.out, out_low, e, w);
         }
     }
 }
@@ -261,11 +233,14 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
     const int t = x * per + (x < rem ? x : rem) + (blockIdx.x >> 3);       // consecutive tiles to one XCD
     const int pi = ns_find(a.start, a.n, t);
     const NsProb& P = a.p[pi];
-    const int local = t - a.start[pi], r = P.r, ldr = P.ldr, ldc = P.ldc;
+    const NsWork W(P.rows, P.cols);
+    const int local = t - a.start[pi], r = W.r, ldr = W.ldr, ldc = W.ldc;
+    char* const Xs[2] = {P.work, P.work + W.x};
+    char *const S = P.work + 2 * W.x, *const B = S + W.s;
     constexpr bool STEP = MODE == NS_STEP || MODE == NS_LAST;
     int ti, tj;
     if constexpr (STEP) {
-        const int ti_n = (P.c + T::BI - 1) / T::BI, tj_n = (r + T::BJ - 1) / T::BJ;
+        const int ti_n = (W.c + T::BI - 1) / T::BI, tj_n = (r + T::BJ - 1) / T::BJ;
         const int band = min(8, tj_n), full = band * ti_n, bd = local / full, w = min(band, tj_n - bd * band), in = local - bd * full;
         ti = in / w; tj = bd * band + in - ti * w;
     } else {                                                      // symmetric: the tiles with ti <= tj, and what they mirror
@@ -275,8 +250,8 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
         ti = local - tj * (tj + 1) / 2;
     }
     const int i0 = ti * T::BI, j0 = tj * T::BJ;
-    char* const X = a.odd ? P.x1 : P.x0;
-    const GemmOperand ox = {X, 0, ldc, STEP ? ldc : r}, os = {P.s, 0, ldr, r}, ob = {P.b, 0, ldr, r};
+    char* const X = Xs[a.odd];
+    const GemmOperand ox = {X, 0, ldc, STEP ? ldc : r}, os = {S, 0, ldr, r}, ob = {B, 0, ldr, r};
     const GemmPairs one = {1, 0, 0};
     typename T::Acc acc;
 #pragma unroll
@@ -285,7 +260,7 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
         for (int j = 0; j < T::TJ / 32; ++j)
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
-    if constexpr (MODE == NS_GRAM) T::run(ox, ox, one, i0, j0, 0, P.c, (GemmMask)nullptr, smem, acc);
+    if constexpr (MODE == NS_GRAM) T::run(ox, ox, one, i0, j0, 0, W.c, (GemmMask)nullptr, smem, acc);
     else if constexpr (MODE == NS_POLY) T::run(os, os, one, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
     else T::run(ox, ob, one, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
 
@@ -328,7 +303,7 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
     }
     // the two parts of the result, 32 x 32 at a time through LDS, from where they go out as whole cache lines
     constexpr float scale = MODE == NS_GRAM ? kScaleS / (kScaleX * kScaleX) : MODE == NS_POLY ? kC * kScaleB / (kScaleS * kScaleS) : 1.f / kScaleB;
-    char* const out = MODE == NS_GRAM ? P.s : MODE == NS_POLY ? P.b : (a.odd ? P.x0 : P.x1);
+    char* const out = MODE == NS_GRAM ? S : MODE == NS_POLY ? B : Xs[a.odd ^ 1];
     const int ldo = STEP ? ldc : ldr;
     unsigned char* const E = smem + wave * kPiece;
 #pragma unroll
@@ -336,7 +311,7 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
 #pragma unroll
         for (int i = 0; i < FI; ++i) {
             const int jj = jb + j * 32 + lr, jp = jb + j * 32, ip = ib + i * 32;
-            unsigned hb[16], lb[16];
+            unsigned hb[8], lb[8];                              // pairs along i
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int ii = ip + 8 * q + 4 * h;
@@ -345,7 +320,7 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
                 for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e] * scale;
                 if constexpr (MODE == NS_POLY) {
                     if (jj < r && 2 * ip < ldr) {
-                        const char* const sp = P.s + ((size_t)jj * ldr + 2 * ip + (ii - ip)) * 2;
+                        const char* const sp = S + ((size_t)jj * ldr + 2 * ip + (ii - ip)) * 2;
                         const u32x2 s0 = *reinterpret_cast<const u32x2*>(sp), s1 = *reinterpret_cast<const u32x2*>(sp + 64);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
@@ -355,11 +330,11 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
                         }
                     }
                 }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { hb[4 * q + e] = f16_bits(v[e]); lb[4 * q + e] = f16_bits(v[e] - f16_up(hb[4 * q + e])); }
+                split_f16x2(v[0], v[1], hb[2 * q], lb[2 * q]);
+                split_f16x2(v[2], v[3], hb[2 * q + 1], lb[2 * q + 1]);
                 unsigned char* const d = E + lr * kPiecePitch + (8 * q + 4 * h) * 2;
-                *reinterpret_cast<u32x2*>(d) = u32x2{hb[4 * q] | (hb[4 * q + 1] << 16), hb[4 * q + 2] | (hb[4 * q + 3] << 16)};
-                *reinterpret_cast<u32x2*>(d + 64) = u32x2{lb[4 * q] | (lb[4 * q + 1] << 16), lb[4 * q + 2] | (lb[4 * q + 3] << 16)};
+                *reinterpret_cast<u32x2*>(d) = u32x2{hb[2 * q], hb[2 * q + 1]};
+                *reinterpret_cast<u32x2*>(d + 64) = u32x2{lb[2 * q], lb[2 * q + 1]};
             }
             auto visible = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_s_waitcnt(0xc07f); };
             visible();
@@ -369,8 +344,8 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
 #pragma unroll
                 for (int q = 0; q < 16; ++q) {
                     unsigned short* const d = reinterpret_cast<unsigned short*>(E + T::row(q, lane) * kPiecePitch + lr * 2);
-                    d[0] = (unsigned short)hb[q];
-                    d[32] = (unsigned short)lb[q];
+                    d[0] = (unsigned short)(hb[q >> 1] >> (16 * (q & 1)));
+                    d[32] = (unsigned short)(lb[q >> 1] >> (16 * (q & 1)));
                 }
                 visible();
                 ns_piece_out(E, out, ldo, ip, r, jp, lane);

@@ -72,6 +72,14 @@ def test_one_matrix(m, n, dtype):
     _check(ops.orthogonalize([u])[0], u, f"{m} x {n} {dtype}")
 
 
+@pytest.mark.parametrize("m,n", [(32, 1152), (32, 1153), (33, 576), (64, 576), (64, 577), (1152, 32), (576, 64), (577, 64), (5, 1152), (33, 33), (1, 1200)])
+def test_where_small_matrices_end(m, n):
+    """Up to 64 rows a matrix stays in one workgroup where its columns fit."""
+    from paper_2112_05387_amd import ops
+    u = _matrix(m, n, "noise", m * n)
+    _check(ops.orthogonalize([u])[0], u, f"{m} x {n}")
+
+
 @pytest.mark.parametrize("kind", ["low_rank", "large", "small", "zero"])
 @pytest.mark.parametrize("m,n", [(48, 200), (300, 70)])
 def test_ill_conditioned_and_extreme_values(m, n, kind):
