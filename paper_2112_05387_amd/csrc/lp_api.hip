@@ -3234,6 +3234,7 @@ struct CePlan {
     int piece, pieces, ldv;                  // classes of a piece of the probabilities
     size_t o_x, o_w, o_partial, o_slices, o_bsum, o_bcnt, o_mask, o_count, o_prob, o_dx, o_dw, o_colsum, bytes;
     int parts, colparts;
+    int direct;                              // waves a row of the kernels for small problems, or 0
 };
 
 constexpr size_t kProbBytes = (size_t)512 << 20;
@@ -3248,6 +3249,15 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     p.ldx = d->ld_features ? d->ld_features : p.C; p.ldw = d->ld_weight ? d->ld_weight : p.C; p.lddx = d->ld_dfeatures ? d->ld_dfeatures : p.C;
     for (const long ld : {p.ldx, p.ldw, p.lddx})
         if (ld < p.C || ld > (1l << 40)) return fail(LP_ERR_SHAPE, "a row stride of %ld for %d channels", ld, p.C);
+    p.direct = ce_direct_waves(p.N, p.C, p.V);
+    if (p.direct) {
+        WsAlloc ws;
+        p.o_bsum = ws.take((size_t)p.N * 4);
+        p.o_bcnt = ws.take((size_t)p.N * 4);
+        p.o_prob = backward ? ws.take((size_t)p.N * p.V * 4) : 0;
+        p.bytes = ws.off;
+        return LP_OK;
+    }
     const bool low = d->dtype == LP_BF16;
     p.nplanes = low ? 1 : 3; p.nprob = low ? 2 : 3;
     // bf16 rows of whole 16-byte vectors are read where they are (the strides of a tile's rows within 32 bits)
@@ -3330,6 +3340,14 @@ static lp_status ce_check(const CePlan& p, const void* x, const void* w, const i
     return LP_OK;
 }
 
+static CeDirect ce_direct(const CePlan& p, const void* x, const void* w, const float* bias, const int32_t* labels) {
+    CeDirect a;
+    memset(&a, 0, sizeof(a));
+    a.N = p.N; a.C = p.C; a.V = p.V; a.x = x; a.w = w; a.ldx = p.ldx; a.ldw = p.ldw; a.bias = bias; a.labels = labels;
+    a.vec = p.ldw % 8 == 0;
+    return a;
+}
+
 static CeLogits ce_logits(const CePlan& p, const GemmOperand& X, const GemmOperand& W, const float* bias, int v0, int V) {
     CeLogits a;
     memset(&a, 0, sizeof(a));
@@ -3364,6 +3382,12 @@ lp_status lp_linear_ce_forward(const lp_linear_ce_desc* d, void* stream, const v
     hipStream_t s = (hipStream_t)stream;
     char* const ws = (char*)workspace;
     if (p.N == 0) return hip_status(launch_ce_zero(loss, 1, s));
+    if (p.direct) {
+        CeDirect a = ce_direct(p, features, weight, bias, labels);
+        a.lse_out = lse; a.row_loss = row_loss; a.loss = loss;
+        a.bsum = (float*)(ws + p.o_bsum); a.bcnt = (int*)(ws + p.o_bcnt);
+        return hip_status(launch_ce_direct_forward(a, d->dtype, p.direct, s));
+    }
     GemmOperand X, W;
     if ((st = ce_operands(p, d->dtype, features, weight, ws, X, W, s)) != LP_OK) return st;
     CeLogits a = ce_logits(p, X, W, bias, 0, p.V);
@@ -3402,6 +3426,12 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
         return st;
     }
     if (!dfeatures && !dweight && !dbias) return LP_OK;
+    if (p.direct) {
+        CeDirect a = ce_direct(p, features, weight, bias, labels);
+        a.lse = lse; a.scale = loss_scale; a.d = (float*)(ws + p.o_prob);
+        a.dx = dfeatures; a.lddx = p.lddx; a.dw = dweight; a.dbias = dbias;
+        return hip_status(launch_ce_direct_backward(a, d->dtype, p.direct, s));
+    }
     GemmOperand X, W;
     if ((st = ce_operands(p, d->dtype, features, weight, ws, X, W, s)) != LP_OK) return st;
     unsigned long long* const mask = (unsigned long long*)(ws + p.o_mask);
@@ -3455,7 +3485,7 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
             if ((st = hip_status(launch_ce_dx(g, t.slices, t.cfg, s))) != LP_OK) return st;
         }
         // the bias of this piece: with the last one beside the other sums
-        f.blocks_b = dbias ? div_up(V, 32) : 0; f.V = V; f.dbias = dbias ? dbias + v0 : nullptr;
+        f.blocks_b = dbias ? div_up(V, p.cut ? 8 : 32) : 0; f.V = V; f.dbias = dbias ? dbias + v0 : nullptr;
         if (piece + 1 < p.pieces && (st = hip_status(launch_ce_finish(f, d->dtype, s))) != LP_OK) return st;
     }
     f.x = CeSum{(float*)(ws + p.o_dx), (size_t)p.N * p.K, p.tx.slices, p.K, dfeatures, (size_t)p.lddx, p.N, p.C};

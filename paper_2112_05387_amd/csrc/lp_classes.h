@@ -55,6 +55,21 @@ struct CeFinish {
     float* dbias;
 };
 
+// Small problems, straight from the caller's operands (lp_classes_direct.hip)
+struct CeDirect {
+    int N, C, V;
+    const void *x, *w; long ldx, ldw;
+    int vec;                            // rows of the weights can be read 16 bytes at a time
+    const float* bias; const int* labels;
+    float *lse_out, *row_loss, *loss, *bsum; int* bcnt;      // forward
+    const float* lse; float scale; float* d;                // backward: d [N][V] between its two kernels
+    void* dx; long lddx; float *dw, *dbias;
+};
+int ce_direct_waves(int N, int C, int V);
+hipError_t launch_ce_direct_forward(const CeDirect& a, int dtype, int waves, hipStream_t s);
+hipError_t launch_ce_direct_backward(const CeDirect& a, int dtype, int waves, hipStream_t s);
+hipError_t launch_ce_total(const float* sums, const int* counts, int n, float* loss, hipStream_t s);
+
 // tiles: 0 256 x 256, 1 128 x 128, 2 64 x 64, 3 128 x 32 (few samples); waves along either side
 void ce_tile_size(int cfg, int* bi, int* bj, int* wi, int* wj);
 double ce_tile_time(int cfg, long blocks, int ktiles);

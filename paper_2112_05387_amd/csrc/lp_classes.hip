@@ -496,25 +496,48 @@ template <class T> __global__ __launch_bounds__(256) void ce_finish_kernel(const
         }
         return;
     }
-    // bias: 32 classes a workgroup, eight groups of threads a part of the rows each
-    __shared__ float s_b[8][32];
-    const int col = threadIdx.x & 31, grp = threadIdx.x >> 5, v = (b - a.blocks_x - a.blocks_w) * 32 + col;
-    float t = 0.f;
-    if (v < a.V) {
-        if (a.colsum) {
+    if (a.colsum) {  // bias from the tiles' sums: 32 classes a workgroup, eight groups of threads a part of the tiles each
+        __shared__ float s_b[8][32];
+        const int col = threadIdx.x & 31, grp = threadIdx.x >> 5, v = (b - a.blocks_x - a.blocks_w) * 32 + col;
+        float t = 0.f;
+        if (v < a.V) {
 #pragma unroll 8
             for (int k = grp; k < a.parts; k += 8) t += a.colsum[(size_t)k * a.ld_colsum + v];
-        } else {
-#pragma unroll 8
-            for (int n = grp; n < a.N; n += 8)
-                for (int p = 0; p < a.nplanes; ++p) t += bf16_up(a.prob[p * (a.pplane / 2) + (size_t)n * a.ldv + v]);
+        }
+        s_b[grp][col] = t;
+        __syncthreads();
+        if (grp == 0 && v < a.V) {
+            for (int k = 1; k < 8; ++k) t += s_b[k][col];
+            a.dbias[v] = t * g;
+        }
+        return;
+    }
+    // bias from the planes of P: eight classes a workgroup, a thread reads them in 16 bytes and takes every 256th row (3399 rows of
+    // 22 classes in three planes: 32 classes a workgroup and an element a load, 1300 loads in a chain, took 300 us).  P's rows are padded
+    // to whole eight classes.
+    __shared__ float s_p[4][8];
+    const int v0 = (b - a.blocks_x - a.blocks_w) * 8;
+    float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < a.nplanes; ++p) {
+        const unsigned short* const q = a.prob + p * (a.pplane / 2) + v0;
+#pragma unroll 4
+        for (int n = threadIdx.x; n < a.N; n += 256) {
+            const u32x4 u = *reinterpret_cast<const u32x4*>(q + (size_t)n * a.ldv);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { t[2 * e] += __uint_as_float(u[e] << 16); t[2 * e + 1] += __uint_as_float(u[e] & 0xffff0000u); }
         }
     }
-    s_b[grp][col] = t;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) t[e] += __shfl_xor(t[e], o);
+        if ((threadIdx.x & 63) == 0) s_p[threadIdx.x >> 6][e] = t[e];
+    }
     __syncthreads();
-    if (grp == 0 && v < a.V) {
-        for (int k = 1; k < 8; ++k) t += s_b[k][col];
-        a.dbias[v] = t * g;
+    if (threadIdx.x < 8 && v0 + (int)threadIdx.x < a.V) {
+        float u = 0.f;
+        for (int w = 0; w < 4; ++w) u += s_p[w][threadIdx.x];
+        a.dbias[v0 + threadIdx.x] = u * g;
     }
 }
 
@@ -601,7 +624,11 @@ hipError_t launch_ce_rows(const CeRows& a, hipStream_t s) {
     if (a.slices) hipLaunchKernelGGL((ce_rows_kernel<true, 4>), dim3(blocks), dim3(256), 0, s, a);
     else if (wide) hipLaunchKernelGGL((ce_rows_kernel<false, 4>), dim3(blocks), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((ce_rows_kernel<false, 1>), dim3(blocks), dim3(256), 0, s, a);
-    if (blocks > 1) hipLaunchKernelGGL(ce_total_kernel, dim3(1), dim3(256), 0, s, a.bsum, a.bcnt, blocks, a.loss);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || blocks == 1) return e;
+    return launch_ce_total(a.bsum, a.bcnt, blocks, a.loss, s);
+}
+hipError_t launch_ce_total(const float* sums, const int* counts, int n, float* loss, hipStream_t s) {
+    hipLaunchKernelGGL(ce_total_kernel, dim3(1), dim3(256), 0, s, sums, counts, n, loss);
     return hipGetLastError();
 }
 hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int planes, hipStream_t s) {

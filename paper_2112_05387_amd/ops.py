@@ -4,6 +4,7 @@ Every call enqueues its work on the current stream of the tensors' device and re
 torch's allocator on that stream, so calls on several streams, and calls captured into HIP graphs, do not share any.  As with
 any torch operator, a tensor that another stream produced has to be waited for by the caller.
 """
+import contextlib
 import functools
 import math
 
@@ -26,6 +27,16 @@ def _device(*tensors):
         elif t.device != dev:
             raise ValueError(f"tensors on {dev} and on {t.device}")
     return dev
+
+
+def _on(dev):
+    """The device's own context where it is not the current one (changing to the same costs as much as a launch)."""
+    return contextlib.nullcontext() if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+
+
+@functools.lru_cache(maxsize=1024)
+def _ce_workspace(rows, channels, classes, dtype, ld_features, ld_weight, backward):
+    return B.lp_linear_ce_workspace_bytes(B.lp_linear_ce_desc(rows, channels, classes, dtype, ld_features, ld_weight, 0), backward)
 
 
 def _rows(t, name):
@@ -69,10 +80,10 @@ def linear_ce_forward(features, weight, labels, bias=None):
     Rows whose label is outside [0, V) are left out.  Returns (loss [1], row_loss [N], lse [N]), float32: the mean over
     the rows that count, the loss of every row, and the log of every row's sum of exponentials."""
     dev, d, features, weight, labels, bias = _ce_args(features, weight, labels, bias)
-    with torch.cuda.device(dev):
+    with _on(dev):
         out = torch.empty(1 + 2 * d.rows, dtype=torch.float32, device=dev)
         loss, row_loss, lse = out[:1], out[1:1 + d.rows], out[1 + d.rows:]
-        size = B.lp_linear_ce_workspace_bytes(d, False)
+        size = _ce_workspace(d.rows, d.channels, d.classes, d.dtype, d.ld_features, d.ld_weight, False)
         ws = torch.empty(size, dtype=torch.uint8, device=dev)
         B.lp_linear_ce_forward(d, torch.cuda.current_stream().cuda_stream, features.data_ptr(), weight.data_ptr(), _ptr(bias), labels.data_ptr(),
                                loss.data_ptr(), row_loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), size)
@@ -87,11 +98,11 @@ def linear_ce_backward(features, weight, labels, lse, bias=None, scale=1.0):
     if lse.shape != (d.rows,) or lse.dtype != torch.float32:
         raise ValueError(f"lse: expected float32 [{d.rows}], got {lse.dtype} {tuple(lse.shape)}")
     lse = lse.contiguous()
-    with torch.cuda.device(dev):
+    with _on(dev):
         dx = torch.empty((d.rows, d.channels), dtype=features.dtype, device=dev)
         dw = torch.empty((d.classes, d.channels), dtype=torch.float32, device=dev)
         db = None if bias is None else torch.empty(d.classes, dtype=torch.float32, device=dev)
-        size = B.lp_linear_ce_workspace_bytes(d, True)
+        size = _ce_workspace(d.rows, d.channels, d.classes, d.dtype, d.ld_features, d.ld_weight, True)
         ws = torch.empty(size, dtype=torch.uint8, device=dev)
         B.lp_linear_ce_backward(d, torch.cuda.current_stream().cuda_stream, features.data_ptr(), weight.data_ptr(), _ptr(bias), labels.data_ptr(),
                                 lse.data_ptr(), scale, dx.data_ptr(), dw.data_ptr(), _ptr(db), ws.data_ptr(), size)
@@ -117,7 +128,7 @@ def orthogonalize(matrices, steps=5, out_dtype=None):
         mats[i] = B.lp_matrix(m.shape[0], m.shape[1], _DTYPES[m.dtype], _DTYPES[o], m.data_ptr(), out.data_ptr(), _ld(m), 0)
     if dev is None:
         return outs
-    with torch.cuda.device(dev):
+    with _on(dev):
         size = B.lp_orthogonalize_workspace_bytes(mats)
         ws = torch.empty(size, dtype=torch.uint8, device=dev)
         B.lp_orthogonalize(torch.cuda.current_stream().cuda_stream, mats, steps, ws.data_ptr(), size)
@@ -154,7 +165,7 @@ def muon_update(table, params, grads, velocity, master=None, *, lr, momentum=0.9
         if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or 4 * t.numel() < gend):
             raise ValueError(f"{name}: expected {gend // 4} float32, contiguous, got {t.dtype} {tuple(t.shape)}")
     opts = B.lp_muon_opts(lr, momentum, weight_decay, lr if rest_lr is None else rest_lr, int(nesterov), steps)
-    with torch.cuda.device(dev):
+    with _on(dev):
         ws = torch.empty(size, dtype=torch.uint8, device=dev)
         B.lp_muon_step(torch.cuda.current_stream().cuda_stream, arr, params.data_ptr(), grads.data_ptr(), velocity.data_ptr(), _ptr(master),
                        opts, ws.data_ptr(), size)

@@ -100,6 +100,10 @@ SHAPES = [
     (1, 1, 1), (1, 16, 10), (4, 8, 2), (33, 17, 5), (65, 640, 100), (256, 16, 10), (130, 72, 257), (64, 2048, 1000), (5, 1000, 63),
     # few rows and many classes; tiles of 64, 128, 256; ragged on every side
     (1, 128, 20000), (31, 200, 17001), (300, 333, 3001), (1000, 64, 8200), (1025, 40, 17000), (2500, 96, 8195), (8192, 40, 90),
+    # around the limits of what is small: rows, channels, classes, and the work of all
+    (1024, 3, 5), (1025, 3, 5), (2, 14980, 3), (2, 15010, 3), (3, 9, 2990), (3, 9, 3010), (256, 9, 880), (512, 64, 512), (512, 64, 520), (7, 300, 800),
+    # columns of few classes over many rows
+    (3399, 171, 22),
 ]
 
 
