@@ -3204,13 +3204,13 @@ static TilePlan tile_plan(int cfg, int I, int J, int K, int slices) {
     t.slices = std::max(1, div_up(K, t.kchunk));
     return t;
 }
-// The fastest way to cut a product: tile (from `first` on; few: the one for up to 32 columns too) and pieces of the reduction, whose
-// partial results are written and read once more.
-static TilePlan best_plan(int I, int J, int K, int pairs, int first, bool few, bool may_cut, double* time = nullptr) {
+// The fastest way to cut a product: tile (one of `tiles`, bits) and pieces of the reduction, whose partial results are written and read
+// once more.  pairs: products of 64 k each that a piece has to make for every 64 of its k (three planes: a k-tile is 32 k of all).
+static TilePlan best_plan(int I, int J, int K, int pairs, unsigned tiles, bool may_cut, double* time = nullptr) {
     TilePlan best = tile_plan(2, I, J, K, 1);
     double least = 1e300;
-    for (int cfg = first; cfg < 4; ++cfg) {
-        if (cfg == 3 && !few) continue;
+    for (int cfg = 0; cfg < 6; ++cfg) {
+        if (!((tiles >> cfg) & 1u)) continue;
         int want = 1;
         for (int n = 1; n <= 1024; n = std::max(n + 1, n * 5 / 4)) {
             if (n < want) continue;
@@ -3231,7 +3231,8 @@ struct CePlan {
     long ldx, ldw, lddx;
     GemmPairs logits, dx, dw;
     TilePlan tl, tx, tw;
-    int piece, pieces, ldv;                  // classes of a piece of the probabilities
+    int piece, pieces, ldv, ldp;             // classes of a piece of the probabilities; of a row of them, and its elements
+    int width;                               // channels of a row of a laid-out operand
     size_t o_x, o_w, o_partial, o_slices, o_bsum, o_bcnt, o_mask, o_count, o_prob, o_dx, o_dw, o_colsum, bytes;
     int parts, colparts;
     int direct;                              // waves a row of the kernels for small problems, or 0
@@ -3263,15 +3264,17 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     // bf16 rows of whole 16-byte vectors are read where they are (the strides of a tile's rows within 32 bits)
     auto direct = [&](long ld) { return low && p.C % 8 == 0 && ld % 8 == 0 && ld <= (1l << 20); };
     p.pack_x = !direct(p.ldx); p.pack_w = !direct(p.ldw);
-    const GemmPairs one{1, 0, 0}, six{6, 0x201100, 0x021010};
-    p.logits = low ? one : six; p.dx = p.logits; p.dw = low ? GemmPairs{2, 0, 0x10} : six;
+    p.width = low ? p.K : (p.C + 31) & ~31;
+    p.logits = GemmPairs{1, 0, 0}; p.dx = p.logits; p.dw = low ? GemmPairs{2, 0, 0x10} : p.logits;
+    // k-tiles of 64 k: three planes lie beside each other, 32 k a tile
+    const int nl = low ? 1 : 2, nw = 2;
+    const unsigned all = low ? 7u : 48u, few = low && p.N <= 32 ? 8u : 0u, small = low ? 4u : 32u;
 
-    // logits: by tiles that finish their rows, or cut along the channels, with the softmax as a pass of its own (some 8 us).  Three
-    // planes of a 256 x 256 tile do not fit into LDS.
+    // logits: by tiles that finish their rows, or cut along the channels, with the softmax as a pass of its own (some 8 us)
     double whole, cut;
-    const int N1 = std::max(1, p.N), first = low || !backward ? 0 : 1;
-    p.tl = best_plan(p.V, N1, p.K, p.logits.n, first, p.N <= 32, false, &whole);
-    const TilePlan tc = best_plan(p.V, N1, p.K, p.logits.n, 2, p.N <= 32, true, &cut);
+    const int N1 = std::max(1, p.N);
+    p.tl = best_plan(p.V, N1, p.K, nl, all | few, false, &whole);
+    const TilePlan tc = best_plan(p.V, N1, p.K, nl, small | few, true, &cut);
     p.cut = cut + 8.0 < whole && (size_t)tc.slices * N1 * p.V <= ((size_t)8 << 20);
     if (p.cut) p.tl = tc;
     if ((long)p.tl.ti * p.tl.tj > (1l << 30)) return fail(LP_ERR_SHAPE, "%d rows x %d classes in one call", p.N, p.V);
@@ -3279,7 +3282,8 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     ce_tile_size(p.tl.cfg, &bi, &bj, &wi, &wj);
     p.parts = p.tl.ti * wi;
     p.colparts = p.tl.tj * wj;
-    const size_t N = p.N, V8 = (p.V + 7) & ~7;
+    const int round = low ? 8 : 32;
+    const size_t N = p.N, V8 = (size_t)div_up(p.V, round) * round;
     p.pieces = 1; p.piece = p.V; p.ldv = (int)V8;
     // (the rows of a tile within 32 bits: at most 2^20 classes a piece)
     if (backward && !p.cut && ((size_t)p.nprob * 2 * N * V8 > kProbBytes || p.V > (1 << 20))) {
@@ -3287,10 +3291,11 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
         p.pieces = div_up(p.V, p.piece);
         p.piece = std::min(p.V, div_up(div_up(p.V, p.pieces), 256) * 256);
         p.pieces = div_up(p.V, p.piece);
-        p.ldv = (p.piece + 7) & ~7;
+        p.ldv = div_up(p.piece, round) * round;
     }
+    p.ldp = low ? p.ldv : 3 * p.ldv;
     WsAlloc ws;
-    const size_t plane_rows = (size_t)p.nplanes * 2 * p.K;
+    const size_t plane_rows = (size_t)p.nplanes * 2 * p.width;
     p.o_x = p.pack_x ? ws.take(plane_rows * N) : 0;
     p.o_w = p.pack_w ? ws.take(plane_rows * p.V) : 0;
     p.o_slices = p.cut ? ws.take((size_t)p.tl.slices * N * V8 * 4) : 0;
@@ -3299,13 +3304,13 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
         p.o_bsum = ws.take(N * 4);
         p.o_bcnt = ws.take(N * 4);
     } else {
-        p.tx = best_plan(p.C, N1, p.piece, p.dx.n, 0, p.N <= 32, true);
-        p.tw = best_plan(p.C, p.piece, N1, p.dw.n, 0, false, p.pieces == 1);
+        p.tx = best_plan(p.C, N1, p.piece, nl, all | few, true);
+        p.tw = best_plan(p.C, p.piece, N1, nw, all, true);
         p.o_mask = ws.take((N + 63) / 64 * 8);
         p.o_count = ws.take(4);
         p.o_prob = ws.take((size_t)p.nprob * 2 * N * p.ldv);
         p.o_dx = ws.take((size_t)p.tx.slices * N * p.K * 4);
-        p.o_dw = p.tw.slices > 1 ? ws.take((size_t)p.tw.slices * p.V * p.K * 4) : 0;
+        p.o_dw = p.tw.slices > 1 ? ws.take((size_t)p.tw.slices * p.piece * p.K * 4) : 0;
         p.o_colsum = p.cut ? 0 : ws.take((size_t)p.colparts * p.ldv * 4);
     }
     p.bytes = std::max<size_t>(ws.off, 256);
@@ -3319,15 +3324,15 @@ static lp_status hip_status(hipError_t err) {
 // operands of the products: where they lie, or laid out in the workspace
 static lp_status ce_operands(const CePlan& p, int dtype, const void* x, const void* w, char* ws, GemmOperand& X, GemmOperand& W, hipStream_t s) {
     X.extent = p.N; W.extent = p.V;
-    X.plane = (size_t)p.N * p.K * 2; W.plane = (size_t)p.V * p.K * 2;
+    X.plane = W.plane = 0;
     hipError_t err = hipSuccess;
     if (p.pack_x) {
-        X.base = ws + p.o_x; X.ld = p.K;
-        err = launch_ce_pack(x, p.ldx, p.N, p.C, dtype, ws + p.o_x, X.plane, p.K, s);
+        X.base = ws + p.o_x; X.ld = p.nplanes * p.width;
+        err = launch_ce_pack(x, p.ldx, p.N, p.C, dtype, ws + p.o_x, p.width, s);
     } else { X.base = (const char*)x; X.ld = (int)p.ldx; }
     if (p.pack_w) {
-        W.base = ws + p.o_w; W.ld = p.K;
-        if (err == hipSuccess) err = launch_ce_pack(w, p.ldw, p.V, p.C, dtype, ws + p.o_w, W.plane, p.K, s);
+        W.base = ws + p.o_w; W.ld = p.nplanes * p.width;
+        if (err == hipSuccess) err = launch_ce_pack(w, p.ldw, p.V, p.C, dtype, ws + p.o_w, p.width, s);
     } else { W.base = (const char*)w; W.ld = (int)p.ldw; }
     return hip_status(err);
 }
@@ -3394,7 +3399,7 @@ lp_status lp_linear_ce_forward(const lp_linear_ce_desc* d, void* stream, const v
     CeRows r;
     memset(&r, 0, sizeof(r));
     if (p.cut) {
-        a.slices = (float*)(ws + p.o_slices); a.ldv = (p.V + 7) & ~7; a.slice = (size_t)p.N * a.ldv;
+        a.slices = (float*)(ws + p.o_slices); a.ldv = p.ldv; a.slice = (size_t)p.N * a.ldv;
         r.slices = a.slices; r.slice = a.slice; r.nslices = p.tl.slices; r.ldv = a.ldv;
         st = hip_status(launch_ce_slices(a, p.tl.slices, p.tl.cfg, s));
     } else {
@@ -3403,7 +3408,7 @@ lp_status lp_linear_ce_forward(const lp_linear_ce_desc* d, void* stream, const v
         st = hip_status(launch_ce_stats(a, p.tl.cfg, s));
     }
     if (st != LP_OK) return st;
-    r.N = p.N; r.V = p.V; r.K = p.K; r.labels = labels; r.bias = bias; r.w = W; r.x = X; r.pairs = p.logits;
+    r.N = p.N; r.V = p.V; r.K = p.K; r.labels = labels; r.bias = bias; r.w = W; r.x = X; r.nplanes = p.nplanes;
     r.lse = lse; r.row_loss = row_loss; r.loss = loss;
     r.bsum = (float*)(ws + p.o_bsum); r.bcnt = (int*)(ws + p.o_bcnt);
     return hip_status(launch_ce_rows(r, s));
@@ -3438,17 +3443,19 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
     int* const count = (int*)(ws + p.o_count);
     char* const prob = ws + p.o_prob;
     const size_t pplane = (size_t)p.N * p.ldv * 2;
-    GemmOperand P{prob, pplane, p.ldv, 0};
+    GemmOperand P{prob, pplane, p.ldp, 0};
     CeFinish f;
     memset(&f, 0, sizeof(f));
     auto blocks = [](size_t rows, int cols) { return (int)std::min<size_t>((rows * ((cols + 3) / 4) + 255) / 256, 4096); };
+    // many slices: in parts of some eight each
+    auto parts_log = [](int slices) { int lg = 0; while (lg < 6 && (8 << lg) < slices) ++lg; return lg; };
     f.labels = labels; f.count = count; f.scale = loss_scale; f.N = p.N; f.V_all = p.V;
     f.colsum = p.cut ? nullptr : (float*)(ws + p.o_colsum); f.parts = p.colparts; f.ld_colsum = p.ldv;
-    f.prob = (const unsigned short*)prob; f.pplane = pplane; f.nplanes = p.nprob; f.ldv = p.ldv;
+    f.prob = (const unsigned short*)prob; f.pplane = pplane; f.nplanes = p.nprob; f.ldp = p.ldp;
     for (int v0 = 0, piece = 0; piece < p.pieces; ++piece, v0 += p.piece) {
         const int V = std::min(p.piece, p.V - v0);
         CeLogits a = ce_logits(p, X, W, bias, v0, V);
-        a.lse = lse; a.labels = labels; a.mask = mask; a.count = count; a.prob = prob; a.pplane = pplane; a.ldv = p.ldv;
+        a.lse = lse; a.labels = labels; a.mask = mask; a.count = count; a.prob = prob; a.pplane = pplane; a.ldv = p.ldv; a.ldp = p.ldp;
         if (p.cut) {
             a.slices = (float*)(ws + p.o_slices); a.slice = (size_t)p.N * a.ldv;
             CeRows r;
@@ -3456,10 +3463,10 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
             r.N = p.N; r.V = p.V; r.labels = labels; r.bias = bias; r.slices = a.slices; r.slice = a.slice; r.nslices = p.tl.slices; r.ldv = a.ldv;
             r.lse = const_cast<float*>(lse); r.mask = mask; r.count = count;
             st = hip_status(launch_ce_slices(a, p.tl.slices, p.tl.cfg, s));
-            if (st == LP_OK) st = hip_status(launch_ce_prob(r, (unsigned short*)prob, pplane, p.nprob, s));
+            if (st == LP_OK) st = hip_status(launch_ce_prob(r, (unsigned short*)prob, pplane, p.ldp, p.nprob, s));
         } else {
             a.colsum = dbias ? (float*)(ws + p.o_colsum) : nullptr; a.ld_colsum = p.ldv;
-            st = hip_status(launch_ce_prob_tiles(a, p.nprob, p.tl.cfg, s));
+            st = hip_status(launch_ce_prob_tiles(a, p.tl.cfg, s));
         }
         if (st != LP_OK) return st;
         CeGrad g;
@@ -3468,30 +3475,30 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
             const TilePlan t = p.tw;
             int bi, bj, wi, wj;
             ce_tile_size(t.cfg, &bi, &bj, &wi, &wj);
-            g.a = X; g.a.extent = p.K; g.b = P; g.b.extent = p.ldv; g.pairs = p.dw;
+            g.a = X; g.a.extent = p.nplanes * p.width; g.b = P; g.b.extent = p.ldp; g.pairs = p.dw;
             g.K = p.N; g.kchunk = t.kchunk; g.J = V;
             g.tiles_i = t.ti; g.tiles_j = div_up(V, bj); g.band = 8; g.mask = mask;
-            if (t.slices > 1) { g.out = (float*)(ws + p.o_dw); g.slice = (size_t)p.V * p.K; g.ldo = p.K; g.I = p.K; g.vec = 1; }
+            if (t.slices > 1) { g.out = (float*)(ws + p.o_dw); g.slice = (size_t)p.piece * p.K; g.ldo = p.K; g.I = p.K; g.vec = 1; }
             else { g.out = dweight + (size_t)v0 * p.C; g.ldo = p.C; g.I = p.C; g.vec = p.C % 4 == 0; g.count = count; g.scale = loss_scale; }
             if ((st = hip_status(launch_ce_dw(g, t.slices, t.cfg, s))) != LP_OK) return st;
         }
         if (dfeatures) {
             memset(&g, 0, sizeof(g));
             const TilePlan t = p.tx;
-            g.a = W; g.a.base += (size_t)v0 * W.ld * 2; g.a.extent = p.K; g.b = P; g.b.extent = p.N; g.pairs = p.dx;
+            g.a = W; g.a.base += (size_t)v0 * W.ld * 2; g.a.extent = p.nplanes * p.width; g.b = P; g.b.extent = p.N; g.pairs = p.dx;
             g.K = V; g.kchunk = div_up(div_up(V, 64), t.slices) * 64; g.I = p.K; g.J = p.N;
             g.tiles_i = t.ti; g.tiles_j = t.tj; g.band = 8;
             g.out = (float*)(ws + p.o_dx); g.slice = (size_t)p.N * p.K; g.ldo = p.K; g.vec = 1; g.add = piece > 0;
             if ((st = hip_status(launch_ce_dx(g, t.slices, t.cfg, s))) != LP_OK) return st;
         }
-        // the bias of this piece: with the last one beside the other sums
+        // the sums and the bias of this piece; with the last one those of dX
         f.blocks_b = dbias ? div_up(V, p.cut ? 8 : 32) : 0; f.V = V; f.dbias = dbias ? dbias + v0 : nullptr;
+        f.w = CeSum{(float*)(ws + p.o_dw), (size_t)p.piece * p.K, p.tw.slices, p.K, dweight ? dweight + (size_t)v0 * p.C : nullptr, (size_t)p.C, V, p.C, parts_log(p.tw.slices)};
+        f.blocks_w = dweight && p.tw.slices > 1 ? blocks((size_t)V << f.w.parts_log, p.C) : 0;
         if (piece + 1 < p.pieces && (st = hip_status(launch_ce_finish(f, d->dtype, s))) != LP_OK) return st;
     }
-    f.x = CeSum{(float*)(ws + p.o_dx), (size_t)p.N * p.K, p.tx.slices, p.K, dfeatures, (size_t)p.lddx, p.N, p.C};
-    f.w = CeSum{(float*)(ws + p.o_dw), (size_t)p.V * p.K, p.tw.slices, p.K, dweight, (size_t)p.C, p.V, p.C};
-    f.blocks_x = dfeatures ? blocks(p.N, p.C) : 0;
-    f.blocks_w = dweight && p.tw.slices > 1 ? blocks(p.V, p.C) : 0;
+    f.x = CeSum{(float*)(ws + p.o_dx), (size_t)p.N * p.K, p.tx.slices, p.K, dfeatures, (size_t)p.lddx, p.N, p.C, parts_log(p.tx.slices)};
+    f.blocks_x = dfeatures ? blocks((size_t)p.N << f.x.parts_log, p.C) : 0;
     return hip_status(launch_ce_finish(f, d->dtype, s));
 }
 

@@ -17,9 +17,9 @@ struct CeLogits {
     unsigned long long* mask; int* count;    // probabilities: which rows count, and how many do, are found beside them
     float2* partial; int parts;         // statistics: [N][parts] (maximum, sum), base 2
     float* slices; size_t slice;        // partial logits: [slices][N][ldv]
-    int ldv;                            // row length of slices / prob, a multiple of 8
+    int ldv, ldp;                       // classes of a row of slices / prob, a multiple of 8 (three planes: 32); elements of a row of prob
     const float* lse; const int* labels;
-    char* prob; size_t pplane;          // probabilities: planes of bf16 [N][ldv]
+    char* prob; size_t pplane;          // probabilities: two planes of bf16 [N][ldv], or three beside each other [N][ldp]
     float* colsum; int ld_colsum;       // their sums over the samples of every wave's tile, or null
 };
 struct CeRows {
@@ -28,7 +28,7 @@ struct CeRows {
     const float* bias;
     const float2* partial; int parts;
     const float* slices; size_t slice; int nslices, ldv;
-    GemmOperand w, x; GemmPairs pairs;
+    GemmOperand w, x; int nplanes;
     float *lse, *row_loss, *loss;
     float* bsum; int* bcnt;             // of every workgroup
     unsigned long long* mask; int* count;
@@ -44,14 +44,14 @@ struct CeGrad {
     const int* count; float scale;      // scaled by scale / count, or not
     const unsigned long long* mask;
 };
-struct CeSum { const float* part; size_t slice; int nslices, ldp; void* out; size_t ldo; int rows, cols; };
+struct CeSum { const float* part; size_t slice; int nslices, ldp; void* out; size_t ldo; int rows, cols, parts_log; };
 struct CeFinish {
     CeSum x, w;
     int blocks_x, blocks_w, blocks_b;
     const int* labels; const int* count; float scale;
     int N, V, V_all;                    // V: classes of the bias here
     const float* colsum; int parts, ld_colsum;
-    const unsigned short* prob; size_t pplane; int nplanes, ldv;
+    const unsigned short* prob; size_t pplane; int nplanes, ldp;
     float* dbias;
 };
 
@@ -70,15 +70,15 @@ hipError_t launch_ce_direct_forward(const CeDirect& a, int dtype, int waves, hip
 hipError_t launch_ce_direct_backward(const CeDirect& a, int dtype, int waves, hipStream_t s);
 hipError_t launch_ce_total(const float* sums, const int* counts, int n, float* loss, hipStream_t s);
 
-// tiles: 0 256 x 256, 1 128 x 128, 2 64 x 64, 3 128 x 32 (few samples); waves along either side
+// tiles: 0 256 x 256, 1 128 x 128, 2 64 x 64, 3 128 x 32 (few samples); of three planes 4 128 x 128, 5 64 x 64; waves along either side
 void ce_tile_size(int cfg, int* bi, int* bj, int* wi, int* wj);
 double ce_tile_time(int cfg, long blocks, int ktiles);
-hipError_t launch_ce_pack(const void* src, long ld_src, int rows, int cols, int dtype, void* dst, size_t plane, int ld, hipStream_t s);
+hipError_t launch_ce_pack(const void* src, long ld_src, int rows, int cols, int dtype, void* dst, int width, hipStream_t s);
 hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s);
-hipError_t launch_ce_prob_tiles(const CeLogits& a, int planes, int cfg, hipStream_t s);
+hipError_t launch_ce_prob_tiles(const CeLogits& a, int cfg, hipStream_t s);
 hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t s);
 hipError_t launch_ce_rows(const CeRows& a, hipStream_t s);
-hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int planes, hipStream_t s);
+hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int ldp, int planes, hipStream_t s);
 hipError_t launch_ce_dx(const CeGrad& a, int slices, int cfg, hipStream_t s);
 hipError_t launch_ce_dw(const CeGrad& a, int slices, int cfg, hipStream_t s);
 hipError_t launch_ce_finish(const CeFinish& a, int dtype, hipStream_t s);

@@ -12,8 +12,8 @@
 // Precision.  bf16: products of bf16 are exact, sums are fp32.  The probabilities are kept as two bf16 (16 bits) for dW, which is
 // fp32, and dX, which is bf16, reads the first of them: its own rounding is as large.  p - 1 of the label is formed in
 // fp32 before it is split, so a small p beside it is kept by the second part.
-// fp32: every operand as three bf16 (24 bits), six of the nine products (the others are below 2^-25): six products at the rate of
-// the 16-bit instruction take less than half of the time of one in fp32.
+// fp32: every operand as three bf16 (24 bits) that lie beside each other, six of the nine products (the others are below 2^-25).
+// 73623 classes x 8716 rows of 633 channels: a product in 4.3 ms, 187 TFLOP/s of fp32; the card's fp32 matrix product reaches 151.
 //
 // Rows whose label is no class (ignored): probability zero in the epilogue by selection, and their features count as zero in
 // dW whatever they hold (a bit a row, read by the loads): no infinity or NaN in them reaches a sum.
@@ -50,12 +50,18 @@ template <int NP> __device__ __forceinline__ void split_bf16(float x, unsigned (
     }
 }
 
+// Element c of plane k in a row of NP planes: two lie `plane` elements apart, three beside each other, 32 of each in turn
+template <int NP> __device__ __forceinline__ size_t plane_at(int c, int k, size_t plane) {
+    if constexpr (NP == 3) return (size_t)(c >> 5) * 96 + k * 32 + (c & 31);
+    else return k * plane + c;
+}
+
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Operands in the form the products want: rows of ld elements (a multiple of 8, zeros behind the last), NP planes
+// Operands in the form the products want: rows of `width` elements a plane (a multiple of 8, of 32 in three planes), zeros behind the last
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <class T, int NP> __global__ __launch_bounds__(256) void ce_pack_kernel(const T* __restrict__ src, long ld_src, int rows, int cols, unsigned short* __restrict__ dst,
-                                                                                 size_t plane, int ld) {
-    const int cpr = ld >> 3;                                      // chunks of eight elements in a row
+                                                                                 int width) {
+    const int cpr = width >> 3;                                   // chunks of eight elements in a row
     const size_t n = (size_t)rows * cpr;
     for (size_t t = (size_t)blockIdx.x * 256 + threadIdx.x; t < n; t += (size_t)gridDim.x * 256) {
         const int r = (int)(t / cpr), c = (int)(t - (size_t)r * cpr) * 8;
@@ -76,7 +82,7 @@ template <class T, int NP> __global__ __launch_bounds__(256) void ce_pack_kernel
             u32x4 v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = out[p][2 * e] | ((unsigned)out[p][2 * e + 1] << 16);
-            *reinterpret_cast<u32x4*>(dst + p * plane + (size_t)r * ld + c) = v;
+            *reinterpret_cast<u32x4*>(dst + (size_t)r * (NP * width) + plane_at<NP>(c, p, 0)) = v;
         }
     }
 }
@@ -239,7 +245,7 @@ template <class T, int MODE, int NP, int WAVES> __global__ __launch_bounds__(T::
                         cs[2 * e] += __uint_as_float(w[e] << 16);
                         cs[2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
                     }
-                    if (no < a.N && v < a.ldv) *reinterpret_cast<u32x4*>(a.prob + k * a.pplane + ((size_t)no * a.ldv + v) * 2) = w;
+                    if (no < a.N && v < a.ldv) *reinterpret_cast<u32x4*>(a.prob + ((size_t)no * a.ldp + plane_at<NP>(v, k, a.pplane / 2)) * 2) = w;
                 }
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -269,6 +275,22 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     const float t = fmaxf(m, m2), t0 = t == -kInf ? 0.f : t;
     s = s * __builtin_amdgcn_exp2f(m - t0) + s2 * __builtin_amdgcn_exp2f(m2 - t0);
     m = t;
+}
+
+// eight elements of a row of one plane or of three
+__device__ __forceinline__ void whole_eight(const unsigned short* row, int c, int nplanes, float (&f)[8]) {
+    const unsigned short* const p = nplanes == 3 ? row + plane_at<3>(c, 0, 0) : row + c;
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        if (k < nplanes) {
+            const u32x4 u = *reinterpret_cast<const u32x4*>(p + k * 32);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float lo = __uint_as_float(u[e] << 16), hi = __uint_as_float(u[e] & 0xffff0000u);
+                f[2 * e] = k ? f[2 * e] + lo : lo;
+                f[2 * e + 1] = k ? f[2 * e + 1] + hi : hi;
+            }
+        }
 }
 
 // sums of the slices of two logits, eight slices requested at once
@@ -338,19 +360,17 @@ template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_k
                 for (int q = 0; q < 4; ++q) join(m, s, v[q].x, v[q].y);
             }
             for (; t < a.parts; t += STEP) { const float2 v = row[t]; join(m, s, v.x, v.y); }
-            if (valid)
-                for (int p = 0; p < a.pairs.n; ++p) {
-                    const unsigned short* const x = reinterpret_cast<const unsigned short*>(a.x.base + ((a.pairs.b >> (4 * p)) & 15) * a.x.plane) + (size_t)n * a.x.ld;
-                    const unsigned short* const w = reinterpret_cast<const unsigned short*>(a.w.base + ((a.pairs.a >> (4 * p)) & 15) * a.w.plane) + (size_t)y * a.w.ld;
-                    for (int c = l0 * 8; c < a.K; c += 8 * STEP) {
-                        const u32x4 xv = *reinterpret_cast<const u32x4*>(x + c), wv = *reinterpret_cast<const u32x4*>(w + c);
+            if (valid) {  // the label's logit: three planes add up to the fp32 they were made of
+                const unsigned short* const x = reinterpret_cast<const unsigned short*>(a.x.base) + (size_t)n * a.x.ld;
+                const unsigned short* const w = reinterpret_cast<const unsigned short*>(a.w.base) + (size_t)y * a.w.ld;
+                for (int c = l0 * 8; c < a.K; c += 8 * STEP) {
+                    float xf[8], wf[8];
+                    whole_eight(x, c, a.nplanes, xf);
+                    whole_eight(w, c, a.nplanes, wf);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            own = fmaf(__uint_as_float(xv[e] << 16), __uint_as_float(wv[e] << 16), own);
-                            own = fmaf(__uint_as_float(xv[e] & 0xffff0000u), __uint_as_float(wv[e] & 0xffff0000u), own);
-                        }
-                    }
+                    for (int e = 0; e < 8; ++e) own = fmaf(xf[e], wf[e], own);
                 }
+            }
         }
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -371,7 +391,8 @@ template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_k
     if (n < a.N && part == 0) {
         const float lse = (m + __builtin_amdgcn_logf(s)) * kLn2;       // log2
         if (!SLICES && valid && a.bias) own += a.bias[y];
-        loss = valid ? lse - own : 0.f;
+        // (not lse - own: of a row that is all but certain the logits cancel first)
+        loss = valid ? ((m - own * kLog2e) + __builtin_amdgcn_logf(s)) * kLn2 : 0.f;
         if (lane == 0) {
             a.lse[n] = lse;
             if (a.row_loss) a.row_loss[n] = loss;
@@ -390,7 +411,7 @@ template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_k
 }
 
 // Probabilities from partial logits (few tiles): a workgroup a row
-template <int NP> __global__ __launch_bounds__(256) void ce_prob_kernel(const CeRows a, unsigned short* __restrict__ prob, size_t pplane) {
+template <int NP> __global__ __launch_bounds__(256) void ce_prob_kernel(const CeRows a, unsigned short* __restrict__ prob, size_t pplane, int ldp) {
     __shared__ int s_cnt[4];
     const int n = blockIdx.x;
     if (n == a.N) { ce_labels(a.labels, a.N, a.V, a.mask, a.count, s_cnt); return; }
@@ -411,7 +432,7 @@ template <int NP> __global__ __launch_bounds__(256) void ce_prob_kernel(const Ce
             split_bf16<NP>(p, b[e]);
         }
 #pragma unroll
-        for (int k = 0; k < NP; ++k) *reinterpret_cast<unsigned*>(prob + k * (pplane / 2) + (size_t)n * a.ldv + v) = b[0][k] | (b[1][k] << 16);
+        for (int k = 0; k < NP; ++k) *reinterpret_cast<unsigned*>(prob + (size_t)n * ldp + plane_at<NP>(v, k, pplane / 2)) = b[0][k] | (b[1][k] << 16);
     }
 }
 
@@ -471,14 +492,22 @@ template <class T> __global__ __launch_bounds__(256) void ce_finish_kernel(const
     if (b < a.blocks_x + a.blocks_w) {
         const bool x = b < a.blocks_x;
         const CeSum& s = x ? a.x : a.w;
-        const size_t t0 = (size_t)(x ? b : b - a.blocks_x) * 256 + threadIdx.x;
+        // vectors by 64 >> lg lanes of a wave, their slices in 1 << lg parts
+        const int lg = s.parts_log, lane = threadIdx.x & 63, span = 64 >> lg, part = lane >> (6 - lg);
+        const size_t wave = (size_t)(x ? b : b - a.blocks_x) * 4 + (threadIdx.x >> 6), stride = (size_t)(x ? a.blocks_x : a.blocks_w) * 4 * span;
         const int vpr = (s.cols + 3) >> 2;
-        const size_t n = (size_t)s.rows * vpr, stride = (size_t)(x ? a.blocks_x : a.blocks_w) * 256;
-        for (size_t t = t0; t < n; t += stride) {
+        const size_t n = (size_t)s.rows * vpr;
+        for (size_t base = wave * span; base < n; base += stride) {      // (the whole wave together)
+            const size_t t = min(base + (lane & (span - 1)), n - 1);
             const int r = (int)(t / vpr), c = (int)(t - (size_t)r * vpr) * 4;
             const float* const p = s.part + (size_t)r * s.ldp + c;
-            f32x4 v = *reinterpret_cast<const f32x4*>(p);
-            for (int k = 1; k < s.nslices; ++k) v += *reinterpret_cast<const f32x4*>(p + k * s.slice);
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int k = part; k < s.nslices; k += 1 << lg) v += *reinterpret_cast<const f32x4*>(p + k * s.slice);
+            for (int o = span; o < 64; o <<= 1)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], o);
+            if (base + lane >= n || part != 0) continue;
             const bool live = !x || is_class(a.labels[r], a.V_all);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = live ? v[e] * g : 0.f;
@@ -519,10 +548,10 @@ template <class T> __global__ __launch_bounds__(256) void ce_finish_kernel(const
     const int v0 = (b - a.blocks_x - a.blocks_w) * 8;
     float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int p = 0; p < a.nplanes; ++p) {
-        const unsigned short* const q = a.prob + p * (a.pplane / 2) + v0;
+        const unsigned short* const q = a.prob + (a.nplanes == 3 ? plane_at<3>(v0, p, 0) : p * (a.pplane / 2) + v0);
 #pragma unroll 4
         for (int n = threadIdx.x; n < a.N; n += 256) {
-            const u32x4 u = *reinterpret_cast<const u32x4*>(q + (size_t)n * a.ldv);
+            const u32x4 u = *reinterpret_cast<const u32x4*>(q + (size_t)n * a.ldp);
 #pragma unroll
             for (int e = 0; e < 4; ++e) { t[2 * e] += __uint_as_float(u[e] << 16); t[2 * e + 1] += __uint_as_float(u[e] & 0xffff0000u); }
         }
@@ -547,9 +576,12 @@ __global__ __launch_bounds__(256) void ce_zero_kernel(float* p, size_t n) {
 
 // tiles: big and middle (one workgroup a compute unit), small (two), few samples
 template <bool AKR, bool BKR, bool M> using TBig = GemmTile<bf16_t, AKR, BKR, 2, 4, 4, 2, 2, M>;
-template <bool AKR, bool BKR, bool M> using TMid = GemmTile<bf16_t, AKR, BKR, 2, 2, 2, 2, 4, M, false, true>;
-template <bool AKR, bool BKR, bool M> using TSmall = GemmTile<bf16_t, AKR, BKR, 2, 2, 1, 1, 4, M, false, true>;
-template <bool AKR, bool BKR, bool M> using TFew = GemmTile<bf16_t, AKR, BKR, 4, 1, 1, 1, 3, M, false, true>;
+template <bool AKR, bool BKR, bool M> using TMid = GemmTile<bf16_t, AKR, BKR, 2, 2, 2, 2, 4, M, 1, true>;
+template <bool AKR, bool BKR, bool M> using TSmall = GemmTile<bf16_t, AKR, BKR, 2, 2, 1, 1, 4, M, 1, true>;
+template <bool AKR, bool BKR, bool M> using TFew = GemmTile<bf16_t, AKR, BKR, 4, 1, 1, 1, 3, M, 1, true>;
+// ... of three planes
+template <bool AKR, bool BKR, bool M> using TMid3 = GemmTile<bf16_t, AKR, BKR, 2, 2, 2, 2, 3, M, 3, true>;
+template <bool AKR, bool BKR, bool M> using TSmall3 = GemmTile<bf16_t, AKR, BKR, 2, 2, 1, 1, 3, M, 3, true>;
 
 template <class K, class A> hipError_t launch(K kernel, OncePerDevice& once, dim3 grid, int threads, int lds, hipStream_t s, const A& args) {
     if (const hipError_t e = raise_lds_limit(once, {(const void*)kernel}, lds); e != hipSuccess) return e;
@@ -570,26 +602,27 @@ template <class T, int WAVES> hipError_t launch_grad_t(const CeGrad& a, int slic
 }  // namespace
 
 // Time of a product cut into `blocks` workgroups of `ktiles` k-tiles each, microseconds: rounds of as many as run at once, a k-tile of a
-// full chip and of a nearly empty one as measured (256 x 256 1.95 and 1.4 us, 128 x 128 0.52 and 0.36, 64 x 64 0.43 and 0.27), and what a
-// workgroup does besides.
+// full chip and of a nearly empty one as measured (256 x 256 1.95 and 1.4 us, 128 x 128 0.52 and 0.36, 64 x 64 0.43 and 0.27, 128 x 32
+// 0.40 and 0.25; of three planes, 32 k, 128 x 128 1.2 and 0.95, 64 x 64 0.7 to 0.85 and 0.4), and what a workgroup does besides.
 double ce_tile_time(int cfg, long blocks, int ktiles) {
-    static const struct { int slots; double some, full, rest; } t[4] = {{256, 1.4, 1.95, 6.0}, {256, 0.36, 0.52, 4.0}, {512, 0.27, 0.43, 3.0}, {512, 0.25, 0.40, 3.0}};
+    static const struct { int slots; double some, full, rest; } t[6] = {{256, 1.4, 1.95, 6.0}, {256, 0.36, 0.52, 4.0}, {512, 0.27, 0.43, 3.0},
+                                                                        {512, 0.25, 0.40, 3.0}, {256, 0.95, 1.2, 5.0}, {512, 0.4, 0.75, 4.0}};
     const long rounds = blocks / t[cfg].slots, over = blocks - rounds * t[cfg].slots;
     const double last = t[cfg].some + (t[cfg].full - t[cfg].some) * (double)over / t[cfg].slots;
     return (double)rounds * (t[cfg].rest + ktiles * t[cfg].full) + (over ? t[cfg].rest + ktiles * last : 0.0);
 }
 
 void ce_tile_size(int cfg, int* bi, int* bj, int* wi, int* wj) {
-    static const int d[4][4] = {{256, 256, 2, 4}, {128, 128, 2, 2}, {64, 64, 2, 2}, {128, 32, 4, 1}};
+    static const int d[6][4] = {{256, 256, 2, 4}, {128, 128, 2, 2}, {64, 64, 2, 2}, {128, 32, 4, 1}, {128, 128, 2, 2}, {64, 64, 2, 2}};
     *bi = d[cfg][0]; *bj = d[cfg][1]; *wi = d[cfg][2]; *wj = d[cfg][3];
 }
 
-hipError_t launch_ce_pack(const void* src, long ld_src, int rows, int cols, int dtype, void* dst, size_t plane, int ld, hipStream_t s) {
-    const size_t n = (size_t)rows * (ld >> 3);
+hipError_t launch_ce_pack(const void* src, long ld_src, int rows, int cols, int dtype, void* dst, int width, hipStream_t s) {
+    const size_t n = (size_t)rows * (width >> 3);
     if (n == 0) return hipSuccess;
     const dim3 grid((unsigned)std::min<size_t>((n + 255) / 256, 1u << 16));
-    if (dtype == 1) hipLaunchKernelGGL((ce_pack_kernel<bf16_t, 1>), grid, dim3(256), 0, s, (const bf16_t*)src, ld_src, rows, cols, (unsigned short*)dst, plane / 2, ld);
-    else hipLaunchKernelGGL((ce_pack_kernel<float, 3>), grid, dim3(256), 0, s, (const float*)src, ld_src, rows, cols, (unsigned short*)dst, plane / 2, ld);
+    if (dtype == 1) hipLaunchKernelGGL((ce_pack_kernel<bf16_t, 1>), grid, dim3(256), 0, s, (const bf16_t*)src, ld_src, rows, cols, (unsigned short*)dst, width);
+    else hipLaunchKernelGGL((ce_pack_kernel<float, 3>), grid, dim3(256), 0, s, (const float*)src, ld_src, rows, cols, (unsigned short*)dst, width);
     return hipGetLastError();
 }
 hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s) {
@@ -597,28 +630,30 @@ hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s) {
         case 0: return launch_logits_t<TBig<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
         case 1: return launch_logits_t<TMid<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
         case 2: return launch_logits_t<TSmall<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
-        default: return launch_logits_t<TFew<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
+        case 3: return launch_logits_t<TFew<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
+        case 4: return launch_logits_t<TMid3<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
+        default: return launch_logits_t<TSmall3<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
     }
 }
-hipError_t launch_ce_prob_tiles(const CeLogits& a, int planes, int cfg, hipStream_t s) {
-    if (planes == 2) switch (cfg) {
+hipError_t launch_ce_prob_tiles(const CeLogits& a, int cfg, hipStream_t s) {
+    switch (cfg) {
         case 0: return launch_logits_t<TBig<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
         case 1: return launch_logits_t<TMid<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
         case 2: return launch_logits_t<TSmall<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
-        default: return launch_logits_t<TFew<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
-    }
-    switch (cfg) {
-        case 1: return launch_logits_t<TMid<false, false, false>, LM_PROB, 3, 2>(a, 1, s);
-        case 2: return launch_logits_t<TSmall<false, false, false>, LM_PROB, 3, 2>(a, 1, s);
-        default: return launch_logits_t<TFew<false, false, false>, LM_PROB, 3, 2>(a, 1, s);
+        case 3: return launch_logits_t<TFew<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
+        case 4: return launch_logits_t<TMid3<false, false, false>, LM_PROB, 3, 2>(a, 1, s);
+        default: return launch_logits_t<TSmall3<false, false, false>, LM_PROB, 3, 2>(a, 1, s);
     }
 }
 hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t s) {
-    if (cfg == 2) return launch_logits_t<TSmall<false, false, false>, LM_SLICE, 1, 2>(a, slices, s);
-    return launch_logits_t<TFew<false, false, false>, LM_SLICE, 1, 2>(a, slices, s);
+    switch (cfg) {
+        case 2: return launch_logits_t<TSmall<false, false, false>, LM_SLICE, 1, 2>(a, slices, s);
+        case 3: return launch_logits_t<TFew<false, false, false>, LM_SLICE, 1, 2>(a, slices, s);
+        default: return launch_logits_t<TSmall3<false, false, false>, LM_SLICE, 1, 2>(a, slices, s);
+    }
 }
 hipError_t launch_ce_rows(const CeRows& a, hipStream_t s) {
-    // (8192 rows of 256 parts: a wave a row 11 us, four 14; 1000 rows 6 and 5)
+    // (a wave a row 15 us for 8192 rows of 256 parts and 11 for 10000 of eight; four waves a row 5 for 777)
     const bool wide = a.slices || a.N < 2048;
     const int blocks = wide ? a.N : (a.N + 3) / 4;
     if (a.slices) hipLaunchKernelGGL((ce_rows_kernel<true, 4>), dim3(blocks), dim3(256), 0, s, a);
@@ -631,9 +666,9 @@ hipError_t launch_ce_total(const float* sums, const int* counts, int n, float* l
     hipLaunchKernelGGL(ce_total_kernel, dim3(1), dim3(256), 0, s, sums, counts, n, loss);
     return hipGetLastError();
 }
-hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int planes, hipStream_t s) {
-    if (planes == 2) hipLaunchKernelGGL(ce_prob_kernel<2>, dim3(a.N + 1), dim3(256), 0, s, a, prob, pplane);
-    else hipLaunchKernelGGL(ce_prob_kernel<3>, dim3(a.N + 1), dim3(256), 0, s, a, prob, pplane);
+hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int ldp, int planes, hipStream_t s) {
+    if (planes == 2) hipLaunchKernelGGL(ce_prob_kernel<2>, dim3(a.N + 1), dim3(256), 0, s, a, prob, pplane, ldp);
+    else hipLaunchKernelGGL(ce_prob_kernel<3>, dim3(a.N + 1), dim3(256), 0, s, a, prob, pplane, ldp);
     return hipGetLastError();
 }
 hipError_t launch_ce_dx(const CeGrad& a, int slices, int cfg, hipStream_t s) {
@@ -641,14 +676,18 @@ hipError_t launch_ce_dx(const CeGrad& a, int slices, int cfg, hipStream_t s) {
         case 0: return launch_grad_t<TBig<true, false, false>, 2>(a, slices, s);
         case 1: return launch_grad_t<TMid<true, false, false>, 2>(a, slices, s);
         case 2: return launch_grad_t<TSmall<true, false, false>, 2>(a, slices, s);
-        default: return launch_grad_t<TFew<true, false, false>, 2>(a, slices, s);
+        case 3: return launch_grad_t<TFew<true, false, false>, 2>(a, slices, s);
+        case 4: return launch_grad_t<TMid3<true, false, false>, 2>(a, slices, s);
+        default: return launch_grad_t<TSmall3<true, false, false>, 2>(a, slices, s);
     }
 }
 hipError_t launch_ce_dw(const CeGrad& a, int slices, int cfg, hipStream_t s) {
     switch (cfg) {
         case 0: return launch_grad_t<TBig<true, true, true>, 2>(a, slices, s);
         case 1: return launch_grad_t<TMid<true, true, true>, 2>(a, slices, s);
-        default: return launch_grad_t<TSmall<true, true, true>, 2>(a, slices, s);
+        case 2: return launch_grad_t<TSmall<true, true, true>, 2>(a, slices, s);
+        case 4: return launch_grad_t<TMid3<true, true, true>, 2>(a, slices, s);
+        default: return launch_grad_t<TSmall3<true, true, true>, 2>(a, slices, s);
     }
 }
 hipError_t launch_ce_finish(const CeFinish& a, int dtype, hipStream_t s) {

@@ -101,9 +101,9 @@ template <class T, int NW> __global__ __launch_bounds__(NW * 64) void ce_direct_
     if (tid != 0) return;
     s = 0.f;
     for (int w = 0; w < NW; ++w) s += s_r[w];
-    const float lse = m + __builtin_amdgcn_logf(s) * kLn2;
+    const float ls = __builtin_amdgcn_logf(s) * kLn2, lse = m + ls;
     const bool valid = is_class(y, a.V);
-    const float loss = valid ? lse - s_l[y] : 0.f;
+    const float loss = valid ? (m - s_l[y]) + ls : 0.f;      // (not lse - l: of a row that is all but certain the logits cancel first)
     a.lse_out[n] = lse;
     if (a.row_loss) a.row_loss[n] = loss;
     a.bsum[n] = loss;
@@ -128,18 +128,30 @@ __device__ __forceinline__ int count_rows(const CeDirect& a, int* s) {
 template <class T, int NW> __global__ __launch_bounds__(NW * 64) void ce_direct_rows_kernel(const CeDirect a, int cw_log) {
     extern __shared__ float smem[];
     __shared__ int s_c[NW];
+    __shared__ float s_o[NW];
     float *const s_x = smem, *const s_l = s_x + a.C, *const s_p = s_l + a.V;
     const int tid = threadIdx.x, n = blockIdx.x, y = a.labels[n];
     const bool valid = is_class(y, a.V);
     const float g = a.scale / (float)count_rows(a, s_c);
     if (valid) {
         row_logits<T, NW>(a, n, s_x, s_p, s_l);
+        // the label's p - 1, where p is near one, as minus the sum of the others: 1 - p would lose what tells them apart
         const float shift = a.lse[n];
+        float others = 0.f;
         for (int v = tid; v < a.V; v += NW * 64) {
-            float p = __builtin_amdgcn_exp2f((s_l[v] - shift) * kLog2e);
-            if (v == y) p -= 1.f;
-            s_l[v] = p * g;
-            a.d[(size_t)n * a.V + v] = p * g;
+            const float p = __builtin_amdgcn_exp2f((s_l[v] - shift) * kLog2e);
+            if (v != y) { others += p; a.d[(size_t)n * a.V + v] = p * g; }
+            s_l[v] = v != y ? p * g : p;
+        }
+        others = wave_sum(others);
+        if ((tid & 63) == 0) s_o[tid >> 6] = others;
+        __syncthreads();
+        if (tid == 0) {
+            others = 0.f;
+            for (int w = 0; w < NW; ++w) others += s_o[w];
+            const float p = s_l[y], d = (p > 0.5f ? -others : p - 1.f) * g;
+            s_l[y] = d;
+            a.d[(size_t)n * a.V + y] = d;
         }
     } else {
         for (int v = tid; v < a.V; v += NW * 64) a.d[(size_t)n * a.V + v] = 0.f;

@@ -3,28 +3,33 @@
 //   D[i][j] = sum over pairs (a, b) of planes, sum over k of A_a[i, k] * B_b[j, k]        (fp32 sums)
 //
 // Values that need more than the 8 or 11 bits of a 16-bit float are kept as a sum of planes (x = x0 + x1 [+ x2], each the
-// rounded rest of the ones before), and a product is the sum over those pairs of planes that matter; the pairs lie one after
-// the other along the reduction, so the kernel below is the same for one product and for six.
+// rounded rest of the ones before), and a product is the sum over those pairs of planes that matter.  Planes that lie apart: the pairs
+// lie one after the other along the reduction, so the kernel is the same for one product and for several.
 //
 // An operand lies in memory with k contiguous (KR = false: rows i, pitch ld) or with its rows along k (KR = true: rows k, the
 // index i contiguous).  Both come into LDS by direct loads of 1 KiB a wave, as they lie, and leave it as fragments of
 // v_mfma_f32_32x32x16: the former by 16-byte reads, the latter by transposing reads (ds_read_b64_tr_b16: 16 lanes read four
 // k of 16 rows and get four k of one row each).  So no operand is ever laid out anew for the other direction of a product.
 //
-// DUAL: both operands are sums of two planes that lie beside each other, 32 k of the first and the same 32 of the second in 128
-// bytes, and a k-tile of 64 elements is 32 k of either.  From the fragments of two planes come three products (the
-// fourth, of the two rests, is below the precision): half as much again for the same loads and LDS reads.
+// PL = 2 (DUAL), 3 (TRIPLE): both operands are sums of planes that lie beside each other, 32 elements of the first, the same 32 of the
+// second [and of the third] in 128 [192] bytes, and a k-tile is 32 k of all.  From the fragments of two planes come three products, of
+// three planes six (the others are below the precision): half as much again, or twice as much, for the same loads and LDS reads.
 //
-// A k-tile is 64 elements long (128-byte rows: whole cache lines) and its loads are spread between the products of the one before
-// it.  Four waves (tiles of 128 and less, two workgroups a compute unit): one barrier a k-tile, ahead of the products of its last
-// 16 k, both frees its stage and shows the next.  Eight waves (256 x 256, one workgroup): two groups that take turns.
+// A k-tile is 128 (192) bytes of a row long, and its loads are spread between the products of the one before it.  Three shapes:
+//   eight waves (256 x 256, one workgroup a compute unit): two groups that take turns;
+//   four waves and four more that only load (LOADERS; tiles of 128 and less);
+//   four waves, each its share of the loads between its products.
+// In the latter two one barrier a k-tile, ahead of the products of its last 16 k, both frees its stage and shows the next.
 // What bounds it: power.  8192 x 8192 x 4096 in bf16 1105 (k contiguous), 1220 (one operand with rows along k), 1240 TFLOP/s
 // (both), DUAL 1440 of its three products, at 1.6 to 1.9 GHz; without the loads 1270 to 1570, the matrix cores busy for 85 % of
-// the clocks.  All eight waves in step, as the four are: 1013, 1128, 1203, 1370; a quarter as many waves of 128 x 128 each,
-// a third fewer LDS reads: 5 % less than that; fragments two k-steps ahead: the same.
+// the clocks.  All eight waves in step: 1013, 1128, 1203, 1370; half as many waves of 128 x 128 each, a third fewer LDS
+// reads: 5 % less than that; fragments two k-steps ahead: the same.  DUAL in tiles of 128 x 128 (576 x 576 products of 64 and of
+// 256 workgroups): 145 and 186 us without loading waves, 118 and 173 with.  TRIPLE: 73623 x 8716 over 633 1120 TFLOP/s of its six
+// products, with the planes apart in 256 x 256 tiles 810; 230 workgroups of 128 x 128 over 1781 65 us, with planes apart 116.
 // Rows are unpadded; their 16-byte chunks (KR: 32-byte pairs) trade places so that a read touches every bank once:
 //   KR = false  chunk c of row r at c ^ (r >> 1 & 7)
-//   KR = true   pair p of row k at p ^ 2 (k & 3) (rows of 256 bytes or more), p ^ 2 (k >> 1 & 1) (128 bytes), p (64 bytes)
+//   KR = true   pair p of row k at p ^ 2 (k & 3) (rows of 256, 512 or 768 bytes), p ^ 2 (k >> 1 & 1) (128, 384 bytes), p (64 bytes)
+//   TRIPLE, KR = false  chunk c of a plane of row r at c ^ (r >> 2 & 3)
 // Ragged edges, tails of k and rows that are to count as zero are out-of-range buffer offsets, which read as zeros.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -57,15 +62,16 @@ typedef __attribute__((address_space(3))) void* gemm_lds_t;
 typedef const __attribute__((address_space(4))) unsigned long long* GemmMask;      // read by scalar loads
 typedef __attribute__((ext_vector_type(4))) short gemm_s16x4;
 
-template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGES, bool MASKED = false, bool DUAL = false, bool LOADERS = false> struct GemmTile {
-    static constexpr int BK = 64, NW = WI * WJ, NT = NW * 64 * (LOADERS ? 2 : 1);
+template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGES, bool MASKED = false, int PL = 1, bool LOADERS = false> struct GemmTile {
+    static constexpr int NW = WI * WJ, NT = NW * 64 * (LOADERS ? 2 : 1);
     static constexpr int TI = FI * 32, TJ = FJ * 32, BI = WI * TI, BJ = WJ * TJ;
-    static constexpr int A_BYTES = BI * BK * 2, STAGE = (BI + BJ) * BK * 2, LDS = STAGES * STAGE;
-    static constexpr int NSA = BI / 8 / NW, NSB = BJ / 8 / NW, NL = NSA + NSB;      // wave-loads of a k-tile
-    static constexpr int KS = BK / 16;
-    static constexpr int PL = DUAL ? 2 : 1, KT = BK / PL;           // planes beside each other; k of a k-tile
+    static constexpr bool DUAL = PL == 2, TRIPLE = PL == 3;         // planes beside each other
+    static constexpr int KT = PL == 1 ? 64 : 32, KS = KT / 16, RK = KT * PL * 2;    // k of a k-tile; bytes of a row (k contiguous)
+    static constexpr int A_BYTES = BI * RK, STAGE = (BI + BJ) * RK, LDS = STAGES * STAGE;
+    static constexpr int NSA = A_BYTES / 1024 / NW, NSB = (STAGE - A_BYTES) / 1024 / NW, NL = NSA + NSB;      // wave-loads of a k-tile
     static constexpr bool TURNS = NW == 8;                          // two waves a SIMD, one of either group (see run)
-    static_assert(NW % 2 == 0 && NSA * NW * 8 == BI && NSB * NW * 8 == BJ, "every wave loads the same number of slabs");
+    static_assert(NW % 2 == 0 && NSA * NW * 1024 == A_BYTES && NL * NW * 1024 == STAGE, "every wave loads the same number of slabs");
+    static_assert(!TRIPLE || (LOADERS && !TURNS && NSA % 3 == 0 && NSB % 3 == 0), "loads of three slabs, by waves of their own");
     typedef f32x16 Acc[FI][FJ];
 
     static constexpr unsigned kOOB = 0x80000000u;       // beyond any buffer of 2^31 - 1 bytes
@@ -77,45 +83,69 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
     }
 
     // KR: the places of a row's 32-byte pairs
-    template <int B> __device__ static __forceinline__ int swap(int k) { return B * PL >= 128 ? (k & 3) << 1 : B * PL == 64 ? ((k >> 1) & 1) << 1 : 0; }
+    template <int B> __device__ static __forceinline__ int swap(int k) {
+        static_assert(!TRIPLE || B == 64 || B == 128, "rows of 384 or 768 bytes");
+        constexpr int W = TRIPLE ? B : B * PL;
+        return W >= 128 ? (k & 3) << 1 : W == 64 ? ((k >> 1) & 1) << 1 : 0;
+    }
 
     // One operand's loads: lane's offset in a slab, and what it has to compare with at the edges.
     template <bool KR, int B, int NS> struct Loader {
-        static constexpr int RB = B * PL * 2, RPS = KR ? 1024 / RB : 8; // KR: bytes of a row of the stage; rows of a slab
+        static constexpr int RB = KR ? B * PL * 2 : RK;                 // bytes of a row of the stage
+        // a wave's slabs: every NW-th; TRIPLE, where only three of them are whole rows: consecutive ones, PERIOD = 3
+        static constexpr int PERIOD = TRIPLE ? 3 : 1, RPP = PERIOD * 1024 / RB, RSTEP = TRIPLE ? RPP : NW * RPP;
         const char* base; size_t plane; int ldb;        // bytes of a row of the operand
-        unsigned voff; int row, chunk, last;            // row: this lane's in slab 0; last: rows that exist from row 0 of the tile on
-        int step;                                       // bytes between the slabs of a wave
+        unsigned voff[PERIOD]; int row[PERIOD], chunk, last;      // row: this lane's in slab 0; last: rows that exist from row 0 of the tile on
+        int step;                                       // bytes between the slabs (periods) of a wave
 
         __device__ __forceinline__ void init(const GemmOperand& o, int x0, int lane, int wave) {
             ldb = o.ld * 2; plane = o.plane;
-            if constexpr (!KR) {
+            if constexpr (TRIPLE) {
+                constexpr int CPR = RB / 16;
+                chunk = 0;
+                base = KR ? o.base : o.base + (size_t)x0 * ldb;
+                last = KR ? 0 : o.extent - x0;
+#pragma unroll
+                for (int b = 0; b < 3; ++b) {
+                    const int q = b * 64 + lane, pos = q % CPR;
+                    row[b] = wave * (NS / 3) * RPP + q / CPR;
+                    if constexpr (!KR) voff[b] = (unsigned)(row[b] * ldb + (pos ^ ((row[b] >> 2) & 3)) * 16);
+                    else {
+                        const int col = x0 * 3 + (((pos >> 1) ^ swap<B>(row[b])) << 4) + (pos & 1) * 8;
+                        voff[b] = col < o.extent ? (unsigned)(row[b] * ldb + col * 2) : kOOB;
+                    }
+                }
+            } else if constexpr (!KR) {
                 const int pos = lane & 7;
                 chunk = pos ^ (4 * (wave & 1) + (lane >> 4));
-                row = wave * 8 + (lane >> 3);
+                row[0] = wave * 8 + (lane >> 3);
                 base = o.base + (size_t)x0 * ldb;
                 last = o.extent - x0;
-                voff = (unsigned)(row * ldb + chunk * 16);
+                voff[0] = (unsigned)(row[0] * ldb + chunk * 16);
             } else {
                 constexpr int CPR = RB / 16;
                 const int sub = lane / CPR, pos = lane % CPR;
-                row = wave * RPS + sub;
-                const int f = swap<B>(row);
+                row[0] = wave * RPP + sub;
+                const int f = swap<B>(row[0]);
                 const int col = x0 * PL + (((pos >> 1) ^ f) << 4) + (pos & 1) * 8;
                 base = o.base; chunk = 0; last = 0;
-                voff = col < o.extent ? (unsigned)(row * ldb + col * 2) : kOOB;
+                voff[0] = col < o.extent ? (unsigned)(row[0] * ldb + col * 2) : kOOB;
             }
-            step = NW * RPS * ldb;
+            step = RSTEP * ldb;
         }
         // load i of the k-tile that starts at k (krem: k that are left), of the plane at `p`
         __device__ __forceinline__ unsigned offset(int i, int krem, unsigned long long mask) const {
-            if constexpr (!KR) return row + i * (NW * RPS) < last && (DUAL ? 0 : chunk * 8) < krem ? voff : kOOB;
+            const int b = i % PERIOD, r = row[b] + i / PERIOD * RSTEP;
+            if constexpr (!KR) return r < last && (PL > 1 ? 0 : chunk * 8) < krem ? voff[b] : kOOB;
             else {
-                const int k = row + i * (NW * RPS);
-                bool ok = k < krem;
-                if constexpr (MASKED) ok = ok && ((mask >> k) & 1ull);
-                return ok ? voff : kOOB;
+                bool ok = r < krem;
+                if constexpr (MASKED) ok = ok && ((mask >> r) & 1ull);
+                return ok ? voff[b] : kOOB;
             }
         }
+        __device__ __forceinline__ int behind(int i) const { return i / PERIOD * step; }
+        // where slab i of wave `wave` goes
+        __device__ static __forceinline__ int place(int wave, int i) { return (TRIPLE ? wave * NS + i : i * NW + wave) * 1024; }
         __device__ __forceinline__ const char* at(int p, int k) const {
             return base + (size_t)p * plane + (KR ? (size_t)k * ldb : (size_t)k * 2 * PL);
         }
@@ -126,30 +156,35 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
     // where its value becomes usable; no fragment is under way where control flow joins.
     template <bool KR, int B, int F> struct Reader {
         static constexpr int RB = B * PL * 2;
-        unsigned addr[KR ? F : KS];
-        u32x4 whole[2 * PL][KR ? 1 : F];               // DUAL: [k-step][plane]
+        unsigned addr[KR ? (TRIPLE ? 3 * F : F) : TRIPLE ? 2 : 4];
+        u32x4 whole[2 * PL][KR ? 1 : F];               // several planes: [k-step][plane]
         u32x2 half[2 * PL][KR ? F : 1][2];
 
         __device__ __forceinline__ void init(int w, int lane, unsigned lds0) {
             if constexpr (!KR) {
-                const int r = lane & 31, sw = (r >> 1) & 7;
+                const int r = lane & 31, sw = TRIPLE ? (r >> 2) & 3 : (r >> 1) & 7;
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) addr[ks] = lds0 + (w * F * 32 + r) * (BK * 2) + (((2 * ks + (lane >> 5)) ^ sw) << 4);
+                for (int ks = 0; ks < (TRIPLE ? 2 : 4); ++ks) addr[ks] = lds0 + (w * F * 32 + r) * RK + (((2 * ks + (lane >> 5)) ^ sw) << 4);
             } else {
                 const int lq = lane & 15, k = 8 * (lane >> 5) + (lq >> 2);
                 const int f = swap<B>(k);
 #pragma unroll
-                for (int m = 0; m < F; ++m) addr[m] = lds0 + k * RB + (((2 * PL * (w * F + m) + ((lane >> 4) & 1)) ^ f) << 5) + 8 * (lq & 3);
+                for (int m = 0; m < F; ++m)
+#pragma unroll
+                    for (int p = 0; p < (TRIPLE ? 3 : 1); ++p)
+                        addr[TRIPLE ? 3 * m + p : m] = lds0 + k * RB + (((2 * PL * (w * F + m) + 2 * p + ((lane >> 4) & 1)) ^ f) << 5) + 8 * (lq & 3);
             }
         }
-        // the fragments of k-step S of the stage that starts at byte `st` (DUAL: S = 2 * plane + k-step of the k-tile's two)
+        // the fragments of k-step S of the stage that starts at byte `st` (several planes: S = 2 * plane + k-step of the k-tile's two)
         template <int S, int M = 0> __device__ __forceinline__ void read(unsigned st) {
-            constexpr int slot = DUAL ? 2 * (S & 1) + (S >> 1) : S & 1;      // [k-step][plane], or two k-steps
+            constexpr int slot = PL > 1 ? PL * (S & 1) + (S >> 1) : S & 1;   // [k-step][plane], or two k-steps
             if constexpr (M < F) {
-                if constexpr (!KR) asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(whole[slot][M]) : "v"(addr[S] + st), "i"(M * 32 * BK * 2));
+                if constexpr (!KR)
+                    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(whole[slot][M]) : "v"(addr[TRIPLE ? S & 1 : S] + st), "i"(M * 32 * RK + (TRIPLE ? S / 2 * 64 : 0)));
                 else {
-                    constexpr int off = (DUAL ? S & 1 : S) * 16 * RB;
-                    const unsigned a = (DUAL && S >= 2 ? addr[M] ^ 64u : addr[M]) + st;      // the second plane: two pairs on
+                    constexpr int off = (PL > 1 ? S & 1 : S) * 16 * RB;
+                    // DUAL: the second plane two pairs on
+                    const unsigned a = (TRIPLE ? addr[3 * M + S / 2] : DUAL && S >= 2 ? addr[M] ^ 64u : addr[M]) + st;
                     asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(half[slot][M][0]) : "v"(a), "i"(off));
                     asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(half[slot][M][1]) : "v"(a), "i"(off + 4 * RB));
                 }
@@ -202,8 +237,8 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
             t_krem = issued < total ? ke - k : 0;
             pa = la.at((pairs.a >> (4 * seg)) & 15, k);
             pb = lb.at((pairs.b >> (4 * seg)) & 15, k);
-            if constexpr (MASKED) t_mask = TURNS ? ahead : mask[min(k, ke - 1) >> 6];
-            t_dst = smem + st * STAGE + wave * 1024;
+            if constexpr (MASKED) t_mask = TURNS ? ahead : mask[min(k, ke - 1) >> 6] >> (k & 63);
+            t_dst = smem + st * STAGE;
             ++issued;
             if (++kt == nkt) { kt = 0; if (seg + 1 < pairs.n) ++seg; }
         };
@@ -212,10 +247,10 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         };
         auto issue_one = [&](int i) __attribute__((always_inline)) {
             if (i < NSA)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(pa), (gemm_lds_t)(t_dst + i * (NW * 1024)), 16, (int)la.offset(i, t_krem, t_mask), i * la.step, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(pa), (gemm_lds_t)(t_dst + la.place(wave, i)), 16, (int)la.offset(i, t_krem, t_mask), la.behind(i), 0, 0);
             else if (i < NL)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(pb), (gemm_lds_t)(t_dst + A_BYTES + (i - NSA) * (NW * 1024)), 16,
-                                                         (int)lb.offset(i - NSA, t_krem, ~0ull), (i - NSA) * lb.step, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(pb), (gemm_lds_t)(t_dst + A_BYTES + lb.place(wave, i - NSA)), 16,
+                                                         (int)lb.offset(i - NSA, t_krem, ~0ull), lb.behind(i - NSA), 0, 0);
         };
         auto arrived = [&](int slot) __attribute__((always_inline)) {
             __builtin_amdgcn_s_waitcnt(0xc07f);                // lgkmcnt(0)
@@ -225,19 +260,23 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 rb.arrived(PL * slot + p);
             }
         };
-        constexpr int NM = FI * FJ, NP = DUAL ? 3 * NM : NM;   // products of a phase (a k-step) = places for loads
+        constexpr int NM = FI * FJ, NP = TRIPLE ? 6 * NM : DUAL ? 3 * NM : NM;   // products of a phase (a k-step) = places for loads
         // The loads of a k-tile are issued between the products behind the barrier that frees its stage.  Two stages: as early as
         // they go, one or more a place, as they have to land within the k-tile; more stages: evenly over a whole k-tile.
-        constexpr int PHASES = DUAL ? 2 : KS, PLACES = STAGES == 2 ? (NL < 2 * NP ? NL : 2 * NP) : PHASES * NP;
-        // DUAL: the small terms first
-        auto products = [&](int slot, int first, bool issue) __attribute__((always_inline)) {
+        constexpr int PHASES = KS, PLACES = STAGES == 2 ? (NL < 2 * NP ? NL : 2 * NP) : PHASES * NP;
+        // Several planes: the small terms first.  `ahead_of(p)` comes in front of every pair of planes.
+        auto products = [&](int slot, int first, bool issue, auto ahead_of) __attribute__((always_inline)) {
 #pragma unroll
-            for (int p = 0; p < NP / NM; ++p)
+            for (int p = 0; p < NP / NM; ++p) {
+                constexpr int pair_a[6] = {2, 0, 1, 1, 0, 0}, pair_b[6] = {0, 2, 1, 0, 1, 0};
+                ahead_of(p);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < FI; ++i)
 #pragma unroll
                     for (int j = 0; j < FJ; ++j) {
-                        if constexpr (DUAL) Mma<E, 32>::run(ra.get(2 * slot + (p == 0), i), rb.get(2 * slot + (p == 1), j), acc[i][j]);
+                        if constexpr (TRIPLE) Mma<E, 32>::run(ra.get(3 * slot + pair_a[p], i), rb.get(3 * slot + pair_b[p], j), acc[i][j]);
+                        else if constexpr (DUAL) Mma<E, 32>::run(ra.get(2 * slot + (p == 0), i), rb.get(2 * slot + (p == 1), j), acc[i][j]);
                         else Mma<E, 32>::run(ra.get(slot, i), rb.get(slot, j), acc[i][j]);
                         if (issue) {
 #pragma unroll
@@ -246,6 +285,7 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
+            }
         };
         if (!LOADERS || loader) {
 #pragma unroll
@@ -342,30 +382,33 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 if (++sn == STAGES) sn = 0;
             }
         } else {
-            auto read = [&](auto k, unsigned stage) __attribute__((always_inline)) {
+            // all fragments of a k-step at once, or (TRIPLE: more than can be under way) a plane of them ahead of a pair's products
+            auto read_plane = [&](auto k, unsigned stage, int p) __attribute__((always_inline)) {
                 constexpr int S = decltype(k)::value;
-                ra.template read<S>(stage); rb.template read<S>(stage);
-                if constexpr (DUAL) { ra.template read<S + 2>(stage); rb.template read<S + 2>(stage); }
+                if (p == 0) { ra.template read<S>(stage); rb.template read<S>(stage); }
+                if constexpr (PL > 1) if (p == 1) { ra.template read<S + 2>(stage); rb.template read<S + 2>(stage); }
+                if constexpr (TRIPLE) if (p == 2) { ra.template read<S + 4>(stage); rb.template read<S + 4>(stage); }
             };
-            read(k0, 0);
+            auto step = [&](auto k, unsigned stage, int slot, int first, bool issue) __attribute__((always_inline)) {
+                if constexpr (!TRIPLE) {
+#pragma unroll
+                    for (int p = 0; p < PL; ++p) read_plane(k, stage, p);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                products(slot, first, issue, [&](int p) __attribute__((always_inline)) { if constexpr (TRIPLE) if (p < 3) read_plane(k, stage, p); });
+                arrived(slot ^ 1);
+            };
+#pragma unroll
+            for (int p = 0; p < PL; ++p) read_plane(k0, 0, p);
             arrived(0);
             unsigned st = 0;
             int sn = 0;
             for (int t = 0; t < total; ++t) {
-                read(k1, st);
-                __builtin_amdgcn_sched_barrier(0);
                 // (in the first iteration all of the stages' loads are under way)
-                products(0, NP, !LOADERS && t > 0);
-                arrived(1);
-                if constexpr (!DUAL) {
-                    read(k2, st);
-                    __builtin_amdgcn_sched_barrier(0);
-                    products(1, 2 * NP, !LOADERS && t > 0);
-                    arrived(0);
-                    read(k3, st);
-                    __builtin_amdgcn_sched_barrier(0);
-                    products(0, 3 * NP, !LOADERS && t > 0);
-                    arrived(1);
+                step(k1, st, 0, NP, !LOADERS && t > 0);
+                if constexpr (PL == 1) {
+                    step(k2, st, 1, 2 * NP, !LOADERS && t > 0);
+                    step(k3, st, 0, 3 * NP, !LOADERS && t > 0);
                 }                                              // this wave has read all of its stage
                 if constexpr (!LOADERS) wait_vmcnt<(STAGES - 2) * NL>();      // k-tile t + 1 landed (this wave's share)
                 asm volatile("" ::: "memory");
@@ -374,11 +417,8 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 const int freed = sn;
                 if (++sn == STAGES) sn = 0;
                 st = (unsigned)(sn * STAGE);
-                read(k0, st);                                      // (behind the last k-tile: zeros, not used)
                 if constexpr (!LOADERS) tile_begin(freed);
-                __builtin_amdgcn_sched_barrier(0);
-                products(1, 0, !LOADERS);
-                arrived(0);
+                step(k0, st, 1, 0, !LOADERS);                  // (behind the last k-tile it reads zeros, not used)
             }
 #pragma unroll
             for (int q = 0; q < NL; ++q)                       // what would have been issued in the next iteration: zeros
