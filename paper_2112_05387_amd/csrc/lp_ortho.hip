@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256) void ns_split_kernel(const NsArgs a) {
 enum NsMode { NS_GRAM, NS_POLY, NS_STEP, NS_LAST };
 
 // A 32 x 32 piece of O, i from i0 along the longer side: what it is the step of is requested before its values lie in LDS.
-struct NsOld { f32x4 w[4]; u32x2 low[4]; };
+struct NsOld { f32x4 w[4]; };         // (bf16: two words of each)
 __device__ __forceinline__ void ns_request(const NsProb& P, NsOld& old, int row0, int col0, int lane) {
     if (P.src || !(P.flags & NS_VEC_OUT)) return;
     const int col = min(col0 + 4 * (lane & 7), P.cols - 4);       // (rows and columns beyond the last: read, not used)
@@ -165,7 +165,10 @@ __device__ __forceinline__ void ns_request(const NsProb& P, NsOld& old, int row0
     for (int k = 0; k < 4; ++k) {
         const size_t e = (size_t)min(row0 + (lane >> 3) + 8 * k, P.rows - 1) * P.ld_out + col;
         if (P.master) old.w[k] = *reinterpret_cast<const f32x4*>(P.master + e);
-        else if (P.flags & NS_OUT_LOW) old.low[k] = *reinterpret_cast<const u32x2*>(reinterpret_cast<const unsigned short*>(P.out) + e);
+        else if (P.flags & NS_OUT_LOW) {
+            const u32x2 b = *reinterpret_cast<const u32x2*>(reinterpret_cast<const unsigned short*>(P.out) + e);
+            old.w[k][0] = __uint_as_float(b[0]); old.w[k][1] = __uint_as_float(b[1]);
+        }
         else old.w[k] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(P.out) + e);
     }
 }
@@ -184,8 +187,10 @@ __device__ __forceinline__ void ns_answer(const NsProb& P, const NsOld& old, con
             for (int e = 0; e < 4; ++e) o[e] = E[m * step + (4 * (lane & 7) + e) * next];
             if (!P.src) {
                 f32x4 w = old.w[k];
-                if (!P.master && out_low) w = f32x4{__uint_as_float(old.low[k][0] << 16), __uint_as_float(old.low[k][0] & 0xffff0000u),
-                                                      __uint_as_float(old.low[k][1] << 16), __uint_as_float(old.low[k][1] & 0xffff0000u)};
+                if (!P.master && out_low) {
+                    const unsigned b0 = __float_as_uint(w[0]), b1 = __float_as_uint(w[1]);
+                    w = f32x4{__uint_as_float(b0 << 16), __uint_as_float(b0 & 0xffff0000u), __uint_as_float(b1 << 16), __uint_as_float(b1 & 0xffff0000u)};
+                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(-P.lr, o[e], w[e] * P.shrink);
             }
@@ -280,22 +285,26 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
             const int ip = ib + (n % FI) * 32, jp = jb + (n / FI) * 32;
             row0 = tall ? ip : jp; col0 = tall ? jp : ip;
         };
-        NsOld old[2];
+        constexpr int DEEP = FI * FJ > 8 ? 3 : 4;
+        NsOld old[DEEP];
         int row0, col0;
-        place(0, row0, col0);
-        ns_request(P, old[0], row0, col0, lane);
+#pragma unroll
+        for (int n = 0; n < DEEP - 1 && n < FI * FJ; ++n) {
+            place(n, row0, col0);
+            ns_request(P, old[n], row0, col0, lane);
+        }
 #pragma unroll
         for (int n = 0; n < FI * FJ; ++n) {
-            if (n + 1 < FI * FJ) {
-                place(n + 1, row0, col0);
-                ns_request(P, old[(n + 1) & 1], row0, col0, lane);
+            if (n + DEEP - 1 < FI * FJ) {
+                place(n + DEEP - 1, row0, col0);
+                ns_request(P, old[(n + DEEP - 1) % DEEP], row0, col0, lane);
             }
 #pragma unroll
             for (int q = 0; q < 16; ++q) E[lr * 33 + T::row(q, lane)] = acc[n % FI][n / FI][q] * back;
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_s_waitcnt(0xc07f);
             place(n, row0, col0);
-            ns_answer(P, old[n & 1], E, tall, row0, col0, lane);
+            ns_answer(P, old[n % DEEP], E, tall, row0, col0, lane);
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
             __builtin_amdgcn_s_waitcnt(0xc07f);
         }
