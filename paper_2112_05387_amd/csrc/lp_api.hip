@@ -3233,7 +3233,7 @@ struct CePlan {
     TilePlan tl, tx, tw;
     int piece, pieces, ldv, ldp;             // classes of a piece of the probabilities; of a row of them, and its elements
     int width;                               // channels of a row of a laid-out operand
-    size_t o_x, o_w, o_partial, o_slices, o_bsum, o_bcnt, o_mask, o_count, o_prob, o_dx, o_dw, o_colsum, bytes;
+    size_t o_x, o_w, o_partial, o_slices, o_bsum, o_bcnt, o_mask, o_count, o_prob, o_dx, o_dw, o_colsum, o_ticket, bytes;
     int parts, colparts;
     int direct;                              // waves a row of the kernels for small problems, or 0
 };
@@ -3303,6 +3303,7 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
         p.o_partial = p.cut ? 0 : ws.take(N * p.parts * sizeof(float2));
         p.o_bsum = ws.take(N * 4);
         p.o_bcnt = ws.take(N * 4);
+        p.o_ticket = ws.take(4);
     } else {
         p.tx = best_plan(p.C, N1, p.piece, nl, all | few, true);
         p.tw = best_plan(p.C, p.piece, N1, nw, all, true);
@@ -3325,16 +3326,12 @@ static lp_status hip_status(hipError_t err) {
 static lp_status ce_operands(const CePlan& p, int dtype, const void* x, const void* w, char* ws, GemmOperand& X, GemmOperand& W, hipStream_t s) {
     X.extent = p.N; W.extent = p.V;
     X.plane = W.plane = 0;
-    hipError_t err = hipSuccess;
-    if (p.pack_x) {
-        X.base = ws + p.o_x; X.ld = p.nplanes * p.width;
-        err = launch_ce_pack(x, p.ldx, p.N, p.C, dtype, ws + p.o_x, p.width, s);
-    } else { X.base = (const char*)x; X.ld = (int)p.ldx; }
-    if (p.pack_w) {
-        W.base = ws + p.o_w; W.ld = p.nplanes * p.width;
-        if (err == hipSuccess) err = launch_ce_pack(w, p.ldw, p.V, p.C, dtype, ws + p.o_w, p.width, s);
-    } else { W.base = (const char*)w; W.ld = (int)p.ldw; }
-    return hip_status(err);
+    CePack px{x, ws + p.o_x, p.ldx, 0, p.C, p.width, 0}, pw{w, ws + p.o_w, p.ldw, 0, p.C, p.width, 0};
+    if (p.pack_x) { X.base = ws + p.o_x; X.ld = p.nplanes * p.width; px.rows = p.N; }
+    else { X.base = (const char*)x; X.ld = (int)p.ldx; }
+    if (p.pack_w) { W.base = ws + p.o_w; W.ld = p.nplanes * p.width; pw.rows = p.V; }
+    else { W.base = (const char*)w; W.ld = (int)p.ldw; }
+    return hip_status(launch_ce_pack(px, pw, dtype, s));
 }
 
 static lp_status ce_check(const CePlan& p, const void* x, const void* w, const int32_t* labels, const void* ws, size_t ws_bytes) {
@@ -3398,6 +3395,7 @@ lp_status lp_linear_ce_forward(const lp_linear_ce_desc* d, void* stream, const v
     CeLogits a = ce_logits(p, X, W, bias, 0, p.V);
     CeRows r;
     memset(&r, 0, sizeof(r));
+    a.ticket = r.ticket = (int*)(ws + p.o_ticket);
     if (p.cut) {
         a.slices = (float*)(ws + p.o_slices); a.ldv = p.ldv; a.slice = (size_t)p.N * a.ldv;
         r.slices = a.slices; r.slice = a.slice; r.nslices = p.tl.slices; r.ldv = a.ldv;
@@ -3444,6 +3442,7 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
     char* const prob = ws + p.o_prob;
     const size_t pplane = (size_t)p.N * p.ldv * 2;
     GemmOperand P{prob, pplane, p.ldp, 0};
+    const bool straight = p.tx.slices == 1;      // dX comes whole out of its product (of the last piece)
     CeFinish f;
     memset(&f, 0, sizeof(f));
     auto blocks = [](size_t rows, int cols) { return (int)std::min<size_t>((rows * ((cols + 3) / 4) + 255) / 256, 4096); };
@@ -3489,6 +3488,12 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
             g.K = V; g.kchunk = div_up(div_up(V, 64), t.slices) * 64; g.I = p.K; g.J = p.N;
             g.tiles_i = t.ti; g.tiles_j = t.tj; g.band = 8;
             g.out = (float*)(ws + p.o_dx); g.slice = (size_t)p.N * p.K; g.ldo = p.K; g.vec = 1; g.add = piece > 0;
+            if (straight && piece + 1 == p.pieces) {
+                const size_t es = d->dtype == LP_BF16 ? 2 : 4;
+                g.last = dfeatures; g.ldlast = p.lddx; g.C = p.C; g.low = d->dtype == LP_BF16; g.labels = labels; g.V_all = p.V;
+                g.vec_last = p.C % 4 == 0 && p.lddx % 4 == 0 && reinterpret_cast<uintptr_t>(dfeatures) % (4 * es) == 0;
+                g.count = count; g.scale = loss_scale;
+            }
             if ((st = hip_status(launch_ce_dx(g, t.slices, t.cfg, s))) != LP_OK) return st;
         }
         // the sums and the bias of this piece; with the last one those of dX
@@ -3498,7 +3503,7 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
         if (piece + 1 < p.pieces && (st = hip_status(launch_ce_finish(f, d->dtype, s))) != LP_OK) return st;
     }
     f.x = CeSum{(float*)(ws + p.o_dx), (size_t)p.N * p.K, p.tx.slices, p.K, dfeatures, (size_t)p.lddx, p.N, p.C, parts_log(p.tx.slices)};
-    f.blocks_x = dfeatures ? blocks((size_t)p.N << f.x.parts_log, p.C) : 0;
+    f.blocks_x = dfeatures && !straight ? blocks((size_t)p.N << f.x.parts_log, p.C) : 0;
     return hip_status(launch_ce_finish(f, d->dtype, s));
 }
 

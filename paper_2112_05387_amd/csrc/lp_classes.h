@@ -6,6 +6,9 @@
 
 namespace lp {
 
+// rows of `cols` elements, ld apart, to rows of `width`; rows 0: nothing
+struct CePack { const void* src; void* dst; long ld; int rows, cols, width, blocks; };
+
 // l = X W^T over one piece of the classes (rows i: classes v0 .. v0 + V - 1, columns j: samples)
 struct CeLogits {
     GemmOperand w, x;
@@ -15,6 +18,7 @@ struct CeLogits {
     int tiles_i, tiles_j, band;
     const float* bias;                  // of the piece, or null
     unsigned long long* mask; int* count;    // probabilities: which rows count, and how many do, are found beside them
+    int* ticket;                        // statistics, partial logits: set to zero for the kernel behind, or null
     float2* partial; int parts;         // statistics: [N][parts] (maximum, sum), base 2
     float* slices; size_t slice;        // partial logits: [slices][N][ldv]
     int ldv, ldp;                       // classes of a row of slices / prob, a multiple of 8 (three planes: 32); elements of a row of prob
@@ -31,6 +35,7 @@ struct CeRows {
     GemmOperand w, x; int nplanes;
     float *lse, *row_loss, *loss;
     float* bsum; int* bcnt;             // of every workgroup
+    int* ticket;                        // workgroups that are done, zero before; or null: somebody else adds up
     unsigned long long* mask; int* count;
 };
 // out[j][i] (+)= sum_k a[k][i] * b[..]; i channels, j samples or classes
@@ -43,6 +48,8 @@ struct CeGrad {
     int vec, add;                       // 16-byte stores (I a multiple of four then); add to what is there
     const int* count; float scale;      // scaled by scale / count, or not
     const unsigned long long* mask;
+    // the gradient itself instead of a partial result: its rows (with a class, or zero), type, 16-byte (bf16: 8-byte) stores
+    void* last; long ldlast; int C, low, vec_last, V_all; const int* labels;
 };
 struct CeSum { const float* part; size_t slice; int nslices, ldp; void* out; size_t ldo; int rows, cols, parts_log; };
 struct CeFinish {
@@ -73,7 +80,7 @@ hipError_t launch_ce_total(const float* sums, const int* counts, int n, float* l
 // tiles: 0 256 x 256, 1 128 x 128, 2 64 x 64, 3 128 x 32 (few samples); of three planes 4 128 x 128, 5 64 x 64; waves along either side
 void ce_tile_size(int cfg, int* bi, int* bj, int* wi, int* wj);
 double ce_tile_time(int cfg, long blocks, int ktiles);
-hipError_t launch_ce_pack(const void* src, long ld_src, int rows, int cols, int dtype, void* dst, int width, hipStream_t s);
+hipError_t launch_ce_pack(CePack x, CePack w, int dtype, hipStream_t s);
 hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s);
 hipError_t launch_ce_prob_tiles(const CeLogits& a, int cfg, hipStream_t s);
 hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t s);

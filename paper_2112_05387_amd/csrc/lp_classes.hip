@@ -59,20 +59,23 @@ template <int NP> __device__ __forceinline__ size_t plane_at(int c, int k, size_
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Operands in the form the products want: rows of `width` elements a plane (a multiple of 8, of 32 in three planes), zeros behind the last
 // ---------------------------------------------------------------------------------------------------------------------------------
-template <class T, int NP> __global__ __launch_bounds__(256) void ce_pack_kernel(const T* __restrict__ src, long ld_src, int rows, int cols, unsigned short* __restrict__ dst,
-                                                                                 int width) {
-    const int cpr = width >> 3;                                   // chunks of eight elements in a row
-    const size_t n = (size_t)rows * cpr;
-    for (size_t t = (size_t)blockIdx.x * 256 + threadIdx.x; t < n; t += (size_t)gridDim.x * 256) {
+template <class T, int NP> __global__ __launch_bounds__(256) void ce_pack_kernel(const CePack x, const CePack w) {
+    const bool first = (int)blockIdx.x < x.blocks;
+    const CePack& a = first ? x : w;
+    const T* const src = reinterpret_cast<const T*>(a.src);
+    unsigned short* const dst = reinterpret_cast<unsigned short*>(a.dst);
+    const int cpr = a.width >> 3;                                 // chunks of eight elements in a row
+    const size_t n = (size_t)a.rows * cpr;
+    for (size_t t = (size_t)(blockIdx.x - (first ? 0 : x.blocks)) * 256 + threadIdx.x; t < n; t += (size_t)a.blocks * 256) {
         const int r = (int)(t / cpr), c = (int)(t - (size_t)r * cpr) * 8;
-        const T* s = src + (size_t)r * ld_src + c;
+        const T* s = src + (size_t)r * a.ld + c;
         unsigned short out[NP][8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if constexpr (sizeof(T) == 2) out[0][e] = c + e < cols ? reinterpret_cast<const unsigned short*>(s)[e] : 0;
+            if constexpr (sizeof(T) == 2) out[0][e] = c + e < a.cols ? reinterpret_cast<const unsigned short*>(s)[e] : 0;
             else {
                 unsigned b[NP];
-                split_bf16<NP>(c + e < cols ? to_float(s[e]) : 0.f, b);
+                split_bf16<NP>(c + e < a.cols ? to_float(s[e]) : 0.f, b);
 #pragma unroll
                 for (int p = 0; p < NP; ++p) out[p][e] = (unsigned short)b[p];
             }
@@ -82,7 +85,7 @@ template <class T, int NP> __global__ __launch_bounds__(256) void ce_pack_kernel
             u32x4 v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = out[p][2 * e] | ((unsigned)out[p][2 * e + 1] << 16);
-            *reinterpret_cast<u32x4*>(dst + (size_t)r * (NP * width) + plane_at<NP>(c, p, 0)) = v;
+            *reinterpret_cast<u32x4*>(dst + (size_t)r * (NP * a.width) + plane_at<NP>(c, p, 0)) = v;
         }
     }
 }
@@ -128,6 +131,7 @@ template <class T, int MODE, int NP, int WAVES> __global__ __launch_bounds__(T::
         for (int j = 0; j < T::TJ / 32; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    if ((MODE == LM_STATS || MODE == LM_SLICE) && a.ticket && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.ticket = 0;
     const int kb = blockIdx.y * a.kchunk;
     T::run(a.w, a.x, a.pairs, i0, j0, kb, min(a.K, kb + a.kchunk), (GemmMask)nullptr, smem, acc);
 
@@ -308,14 +312,18 @@ __device__ __forceinline__ float2 sliced(const float* p, size_t slice, int n) {
     return l;
 }
 
-// sum of n losses and number of rows, by a workgroup of 256
-__device__ __forceinline__ void ce_total(const float* sums, const int* counts, int n, float* loss) {
+// sum of n losses and number of rows, by a workgroup of 256.  AGENT: of values that other workgroups of the same launch have stored
+template <bool AGENT> __device__ __forceinline__ void ce_total(const float* sums, const int* counts, int n, float* loss) {
     __shared__ double s_t[4];
     __shared__ int s_c[4];
     const int tid = threadIdx.x;
     double t = 0.0;
     int c = 0;
-    for (int b = tid; b < n; b += 256) { t += sums[b]; c += counts[b]; }
+#pragma unroll 4
+    for (int b = tid; b < n; b += 256) {
+        t += AGENT ? __hip_atomic_load(sums + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : sums[b];
+        c += AGENT ? __hip_atomic_load(counts + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : counts[b];
+    }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) { t += __shfl_xor(t, o); c += __shfl_xor(c, o); }
     if ((tid & 63) == 0) { s_t[tid >> 6] = t; s_c[tid >> 6] = c; }
@@ -325,7 +333,7 @@ __device__ __forceinline__ void ce_total(const float* sums, const int* counts, i
         *loss = (float)(((s_t[0] + s_t[1]) + (s_t[2] + s_t[3])) / (double)(all > 1 ? all : 1));
     }
 }
-__global__ __launch_bounds__(256) void ce_total_kernel(const float* sums, const int* counts, int n, float* loss) { ce_total(sums, counts, n, loss); }
+__global__ __launch_bounds__(256) void ce_total_kernel(const float* sums, const int* counts, int n, float* loss) { ce_total<false>(sums, counts, n, loss); }
 
 template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_kernel(const CeRows a) {
     __shared__ float s_m[4], s_s[4], s_own[4], s_loss[4];
@@ -400,14 +408,23 @@ template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_k
     }
     if (lane == 0) { s_loss[wave] = loss; s_cnt[wave] = part == 0 && valid ? 1 : 0; }
     __syncthreads();
+    const float sum = (s_loss[0] + s_loss[1]) + (s_loss[2] + s_loss[3]);
+    const int cnt = s_cnt[0] + s_cnt[1] + s_cnt[2] + s_cnt[3];
+    if (!a.ticket) {
+        if (tid == 0) { a.bsum[blockIdx.x] = sum; a.bcnt[blockIdx.x] = cnt; }
+        return;
+    }
+    // Few workgroups: the one that finishes last adds up.  It is found by a count of those that have stored, whose order is of no account
+    // to the sums.  Stores and loads of these values go past the L2 of their own die, and a store has arrived before it is counted.
+    __shared__ int s_last;
     if (tid == 0) {
-        a.bsum[blockIdx.x] = (s_loss[0] + s_loss[1]) + (s_loss[2] + s_loss[3]);
-        a.bcnt[blockIdx.x] = s_cnt[0] + s_cnt[1] + s_cnt[2] + s_cnt[3];
+        __hip_atomic_store(a.bsum + blockIdx.x, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(a.bcnt + blockIdx.x, cnt, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        s_last = __hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
     }
-    if (gridDim.x == 1) {
-        __syncthreads();
-        ce_total(a.bsum, a.bcnt, 1, a.loss);
-    }
+    __syncthreads();
+    if (s_last) ce_total<true>(a.bsum, a.bcnt, gridDim.x, a.loss);
 }
 
 // Probabilities from partial logits (few tiles): a workgroup a row
@@ -460,6 +477,41 @@ template <class T, int WAVES> __global__ __launch_bounds__(T::NT, WAVES) void ce
     const int lr = lane & 31, h = lane >> 5;
     const float g = a.count ? a.scale / (float)max(*a.count, 1) : 1.f;
     float* const out = a.out + (size_t)blockIdx.y * a.slice;
+    if (a.last) {  // dX itself
+#pragma unroll
+        for (int j = 0; j < T::TJ / 32; ++j) {
+            const int n = j0 + wj * T::TJ + j * 32 + lr;
+            if (n >= a.J) continue;
+            const bool live = is_class(a.labels[n], a.V_all);
+#pragma unroll
+            for (int i = 0; i < T::TI / 32; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = i0 + wi * T::TI + i * 32 + 8 * q + 4 * h;
+                    if (c >= a.C) continue;
+                    f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    if (a.add) v += *reinterpret_cast<const f32x4*>(out + (size_t)n * a.ldo + c);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = live ? v[e] * g : 0.f;
+                    if (a.low) {
+                        unsigned short* const d = reinterpret_cast<unsigned short*>(a.last) + (size_t)n * a.ldlast + c;
+                        if (a.vec_last) *reinterpret_cast<u32x2*>(d) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                        else
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (c + e < a.C) d[e] = float_to_bf16_bits(v[e]);
+                    } else {
+                        float* const d = reinterpret_cast<float*>(a.last) + (size_t)n * a.ldlast + c;
+                        if (a.vec_last) *reinterpret_cast<f32x4*>(d) = v;
+                        else
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (c + e < a.C) d[e] = v[e];
+                    }
+                }
+        }
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < T::TJ / 32; ++j) {
         const int col = j0 + wj * T::TJ + j * 32 + lr;
@@ -617,12 +669,12 @@ void ce_tile_size(int cfg, int* bi, int* bj, int* wi, int* wj) {
     *bi = d[cfg][0]; *bj = d[cfg][1]; *wi = d[cfg][2]; *wj = d[cfg][3];
 }
 
-hipError_t launch_ce_pack(const void* src, long ld_src, int rows, int cols, int dtype, void* dst, int width, hipStream_t s) {
-    const size_t n = (size_t)rows * (width >> 3);
-    if (n == 0) return hipSuccess;
-    const dim3 grid((unsigned)std::min<size_t>((n + 255) / 256, 1u << 16));
-    if (dtype == 1) hipLaunchKernelGGL((ce_pack_kernel<bf16_t, 1>), grid, dim3(256), 0, s, (const bf16_t*)src, ld_src, rows, cols, (unsigned short*)dst, width);
-    else hipLaunchKernelGGL((ce_pack_kernel<float, 3>), grid, dim3(256), 0, s, (const float*)src, ld_src, rows, cols, (unsigned short*)dst, width);
+hipError_t launch_ce_pack(CePack x, CePack w, int dtype, hipStream_t s) {
+    for (CePack* a : {&x, &w}) a->blocks = (int)std::min<size_t>(((size_t)a->rows * (a->width >> 3) + 255) / 256, 1u << 16);
+    const dim3 grid(x.blocks + w.blocks);
+    if (grid.x == 0) return hipSuccess;
+    if (dtype == 1) hipLaunchKernelGGL((ce_pack_kernel<bf16_t, 1>), grid, dim3(256), 0, s, x, w);
+    else hipLaunchKernelGGL((ce_pack_kernel<float, 3>), grid, dim3(256), 0, s, x, w);
     return hipGetLastError();
 }
 hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s) {
@@ -656,10 +708,13 @@ hipError_t launch_ce_rows(const CeRows& a, hipStream_t s) {
     // (a wave a row 15 us for 8192 rows of 256 parts and 11 for 10000 of eight; four waves a row 5 for 777)
     const bool wide = a.slices || a.N < 2048;
     const int blocks = wide ? a.N : (a.N + 3) / 4;
-    if (a.slices) hipLaunchKernelGGL((ce_rows_kernel<true, 4>), dim3(blocks), dim3(256), 0, s, a);
-    else if (wide) hipLaunchKernelGGL((ce_rows_kernel<false, 4>), dim3(blocks), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((ce_rows_kernel<false, 1>), dim3(blocks), dim3(256), 0, s, a);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess || blocks == 1) return e;
+    // counting workgroups costs 12 ns each (64 rows: 6.3 us against 5.6 and 1.7 of a launch for the sum; 777: 13.8 against 5.1 and 4.6)
+    CeRows r = a;
+    if (blocks > 128) r.ticket = nullptr;
+    if (a.slices) hipLaunchKernelGGL((ce_rows_kernel<true, 4>), dim3(blocks), dim3(256), 0, s, r);
+    else if (wide) hipLaunchKernelGGL((ce_rows_kernel<false, 4>), dim3(blocks), dim3(256), 0, s, r);
+    else hipLaunchKernelGGL((ce_rows_kernel<false, 1>), dim3(blocks), dim3(256), 0, s, r);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || r.ticket) return e;
     return launch_ce_total(a.bsum, a.bcnt, blocks, a.loss, s);
 }
 hipError_t launch_ce_total(const float* sums, const int* counts, int n, float* loss, hipStream_t s) {
