@@ -24,8 +24,10 @@
 namespace lp {
 namespace {
 
-__global__ __launch_bounds__(256) void ns_put_kernel(const NsChunk c) {
-    for (int i = threadIdx.x; i < c.words; i += 256) c.dst[i] = c.w[i];
+// (the arguments lie in host memory: one round trip for all of them)
+__global__ __launch_bounds__(1024) void ns_put_kernel(const NsChunk c) {
+    static_assert(sizeof(c.w) / 4 <= 1024, "a word a thread");
+    if ((int)threadIdx.x < c.words) c.dst[threadIdx.x] = c.w[threadIdx.x];
 }
 
 // Elements: momentum of the matrices and their sums of squares
@@ -404,7 +406,7 @@ double ns_tile_time(int cfg, long tiles) {
 }
 
 hipError_t launch_ns_put(const NsChunk& c, hipStream_t s) {
-    hipLaunchKernelGGL(ns_put_kernel, dim3(1), dim3(256), 0, s, c);
+    hipLaunchKernelGGL(ns_put_kernel, dim3(1), dim3(1024), 0, s, c);
     return hipGetLastError();
 }
 hipError_t launch_ns_norm(const NsArgs& a, hipStream_t s) {

@@ -34,6 +34,11 @@ def _on(dev):
     return contextlib.nullcontext() if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
 
 
+def _stream(dev):
+    """The current stream of the device (without the object around it, which takes as long to make as a launch)."""
+    return torch._C._cuda_getCurrentRawStream(dev.index)
+
+
 @functools.lru_cache(maxsize=1024)
 def _ce_workspace(rows, channels, classes, dtype, ld_features, ld_weight, backward):
     return B.lp_linear_ce_workspace_bytes(B.lp_linear_ce_desc(rows, channels, classes, dtype, ld_features, ld_weight, 0), backward)
@@ -85,7 +90,7 @@ def linear_ce_forward(features, weight, labels, bias=None):
         loss, row_loss, lse = out[:1], out[1:1 + d.rows], out[1 + d.rows:]
         size = _ce_workspace(d.rows, d.channels, d.classes, d.dtype, d.ld_features, d.ld_weight, False)
         ws = torch.empty(size, dtype=torch.uint8, device=dev)
-        B.lp_linear_ce_forward(d, torch.cuda.current_stream().cuda_stream, features.data_ptr(), weight.data_ptr(), _ptr(bias), labels.data_ptr(),
+        B.lp_linear_ce_forward(d, _stream(dev), features.data_ptr(), weight.data_ptr(), _ptr(bias), labels.data_ptr(),
                                loss.data_ptr(), row_loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), size)
     return loss, row_loss, lse
 
@@ -104,7 +109,7 @@ def linear_ce_backward(features, weight, labels, lse, bias=None, scale=1.0):
         db = None if bias is None else torch.empty(d.classes, dtype=torch.float32, device=dev)
         size = _ce_workspace(d.rows, d.channels, d.classes, d.dtype, d.ld_features, d.ld_weight, True)
         ws = torch.empty(size, dtype=torch.uint8, device=dev)
-        B.lp_linear_ce_backward(d, torch.cuda.current_stream().cuda_stream, features.data_ptr(), weight.data_ptr(), _ptr(bias), labels.data_ptr(),
+        B.lp_linear_ce_backward(d, _stream(dev), features.data_ptr(), weight.data_ptr(), _ptr(bias), labels.data_ptr(),
                                 lse.data_ptr(), scale, dx.data_ptr(), dw.data_ptr(), _ptr(db), ws.data_ptr(), size)
     return dx, dw, db
 
@@ -131,7 +136,7 @@ def orthogonalize(matrices, steps=5, out_dtype=None):
     with _on(dev):
         size = B.lp_orthogonalize_workspace_bytes(mats)
         ws = torch.empty(size, dtype=torch.uint8, device=dev)
-        B.lp_orthogonalize(torch.cuda.current_stream().cuda_stream, mats, steps, ws.data_ptr(), size)
+        B.lp_orthogonalize(_stream(dev), mats, steps, ws.data_ptr(), size)
     return outs
 
 
@@ -167,5 +172,5 @@ def muon_update(table, params, grads, velocity, master=None, *, lr, momentum=0.9
     opts = B.lp_muon_opts(lr, momentum, weight_decay, lr if rest_lr is None else rest_lr, int(nesterov), steps)
     with _on(dev):
         ws = torch.empty(size, dtype=torch.uint8, device=dev)
-        B.lp_muon_step(torch.cuda.current_stream().cuda_stream, arr, params.data_ptr(), grads.data_ptr(), velocity.data_ptr(), _ptr(master),
+        B.lp_muon_step(_stream(dev), arr, params.data_ptr(), grads.data_ptr(), velocity.data_ptr(), _ptr(master),
                        opts, ws.data_ptr(), size)
