@@ -3512,8 +3512,13 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
 // ----------------------------------------------------------------------------------------------------
 namespace {
 
+struct OrthoSet { const void* base[4]; };        // params, grads, velocity, master
+struct OrthoAt { int set; uint64_t param, grad; };
 struct OrthoPlan {
     std::vector<NsProb> p;
+    std::vector<OrthoSet> sets;              // of an update: the buffers, and where in them a tensor is
+    std::vector<OrthoAt> at;
+    float lr = 0.f, shrink = 1.f;
     std::vector<int> start[kNsLaunches];     // blocks of the launches: small, elements, pieces, tiles of r x r, of r x c
     int cfg_sq = NT_64, cfg_step = NT_64;
     size_t o_table = 0, o_norm = 0, lds = 0, bytes = 256;
@@ -3584,17 +3589,44 @@ static lp_status ortho_run(OrthoPlan& o, char* ws, size_t ws_bytes, float moment
     if (n == 0) return LP_OK;
     for (NsProb& q : o.p) q.work = ws + (size_t)q.work;
     // the table goes to the device in the arguments of small launches: legal under capture, no host memory to keep
-    std::vector<unsigned> words(o.table_words(), 0u);
-    for (int k = 0; k < kNsLaunches; ++k) memcpy(words.data() + k * (n + 1), o.start[k].data(), (size_t)(n + 1) * 4);
-    memcpy(words.data() + o.probs_word(), o.p.data(), (size_t)n * sizeof(NsProb));
     hipError_t err = hipSuccess;
-    constexpr int room = (int)(sizeof(NsChunk::w) / 4);
-    for (size_t at = 0; at < words.size() && err == hipSuccess; at += room) {
-        NsChunk c;
-        c.dst = (unsigned*)(ws + o.o_table) + at;
-        c.words = (int)std::min<size_t>(room, words.size() - at);
-        memcpy(c.w, words.data() + at, (size_t)c.words * 4);
-        err = launch_ns_put(c, s);
+    if (o.sets.empty()) {
+        std::vector<unsigned> words(o.table_words(), 0u);
+        for (int k = 0; k < kNsLaunches; ++k) memcpy(words.data() + k * (n + 1), o.start[k].data(), (size_t)(n + 1) * 4);
+        memcpy(words.data() + o.probs_word(), o.p.data(), (size_t)n * sizeof(NsProb));
+        constexpr int room = (int)(sizeof(NsChunk::w) / 4);
+        for (size_t at = 0; at < words.size() && err == hipSuccess; at += room) {
+            NsChunk c;
+            c.dst = (unsigned*)(ws + o.o_table) + at;
+            c.words = (int)std::min<size_t>(room, words.size() - at);
+            memcpy(c.w, words.data() + at, (size_t)c.words * 4);
+            err = launch_ns_put(c, s);
+        }
+    } else {
+        static_assert(32 * kNsSetWords + kNsRecordFull <= (int)(sizeof(NsPack::w) / 4), "the buffers of as many modules as a mask has bits");
+        NsPack c;
+        c.table = (int*)(ws + o.o_table); c.probs = (NsProb*)((unsigned*)(ws + o.o_table) + o.probs_word()); c.work = ws;
+        c.n = n; c.sets = (int)o.sets.size(); c.full = o.start[1][n] != 0; c.lr = o.lr; c.shrink = o.shrink;
+        for (int k = 0; k < kNsLaunches; ++k) c.total[k] = o.start[k][n];
+        for (int k = 0; k < c.sets; ++k)
+            for (int b = 0; b < 4; ++b) { const uint64_t v = (uint64_t)(uintptr_t)o.sets[k].base[b]; memcpy(c.w + k * kNsSetWords + 2 * b, &v, 8); }
+        const int rec = c.full ? kNsRecordFull : kNsRecord, room = ((int)(sizeof(NsPack::w) / 4) - c.sets * kNsSetWords) / rec;
+        for (c.first = 0; c.first < n && err == hipSuccess; c.first += room) {
+            c.count = std::min(room, n - c.first);
+            for (int i = 0; i < c.count; ++i) {
+                const int t = c.first + i;
+                unsigned* const r = c.w + c.sets * kNsSetWords + i * rec;
+                const NsProb& q = o.p[t];
+                r[0] = (unsigned)q.rows; r[1] = (unsigned)q.cols; r[2] = (unsigned)q.flags | (unsigned)o.at[t].set << 8;
+                memcpy(r + 3, &o.at[t].param, 8); memcpy(r + 5, &o.at[t].grad, 8);
+                r[7] = (unsigned)o.start[0][t];
+                if (!c.full) continue;
+                const uint64_t work = (uint64_t)(q.work - ws);
+                memcpy(r + 8, &work, 8);
+                for (int k = 1; k < kNsLaunches; ++k) r[9 + k] = (unsigned)o.start[k][t];
+            }
+            err = launch_ns_pack(c, s);
+        }
     }
     NsArgs a;
     memset(&a, 0, sizeof(a));
@@ -3643,7 +3675,7 @@ static lp_status ortho_matrices(int n, const lp_matrix* mats, OrthoPlan& o) {
 }
 
 // one parameter tensor of an update
-static lp_status muon_tensor(int rows, int cols, int dtype, int orthogonal, void* param, const float* grad, float* vel, float* master, const lp_muon_opts* opts, OrthoPlan& o) {
+static lp_status muon_tensor(int rows, int cols, int dtype, int orthogonal, int set, uint64_t param_at, uint64_t grad_at, OrthoPlan& o) {
     if (rows < 1 || cols < 1) return fail(LP_ERR_INVALID_ARG, "a tensor of %d x %d", rows, cols);
     if (dtype != LP_F32 && dtype != LP_BF16) return fail(LP_ERR_DTYPE, "dtype %d is neither LP_F32 nor LP_BF16", dtype);
     if (orthogonal) {
@@ -3653,14 +3685,11 @@ static lp_status muon_tensor(int rows, int cols, int dtype, int orthogonal, void
     NsProb q;
     memset(&q, 0, sizeof(q));
     q.rows = rows; q.cols = cols; q.ld_out = cols;
-    q.out = param; q.grad = grad; q.vel = vel; q.master = master;
-    q.flags = (dtype == LP_BF16 ? NS_OUT_LOW : 0) | (orthogonal ? 0 : NS_PLAIN) | (!misaligned(grad) && !misaligned(vel) ? NS_VEC : 0) |
-              (cols % 4 == 0 && !misaligned(param) && !misaligned(master) ? NS_VEC_OUT : 0);
-    if (opts) {
-        q.lr = (float)(opts->lr * std::sqrt(std::max(1.0, (double)rows / cols)));
-        q.shrink = (float)(1.0 - (double)opts->lr * opts->weight_decay);
-    }
+    // (the buffers are aligned to 16 bytes)
+    q.flags = (dtype == LP_BF16 ? NS_OUT_LOW : 0) | (orthogonal ? 0 : NS_PLAIN) | (grad_at % 16 == 0 ? NS_VEC : 0) |
+              (cols % 4 == 0 && param_at % 16 == 0 && grad_at % 16 == 0 ? NS_VEC_OUT : 0);
     o.p.push_back(q);
+    o.at.push_back(OrthoAt{set, param_at, grad_at});
     return LP_OK;
 }
 
@@ -3670,12 +3699,19 @@ static lp_status muon_opts(const lp_muon_opts* opts) {
     return LP_OK;
 }
 
+static void muon_rates(const lp_muon_opts* opts, OrthoPlan& o) {
+    if (!opts) return;
+    o.lr = opts->lr;
+    o.shrink = (float)(1.0 - (double)opts->lr * opts->weight_decay);
+}
+
 static lp_status muon_tensors(int n, const lp_muon_tensor* t, void* params, const float* grads, float* velocity, float* master, const lp_muon_opts* opts, OrthoPlan& o) {
     if (n < 0 || n > LP_ORTHO_MAX_MATRICES || (n > 0 && !t)) return fail(LP_ERR_INVALID_ARG, "%d tensors, or their list is NULL", n);
+    muon_rates(opts, o);
+    o.sets.push_back(OrthoSet{{params, grads, velocity, master}});
     for (int i = 0; i < n; ++i) {
         if (t[i].offset % (t[i].dtype == LP_BF16 ? 2 : 4) || t[i].grad_offset % 4) return fail(LP_ERR_INVALID_ARG, "tensor %d: misaligned offset", i);
-        auto f = [&](const void* p) { return p ? (float*)((char*)p + t[i].grad_offset) : nullptr; };
-        const lp_status st = muon_tensor(t[i].rows, t[i].cols, t[i].dtype, t[i].orthogonal, params ? (char*)params + t[i].offset : nullptr, f(grads), f(velocity), f(master), opts, o);
+        const lp_status st = muon_tensor(t[i].rows, t[i].cols, t[i].dtype, t[i].orthogonal, 0, t[i].offset, t[i].grad_offset, o);
         if (st != LP_OK) return st;
     }
     return ortho_plan(o);
@@ -3687,6 +3723,7 @@ static lp_status muon_net(const lp_net* net, int aux, uint32_t mask, int head, v
     if (aux && net->aux.empty()) return fail(LP_ERR_STATE, "the net was created without an AuxNet");
     const int n = aux ? (int)net->aux.size() : net->K;
     if (mask == 0 || (n < 32 && (mask >> n) != 0)) return fail(LP_ERR_INVALID_ARG, "mask 0x%x does not fit %d parameter sets", mask, n);
+    muon_rates(opts, o);
     for (int k = 0; k < n; ++k) {
         if (!((mask >> k) & 1u)) continue;
         const std::vector<lp_tensor_info>* t; size_t pb, gb;
@@ -3700,10 +3737,10 @@ static lp_status muon_net(const lp_net* net, int aux, uint32_t mask, int head, v
             if (!w || !g || !v) return fail(LP_ERR_INVALID_ARG, "params[%d], dparams[%d] or velocity[%d] is NULL", k, k, k);
             if (misaligned(w) || misaligned(g) || misaligned(v) || misaligned(m)) return fail(LP_ERR_INVALID_ARG, "parameter set %d: a buffer is not 16-byte aligned", k);
         }
+        o.sets.push_back(OrthoSet{{w, g, v, m}});
         for (const lp_tensor_info& ti : *t) {
             const int orth = ti.kind == LP_T_CONV || (head && ti.kind == LP_T_FC_W);
-            auto f = [&](const void* p) { return p ? (float*)((char*)p + ti.grad_offset) : nullptr; };
-            st = muon_tensor(ti.dims[0], (int)(ti.numel / ti.dims[0]), ti.dtype, orth, w ? (char*)w + ti.offset : nullptr, f(g), f(v), f(m), opts, o);
+            st = muon_tensor(ti.dims[0], (int)(ti.numel / ti.dims[0]), ti.dtype, orth, (int)o.sets.size() - 1, ti.offset, ti.grad_offset, o);
             if (st != LP_OK) return st;
         }
     }

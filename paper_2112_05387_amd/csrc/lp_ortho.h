@@ -52,6 +52,18 @@ struct NsArgs {
 
 struct NsChunk { unsigned* dst; int words; unsigned w[960]; };
 
+// The same for the tensors of an update, whose pointers are offsets in a few buffers: words of the buffers of every set (params, grads,
+// velocity, master), then records.  A record: rows, cols, flags | set << 8, offset in params (two words), in the others (two), first
+// block of launch 0; and where matrices are worked on in memory (`full`) offset of the work (two), first blocks of launches 1 to 4.
+constexpr int kNsSetWords = 8, kNsRecord = 8, kNsRecordFull = 14;
+struct NsPack {
+    int* table; NsProb* probs; char* work;
+    int n, first, count, sets, full;
+    float lr, shrink;
+    int total[kNsLaunches];
+    unsigned w[960];
+};
+
 constexpr int kNsElems = 4096;          // elements of a block of the launches over elements
 
 // Small matrices: one workgroup each, in LDS from the first step to the last.  Bytes it takes, 0: does not fit.
@@ -68,6 +80,7 @@ enum NsTile { NT_256 = 0, NT_256x320, NT_128, NT_64, NT_COUNT };
 void ns_tile_size(int cfg, int* bi, int* bj);
 double ns_tile_time(int cfg, long tiles);
 hipError_t launch_ns_put(const NsChunk& c, hipStream_t s);
+hipError_t launch_ns_pack(const NsPack& c, hipStream_t s);
 hipError_t launch_ns_small(const NsArgs& a, int steps, size_t lds, hipStream_t s);
 hipError_t launch_ns_norm(const NsArgs& a, hipStream_t s);
 hipError_t launch_ns_split(const NsArgs& a, hipStream_t s);
