@@ -190,14 +190,14 @@ __global__ __launch_bounds__(256) void ns_split_kernel(const NsArgs a) {
 
 enum NsMode { NS_GRAM, NS_POLY, NS_STEP, NS_LAST };
 
-// A 32 x 32 piece of O, i from i0 along the longer side: what it is the step of is requested before its values lie in LDS.
-struct NsOld { f32x4 w[4]; };         // (bf16: two words of each)
-__device__ __forceinline__ void ns_request(const NsProb& P, NsOld& old, int row0, int col0, int lane) {
+// A piece of O, 32 rows of 32 W columns as they are stored: what it is the step of is requested before its values lie in LDS.
+template <int W> struct NsOld { f32x4 w[4 * W]; };         // (bf16: two words of each)
+template <int W> __device__ __forceinline__ void ns_request(const NsProb& P, NsOld<W>& old, int row0, int col0, int lane) {
     if (P.src || !(P.flags & NS_VEC_OUT)) return;
-    const int col = min(col0 + 4 * (lane & 7), P.cols - 4);       // (rows and columns beyond the last: read, not used)
+    const int col = min(col0 + 4 * (lane & (8 * W - 1)), P.cols - 4);       // (rows and columns beyond the last: read, not used)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const size_t e = (size_t)min(row0 + (lane >> 3) + 8 * k, P.rows - 1) * P.ld_out + col;
+    for (int k = 0; k < 4 * W; ++k) {
+        const size_t e = (size_t)min(row0 + lane / (8 * W) + 8 / W * k, P.rows - 1) * P.ld_out + col;
         if (P.master) old.w[k] = *reinterpret_cast<const f32x4*>(P.master + e);
         else if (P.flags & NS_OUT_LOW) {
             const u32x2 b = *reinterpret_cast<const u32x2*>(reinterpret_cast<const unsigned short*>(P.out) + e);
@@ -206,19 +206,18 @@ __device__ __forceinline__ void ns_request(const NsProb& P, NsOld& old, int row0
         else old.w[k] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(P.out) + e);
     }
 }
-// ... E[j][i] in LDS: stored, or taken as the step of the parameters
-__device__ __forceinline__ void ns_answer(const NsProb& P, const NsOld& old, const float* E, bool tall, int row0, int col0, int lane) {
-    const int step = tall ? 1 : 33, next = tall ? 33 : 1;         // from a row of the piece to the next, from a column
+// ... in LDS, element (m, l) at E[m * step + l * next]: stored, or taken as the step of the parameters
+template <int W> __device__ __forceinline__ void ns_answer(const NsProb& P, const NsOld<W>& old, const float* E, int step, int next, int row0, int col0, int lane) {
     const int out_low = P.flags & NS_OUT_LOW;
     if (P.flags & NS_VEC_OUT) {
-        const int col = col0 + 4 * (lane & 7), m0 = lane >> 3;
+        const int l0 = 4 * (lane & (8 * W - 1)), col = col0 + l0;
         if (col >= P.cols) return;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int m = m0 + 8 * k;
+        for (int k = 0; k < 4 * W; ++k) {
+            const int m = lane / (8 * W) + 8 / W * k;
             f32x4 o;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = E[m * step + (4 * (lane & 7) + e) * next];
+            for (int e = 0; e < 4; ++e) o[e] = E[m * step + (l0 + e) * next];
             if (!P.src) {
                 f32x4 w = old.w[k];
                 if (!P.master && out_low) {
@@ -236,10 +235,10 @@ __device__ __forceinline__ void ns_answer(const NsProb& P, const NsOld& old, con
         }
         return;
     }
-    const int l = lane & 31, m0 = lane >> 5, col = col0 + l;
+    const int l = lane & (32 * W - 1), col = col0 + l;
     if (col >= P.cols) return;
 #pragma unroll 4
-    for (int m = m0; m < 32; m += 2) {
+    for (int m = lane / (32 * W); m < 32; m += 2 / W) {
         if (row0 + m >= P.rows) break;
         const float o = E[m * step + l * next];
         const size_t e = (size_t)(row0 + m) * P.ld_out + col;
@@ -311,37 +310,44 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
     constexpr int FI = T::TI / 32, FJ = T::TJ / 32;
 
     if constexpr (MODE == NS_LAST) {
-        // the answer: micro-tiles through LDS, so that both orientations go out along rows
-        float* const E = reinterpret_cast<float*>(smem) + wave * (32 * 33);
-        const bool tall = P.rows > P.cols;
+        // the answer through LDS, so that both orientations go out along rows: two micro-tiles side by side at a time (256 bytes of a row)
+        // where there are two, and what later ones are the step of under way as far as the registers go.  (Last step of the wide network's
+        // update 260 us, of the ImageNet-sized one's 186; 128 bytes of a row and one piece ahead: 296 and 223.  The step alone: 135 and 106.)
         constexpr float back = 1.f / (kScaleB * kScaleX);
-        auto place = [&](int n, int& row0, int& col0) __attribute__((always_inline)) {
-            const int ip = ib + (n % FI) * 32, jp = jb + (n / FI) * 32;
-            row0 = tall ? ip : jp; col0 = tall ? jp : ip;
-        };
-        constexpr int DEEP = FI * FJ > 8 ? 3 : 4;
-        NsOld old[DEEP];
-        int row0, col0;
+        auto all = [&](auto tall_c, auto w_c) __attribute__((always_inline)) {
+            constexpr bool TALL = decltype(tall_c)::value;
+            constexpr int W = decltype(w_c)::value, N = FI * FJ / W, DEEP = FI * FJ > 8 ? (W > 1 ? 1 : 3) : W > 1 ? 2 : 4;
+            constexpr int PITCH = TALL ? 33 : 32 * W + 1;
+            float* const E = reinterpret_cast<float*>(smem) + wave * (32 * 33 * W);
+            // piece n: micro-tiles (i, j) and the next along the rows of what is stored
+            auto at_i = [](int n) { return TALL ? n % FI : n % (FI / W) * W; };
+            auto at_j = [](int n) { return TALL ? n / FI * W : n / (FI / W); };
+            NsOld<W> old[DEEP];
+            auto request = [&](int n) __attribute__((always_inline)) {
+                const int ip = ib + at_i(n) * 32, jp = jb + at_j(n) * 32;
+                ns_request<W>(P, old[n % DEEP], TALL ? ip : jp, TALL ? jp : ip, lane);
+            };
 #pragma unroll
-        for (int n = 0; n < DEEP - 1 && n < FI * FJ; ++n) {
-            place(n, row0, col0);
-            ns_request(P, old[n], row0, col0, lane);
-        }
+            for (int n = 0; n < DEEP - 1 && n < N; ++n) request(n);
 #pragma unroll
-        for (int n = 0; n < FI * FJ; ++n) {
-            if (n + DEEP - 1 < FI * FJ) {
-                place(n + DEEP - 1, row0, col0);
-                ns_request(P, old[(n + DEEP - 1) % DEEP], row0, col0, lane);
+            for (int n = 0; n < N; ++n) {
+                if (n + DEEP - 1 < N) request(n + DEEP - 1);
+#pragma unroll
+                for (int w = 0; w < W; ++w)
+#pragma unroll
+                    for (int q = 0; q < 16; ++q)
+                        E[((TALL ? w * 32 : 0) + lr) * PITCH + (TALL ? 0 : w * 32) + T::row(q, lane)] = acc[at_i(n) + (TALL ? 0 : w)][at_j(n) + (TALL ? w : 0)][q] * back;
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_s_waitcnt(0xc07f);
+                const int ip = ib + at_i(n) * 32, jp = jb + at_j(n) * 32;
+                ns_answer<W>(P, old[n % DEEP], E, TALL ? 1 : PITCH, TALL ? PITCH : 1, TALL ? ip : jp, TALL ? jp : ip, lane);
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                __builtin_amdgcn_s_waitcnt(0xc07f);
             }
-#pragma unroll
-            for (int q = 0; q < 16; ++q) E[lr * 33 + T::row(q, lane)] = acc[n % FI][n / FI][q] * back;
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_s_waitcnt(0xc07f);
-            place(n, row0, col0);
-            ns_answer(P, old[n % DEEP], E, tall, row0, col0, lane);
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            __builtin_amdgcn_s_waitcnt(0xc07f);
-        }
+        };
+        static_assert(T::NW * 2 * 32 * 33 * 4 <= T::LDS, "two micro-tiles of every wave");
+        if (P.rows > P.cols) all(std::true_type(), std::integral_constant<int, FJ % 2 == 0 ? 2 : 1>());
+        else all(std::false_type(), std::integral_constant<int, FI % 2 == 0 ? 2 : 1>());
         return;
     }
     // the two parts of the result, 32 x 32 at a time through LDS, from where they go out as whole cache lines
