@@ -291,8 +291,8 @@ lp_status lp_sgd_update(struct lp_net* net, void* stream, int aux, uint32_t mask
  *     X = U / max(|U|_F, 1e-7);   X <- a X + b (X X^T) X + c (X X^T)^2 X,   (a, b, c) = (3.4445, -4.7750, 2.0315)
  * (X^T X for a tall matrix), which take every singular value s > 0 of U / |U|_F towards one (0.7 .. 1.2 after five steps from s
  * > 0.01 or so) and leave the singular vectors.  Each U [rows, cols] in fp32 or bf16, any row stride; the result in either type;
- * `out` may be `in` (with the same row stride and type).  Sizes may differ from matrix to matrix; rows or cols of 0 are passed
- * over.  Products of operands held in two fp16 parts, sums in fp32, |U| in fp64; bit-identical from call to call. */
+ * `out` may be `in` (with the same row stride and type); otherwise no `out` may overlap another matrix's `in` or `out`.  Sizes may
+ * differ from matrix to matrix; rows or cols of 0 are passed over.  Products of operands held in two fp16 parts, sums in fp32, |U| in fp64; bit-identical from call to call. */
 typedef struct {
     int rows, cols;              /* 0 .. 2^20; the shorter side at most 16384 */
     int dtype_in, dtype_out;     /* lp_dtype */

@@ -102,8 +102,8 @@ SHAPES = [
     (1, 128, 20000), (31, 200, 17001), (300, 333, 3001), (1000, 64, 8200), (1025, 40, 17000), (2500, 96, 8195), (8192, 40, 90),
     # around the limits of what is small: rows, channels, classes, and the work of all
     (1024, 3, 5), (1025, 3, 5), (2, 14980, 3), (2, 15010, 3), (3, 9, 2990), (3, 9, 3010), (256, 9, 880), (512, 64, 512), (512, 64, 520), (7, 300, 800),
-    # columns of few classes over many rows
-    (3399, 171, 22),
+    # columns of few classes over many rows; dX straight from its product, odd and even widths
+    (3399, 171, 22), (3000, 37, 60), (4100, 130, 70), (2600, 333, 300),
 ]
 
 
@@ -138,6 +138,38 @@ def test_row_strides_and_padding(n, c, v, dtype):
         _compare(_run(xs[:, :c], ws[:, :c], b, y), _reference(x, w, b, y), f"row stride {c + pad} {dtype}")
     # other orders are copied
     _compare(_run(x.t().contiguous().t(), w, b, y), _reference(x, w, b, y), "columns first")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,v", [(40, 24, 70), (3000, 36, 60), (3000, 37, 60), (300, 64, 4000), (64, 512, 1000)])
+def test_gradient_rows_in_a_wider_tensor(n, c, v, dtype):
+    """dfeatures with a row stride and off its alignment, through the C ABI: what lies between the rows stays."""
+    import torch
+    from paper_2112_05387_amd import binding as B
+    x, w, b, y = _inputs(n, c, v, dtype, ignored=0.2, seed=5)
+    want = _reference(x, w, b, y, scale=2.0)
+    lse = want["lse"][0].float()
+    for pad, shift in ((8, 0), (3, 1)):
+        wide = torch.full((n * (c + pad) + shift,), 7.0, dtype=x.dtype, device="cuda")
+        dx = wide[shift:].view(n, c + pad)
+        dw = torch.empty(v, c, device="cuda")
+        db = torch.empty(v, device="cuda")
+        d = B.lp_linear_ce_desc(n, c, v, B.LP_BF16 if dtype == "bf16" else B.LP_F32, 0, 0, c + pad)
+        ws = torch.empty(B.lp_linear_ce_workspace_bytes(d, True), dtype=torch.uint8, device="cuda")
+        B.lp_linear_ce_backward(d, torch.cuda.current_stream().cuda_stream, x.data_ptr(), w.data_ptr(), b.data_ptr(), y.data_ptr(), lse.data_ptr(), 2.0,
+                                dx.data_ptr(), dw.data_ptr(), db.data_ptr(), ws.data_ptr(), ws.numel())
+        _compare({"dfeatures": dx[:, :c], "dweight": dw, "dbias": db}, want, f"row stride {c + pad}, shifted by {shift}, {dtype}")
+        assert bool((dx[:, c:] == 7.0).all()) and bool((wide[:shift] == 7.0).all())
+        # some gradients only
+        for which in range(3):
+            ptr = [t.data_ptr() if k == which else None for k, t in enumerate((dx, dw, db))]
+            for t in (wide, dw, db):
+                t.fill_(7.0)
+            B.lp_linear_ce_backward(d, torch.cuda.current_stream().cuda_stream, x.data_ptr(), w.data_ptr(), b.data_ptr(), y.data_ptr(), lse.data_ptr(), 2.0,
+                                    *ptr, ws.data_ptr(), ws.numel())
+            name, t = (("dfeatures", dx[:, :c]), ("dweight", dw), ("dbias", db))[which]
+            _compare({name: t}, want, f"{name} alone")
+            assert all(bool((o == 7.0).all()) for k, o in enumerate((wide, dw, db)) if k != which)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -242,6 +242,69 @@ def test_update_of_a_packed_set(low, master, nesterov):
         assert torch.equal(s["grads"], before["grads"])
 
 
+def test_update_of_many_tensors():
+    """Small matrices, large ones and vectors in turn, more than go to the device at once: each as alone."""
+    import torch
+    from paper_2112_05387_amd import ops
+    shapes = [(70 + i, 65 + 3 * i) if i % 5 == 0 else (8 + i, 9) if i % 5 < 3 else (3 + i,) for i in range(160)]
+    table, off, goff = [], 0, 0
+    for i, shape in enumerate(shapes):
+        dt = "bf16" if i % 2 else "f32"
+        table.append((shape, dt, len(shape) > 1, off, goff))
+        off += -(-math.prod(shape) * 4 // 256) * 256 + (4 if i % 7 == 0 else 0)       # some of them unaligned
+        goff += math.prod(shape) * 4
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    grads, vel = (torch.randn(goff // 4, generator=g, device="cuda") for _ in range(2))
+    params = torch.zeros(off, dtype=torch.uint8, device="cuda")
+    for shape, dt, orth, o, go in table:
+        _view(params, dt, o, math.prod(shape)).copy_(torch.randn(math.prod(shape), generator=g, device="cuda"))
+    one_p, one_v = params.clone(), vel.clone()
+    ops.muon_update(tuple(table), params, grads, vel, lr=0.1, momentum=0.9, weight_decay=0.1, rest_lr=0.05)
+    for t in table:
+        ops.muon_update((t,), one_p, grads, one_v, lr=0.1, momentum=0.9, weight_decay=0.1, rest_lr=0.05)
+    assert torch.equal(vel, one_v)
+    for shape, dt, orth, o, go in table:
+        n = math.prod(shape)
+        a, b = (_view(p, dt, o, n).double() for p in (params, one_p))
+        # (other tiles may add up in another order: each within its own tolerance of the definition)
+        tol = 0.0
+        if orth:
+            u = (grads[go // 4:go // 4 + n] + 0.9 * vel[go // 4:go // 4 + n]).view(shape)
+            tol = 2 * (0.1 * math.sqrt(max(1.0, shape[0] / shape[1])) * _tolerance(u) + (2.0 ** -8 if dt == "bf16" else 2.0 ** -22) * float(a.norm()))
+        assert float((a - b).norm()) <= tol, shape
+
+
+def test_first_call_inside_a_capture():
+    """The kernels' attributes are set by the first call, which may be a captured one: in a process of its own."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2112_05387_amd import ops
+g = torch.Generator(device="cuda"); g.manual_seed(0)
+r = lambda *s: torch.randn(s, generator=g, device="cuda")
+x, w, y = r(600, 100), r(2000, 100), torch.randint(0, 2000, (600,), generator=g, device="cuda").to(torch.int32)
+us = [r(300, 200), r(64, 576), r(600, 700)]
+def step():
+    loss, rows, lse = ops.linear_ce_forward(x, w, y)
+    dx, dw, _ = ops.linear_ce_backward(x, w, y, lse)
+    lb, _, sb = ops.linear_ce_forward(x.bfloat16(), w.bfloat16(), y)
+    return [loss, lse, dx, dw, lb, *ops.linear_ce_backward(x.bfloat16(), w.bfloat16(), y, sb)[:2], *ops.orthogonalize(us)]
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = step()
+for _ in range(3):
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, step()))
+print("same", flush=True)
+"""
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=100)
+    assert done.returncode == 0 and "same" in done.stdout, done.stderr[-2000:]
+
+
 @pytest.mark.parametrize("dtype,head", [("f32", False), ("bf16", True)])
 def test_update_of_a_network(dtype, head):
     """LocalStep.muon_update: every filter of a network orthogonalised, the rest by lp_sgd_update's rule; AuxNets; one module only."""
