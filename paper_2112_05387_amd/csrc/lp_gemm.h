@@ -24,8 +24,8 @@
 // (both), DUAL 1440 of its three products, at 1.6 to 1.9 GHz; without the loads 1270 to 1570, the matrix cores busy for 85 % of
 // the clocks.  All eight waves in step: 1013, 1128, 1203, 1370; half as many waves of 128 x 128 each, a third fewer LDS
 // reads: 5 % less than that; fragments two k-steps ahead: the same.  DUAL in tiles of 128 x 128 (576 x 576 products of 64 and of
-// 256 workgroups): 145 and 186 us without loading waves, 118 and 173 with.  TRIPLE: 73623 x 8716 over 633 1120 TFLOP/s of its six
-// products, with the planes apart in 256 x 256 tiles 810; 230 workgroups of 128 x 128 over 1781 65 us, with planes apart 116.
+// 256 workgroups): 145 and 186 us without loading waves, 118 and 173 with.  TRIPLE: 73623 x 8716 over 633 1170 TFLOP/s of its six
+// products, with the planes apart in 256 x 256 tiles 810; 230 workgroups of 128 x 128 over 1781 64 us, with planes apart 116.
 // Rows are unpadded; their 16-byte chunks (KR: 32-byte pairs) trade places so that a read touches every bank once:
 //   KR = false  chunk c of row r at c ^ (r >> 1 & 7)
 //   KR = true   pair p of row k at p ^ 2 (k & 3) (rows of 256, 512 or 768 bytes), p ^ 2 (k >> 1 & 1) (128, 384 bytes), p (64 bytes)
@@ -35,6 +35,7 @@
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
+#include <utility>
 
 #include "lp_mma.h"
 
@@ -176,18 +177,21 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
             }
         }
         // the fragments of k-step S of the stage that starts at byte `st` (several planes: S = 2 * plane + k-step of the k-tile's two)
-        template <int S, int M = 0> __device__ __forceinline__ void read(unsigned st) {
+        template <int S, int M> __device__ __forceinline__ void read_one(unsigned st) {
             constexpr int slot = PL > 1 ? PL * (S & 1) + (S >> 1) : S & 1;   // [k-step][plane], or two k-steps
+            if constexpr (!KR)
+                asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(whole[slot][M]) : "v"(addr[TRIPLE ? S & 1 : S] + st), "i"(M * 32 * RK + (TRIPLE ? S / 2 * 64 : 0)));
+            else {
+                constexpr int off = (PL > 1 ? S & 1 : S) * 16 * RB;
+                // DUAL: the second plane two pairs on
+                const unsigned a = (TRIPLE ? addr[3 * M + S / 2] : DUAL && S >= 2 ? addr[M] ^ 64u : addr[M]) + st;
+                asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(half[slot][M][0]) : "v"(a), "i"(off));
+                asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(half[slot][M][1]) : "v"(a), "i"(off + 4 * RB));
+            }
+        }
+        template <int S, int M = 0> __device__ __forceinline__ void read(unsigned st) {
             if constexpr (M < F) {
-                if constexpr (!KR)
-                    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(whole[slot][M]) : "v"(addr[TRIPLE ? S & 1 : S] + st), "i"(M * 32 * RK + (TRIPLE ? S / 2 * 64 : 0)));
-                else {
-                    constexpr int off = (PL > 1 ? S & 1 : S) * 16 * RB;
-                    // DUAL: the second plane two pairs on
-                    const unsigned a = (TRIPLE ? addr[3 * M + S / 2] : DUAL && S >= 2 ? addr[M] ^ 64u : addr[M]) + st;
-                    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(half[slot][M][0]) : "v"(a), "i"(off));
-                    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(half[slot][M][1]) : "v"(a), "i"(off + 4 * RB));
-                }
+                read_one<S, M>(st);
                 read<S, M + 1>(st);
             }
         }
@@ -203,6 +207,9 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
             else return u32x4{half[slot][m][0][0], half[slot][m][0][1], half[slot][m][1][0], half[slot][m][1][1]};
         }
     };
+
+    // f of every constant of a list
+    template <class F, int... Q> __device__ static __forceinline__ void each(std::integer_sequence<int, Q...>, F f) { (f(std::integral_constant<int, Q>()), ...); }
 
     // waves that have no share of the result
     __device__ static __forceinline__ bool idle() { return LOADERS && (int)threadIdx.x >= NW * 64; }
@@ -264,17 +271,17 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
         // The loads of a k-tile are issued between the products behind the barrier that frees its stage.  Two stages: as early as
         // they go, one or more a place, as they have to land within the k-tile; more stages: evenly over a whole k-tile.
         constexpr int PHASES = KS, PLACES = STAGES == 2 ? (NL < 2 * NP ? NL : 2 * NP) : PHASES * NP;
-        // Several planes: the small terms first.  `ahead_of(p)` comes in front of every pair of planes.
+        // Several planes: the small terms first.  `ahead_of(n)` comes ahead of product n.
         auto products = [&](int slot, int first, bool issue, auto ahead_of) __attribute__((always_inline)) {
 #pragma unroll
             for (int p = 0; p < NP / NM; ++p) {
                 constexpr int pair_a[6] = {2, 0, 1, 1, 0, 0}, pair_b[6] = {0, 2, 1, 0, 1, 0};
-                ahead_of(p);
-                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < FI; ++i)
 #pragma unroll
                     for (int j = 0; j < FJ; ++j) {
+                        ahead_of(p * NM + i * FJ + j);
+                        __builtin_amdgcn_sched_barrier(0);
                         if constexpr (TRIPLE) Mma<E, 32>::run(ra.get(3 * slot + pair_a[p], i), rb.get(3 * slot + pair_b[p], j), acc[i][j]);
                         else if constexpr (DUAL) Mma<E, 32>::run(ra.get(2 * slot + (p == 0), i), rb.get(2 * slot + (p == 1), j), acc[i][j]);
                         else Mma<E, 32>::run(ra.get(slot, i), rb.get(slot, j), acc[i][j]);
@@ -382,24 +389,27 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 if (++sn == STAGES) sn = 0;
             }
         } else {
-            // all fragments of a k-step at once, or (TRIPLE: more than can be under way) a plane of them ahead of a pair's products
-            auto read_plane = [&](auto k, unsigned stage, int p) __attribute__((always_inline)) {
-                constexpr int S = decltype(k)::value;
-                if (p == 0) { ra.template read<S>(stage); rb.template read<S>(stage); }
-                if constexpr (PL > 1) if (p == 1) { ra.template read<S + 2>(stage); rb.template read<S + 2>(stage); }
-                if constexpr (TRIPLE) if (p == 2) { ra.template read<S + 4>(stage); rb.template read<S + 4>(stage); }
+            // The fragments of the next k-step.  A wave that issues an LDS read stands still for a while, and it is the only one of its SIMD
+            // that multiplies: where there are half as many products again as reads, the reads are spread over the first two thirds of
+            // them (128 x 128, two planes: 201 workgroups over 5760 115 -> 105 us; three, rows along k: 510 -> 440).  Where there are fewer
+            // (one plane, or 64 x 64) that is up to 10 % slower than reading ahead of the products, three planes one at a time.
+            constexpr int NR = PL * (FI + FJ), SPAN = NP * 2 / 3;
+            constexpr bool BETWEEN = 2 * NP >= 3 * NR;
+            auto fragment = [&](auto k, auto q, unsigned stage) __attribute__((always_inline)) {
+                constexpr int S = decltype(k)::value + 2 * (decltype(q)::value / (FI + FJ)), M = decltype(q)::value % (FI + FJ);
+                if constexpr (M < FI) ra.template read_one<S, M>(stage);
+                else rb.template read_one<S, M - FI>(stage);
             };
             auto step = [&](auto k, unsigned stage, int slot, int first, bool issue) __attribute__((always_inline)) {
-                if constexpr (!TRIPLE) {
-#pragma unroll
-                    for (int p = 0; p < PL; ++p) read_plane(k, stage, p);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-                products(slot, first, issue, [&](int p) __attribute__((always_inline)) { if constexpr (TRIPLE) if (p < 3) read_plane(k, stage, p); });
+                products(slot, first, issue, [&](int n) __attribute__((always_inline)) {
+                    each(std::make_integer_sequence<int, NR>(), [&](auto q) __attribute__((always_inline)) {
+                        constexpr int Q = decltype(q)::value;
+                        if (n == (BETWEEN ? Q * SPAN / NR + 1 : TRIPLE ? Q / (FI + FJ) * NM : 0)) fragment(k, q, stage);
+                    });
+                });
                 arrived(slot ^ 1);
             };
-#pragma unroll
-            for (int p = 0; p < PL; ++p) read_plane(k0, 0, p);
+            each(std::make_integer_sequence<int, NR>(), [&](auto q) __attribute__((always_inline)) { fragment(k0, q, 0u); });
             arrived(0);
             unsigned st = 0;
             int sn = 0;

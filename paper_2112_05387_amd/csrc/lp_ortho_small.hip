@@ -3,8 +3,9 @@
 // The products of a matrix of at most 64 rows (a filter of a narrow network: 64 x 576) are a few microseconds of work and fifteen
 // launches of it.  Here a workgroup of eight waves keeps X in LDS, both parts (147 KB of the 160), and S and B in the 16 KB beside
 // it, in turn; what a product yields stays in registers until everybody has read what it replaces.  Precision and scales are
-// those of the large matrices' products.  A step of 64 x 576 is 0.1 TFLOP/s a compute unit over three products of fp16 parts, LDS reads
-// bound it: 5 us, against 20 us for the three launches.
+// those of the large matrices' products.  A step of 64 x 576 is 14 MFLOP in three products of fp16 parts and 7.5 us, of which the LDS reads
+// of two products on the same 147 KB and the exchange of S and B between the waves are most; the three launches it replaces take 20.
+// The whole matrix, read, five steps and written: 60 us, an update of 55 of them and 110 vectors 76.
 //
 // X lies in LDS as rows of 128-byte groups, 32 first parts and the same 32 second parts, S and B as rows of two groups.  The 16-byte
 // chunks of every 256 bytes trade places by the row, F(row) = 4 (row & 3) + (row >> 2 & 3): 16 rows of a chunk lie on all banks (fragments
