@@ -655,10 +655,10 @@ template <class T, int WAVES> hipError_t launch_grad_t(const CeGrad& a, int slic
 
 // Time of a product cut into `blocks` workgroups of `ktiles` k-tiles each, microseconds: rounds of as many as run at once, a k-tile of a
 // full chip and of a nearly empty one as measured (256 x 256 1.95 and 1.4 us, 128 x 128 0.52 and 0.36, 64 x 64 0.43 and 0.27, 128 x 32
-// 0.40 and 0.25; of three planes, 32 k, 128 x 128 1.1 and 0.9, 64 x 64 0.7 to 0.85 and 0.4), and what a workgroup does besides.
+// 0.40 and 0.25; of three planes, 32 k, 128 x 128 1.13 and 0.95, 64 x 64 0.7 to 0.85 and 0.4), and what a workgroup does besides.
 double ce_tile_time(int cfg, long blocks, int ktiles) {
     static const struct { int slots; double some, full, rest; } t[6] = {{256, 1.4, 1.95, 6.0}, {256, 0.36, 0.52, 4.0}, {512, 0.27, 0.43, 3.0},
-                                                                        {512, 0.25, 0.40, 3.0}, {256, 0.9, 1.1, 5.0}, {512, 0.4, 0.75, 4.0}};
+                                                                        {512, 0.25, 0.40, 3.0}, {256, 0.95, 1.13, 5.0}, {512, 0.4, 0.75, 4.0}};
     const long rounds = blocks / t[cfg].slots, over = blocks - rounds * t[cfg].slots;
     const double last = t[cfg].some + (t[cfg].full - t[cfg].some) * (double)over / t[cfg].slots;
     return (double)rounds * (t[cfg].rest + ktiles * t[cfg].full) + (over ? t[cfg].rest + ktiles * last : 0.0);
