@@ -64,29 +64,35 @@ template <class T, int NP> __global__ __launch_bounds__(256) void ce_pack_kernel
     const CePack& a = first ? x : w;
     const T* const src = reinterpret_cast<const T*>(a.src);
     unsigned short* const dst = reinterpret_cast<unsigned short*>(a.dst);
-    const int cpr = a.width >> 3;                                 // chunks of eight elements in a row
+    constexpr int E = 4;                                          // elements of a thread: its loads lie beside its neighbours'
+    const int cpr = a.width / E;
     const size_t n = (size_t)a.rows * cpr;
+    const bool vec = a.ld % E == 0;                               // (the first row is aligned)
     for (size_t t = (size_t)(blockIdx.x - (first ? 0 : x.blocks)) * 256 + threadIdx.x; t < n; t += (size_t)a.blocks * 256) {
-        const int r = (int)(t / cpr), c = (int)(t - (size_t)r * cpr) * 8;
+        const int r = (int)(t / cpr), c = (int)(t - (size_t)r * cpr) * E;
         const T* s = src + (size_t)r * a.ld + c;
-        unsigned short out[NP][8];
+        unsigned short out[NP][E];
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if constexpr (sizeof(T) == 2) out[0][e] = c + e < a.cols ? reinterpret_cast<const unsigned short*>(s)[e] : 0;
-            else {
+            for (int e = 0; e < E; ++e) out[0][e] = c + e < a.cols ? reinterpret_cast<const unsigned short*>(s)[e] : 0;
+        } else {
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+            if (vec && c + E <= a.cols) v = *reinterpret_cast<const f32x4*>(s);
+            else
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (c + e < a.cols) v[e] = s[e];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
                 unsigned b[NP];
-                split_bf16<NP>(c + e < a.cols ? to_float(s[e]) : 0.f, b);
+                split_bf16<NP>(v[e], b);
 #pragma unroll
                 for (int p = 0; p < NP; ++p) out[p][e] = (unsigned short)b[p];
             }
         }
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            u32x4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = out[p][2 * e] | ((unsigned)out[p][2 * e + 1] << 16);
-            *reinterpret_cast<u32x4*>(dst + (size_t)r * (NP * a.width) + plane_at<NP>(c, p, 0)) = v;
-        }
+        for (int p = 0; p < NP; ++p)
+            *reinterpret_cast<u32x2*>(dst + (size_t)r * (NP * a.width) + plane_at<NP>(c, p, 0)) = u32x2{out[p][0] | ((unsigned)out[p][1] << 16), out[p][2] | ((unsigned)out[p][3] << 16)};
     }
 }
 
@@ -670,7 +676,7 @@ void ce_tile_size(int cfg, int* bi, int* bj, int* wi, int* wj) {
 }
 
 hipError_t launch_ce_pack(CePack x, CePack w, int dtype, hipStream_t s) {
-    for (CePack* a : {&x, &w}) a->blocks = (int)std::min<size_t>(((size_t)a->rows * (a->width >> 3) + 255) / 256, 1u << 16);
+    for (CePack* a : {&x, &w}) a->blocks = (int)std::min<size_t>(((size_t)a->rows * (a->width / 4) + 255) / 256, 1u << 16);
     const dim3 grid(x.blocks + w.blocks);
     if (grid.x == 0) return hipSuccess;
     if (dtype == 1) hipLaunchKernelGGL((ce_pack_kernel<bf16_t, 1>), grid, dim3(256), 0, s, x, w);
