@@ -146,28 +146,37 @@ __global__ __launch_bounds__(256) void ns_split_kernel(const NsArgs a) {
     const int pi = ns_find(a.start, a.n, blockIdx.x);
     const NsProb& P = a.p[pi];
     const int tid = threadIdx.x;
+    const int local = blockIdx.x - a.start[pi], pc = (P.cols + 63) >> 6;
+    const int r0 = local / pc * 64, c0 = (local - local / pc * pc) * 64;
+    const int col = tid & 63, c = c0 + col;
+    // the elements and the sums of squares under way together
+    float u[16], g[16];
+    auto place = [&](int k, long ld) __attribute__((always_inline)) { return (size_t)min(r0 + (tid >> 6) + 4 * k, P.rows - 1) * ld + min(c, P.cols - 1); };
+    if (P.src && (P.flags & NS_SRC_LOW)) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) u[k] = bf16_bits_to_float(reinterpret_cast<const unsigned short*>(P.src)[place(k, P.ld_src)]);
+    } else if (P.src) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) u[k] = reinterpret_cast<const float*>(P.src)[place(k, P.ld_src)];
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            u[k] = P.vel[place(k, P.cols)];
+            g[k] = a.nesterov ? P.grad[place(k, P.cols)] : 0.f;
+        }
+    }
     const int b0 = a.start_norm[pi], b1 = a.start_norm[pi + 1];
     double sum = 0.0;
+#pragma unroll 4
     for (int b = b0 + tid; b < b1; b += 256) sum += a.norm[b];
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
     if ((tid & 63) == 0) s[tid >> 6] = sum;
-    const int local = blockIdx.x - a.start[pi], pc = (P.cols + 63) >> 6;
-    const int r0 = local / pc * 64, c0 = (local - local / pc * pc) * 64;
-    const int col = tid & 63, c = c0 + col;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-        const int row = (tid >> 6) + 4 * k, rr = r0 + row;
-        float u = 0.f;
-        if (rr < P.rows && c < P.cols) {
-            if (P.src) u = load_low(P.src, P.flags & NS_SRC_LOW, (size_t)rr * P.ld_src + c);
-            else {
-                const size_t e = (size_t)rr * P.cols + c;
-                u = P.vel[e];
-                if (a.nesterov) u = fmaf(a.momentum, u, P.grad[e]);
-            }
-        }
-        t[row][col] = u;
+        const int row = (tid >> 6) + 4 * k;
+        const float w = P.src || !a.nesterov ? u[k] : fmaf(a.momentum, u[k], g[k]);
+        t[row][col] = r0 + row < P.rows && c < P.cols ? w : 0.f;
     }
     __syncthreads();
     const double norm = sqrt((s[0] + s[1]) + (s[2] + s[3]));

@@ -135,11 +135,35 @@ template <int NJ, int NI> __device__ void small_matrix(const NsArgs& a, const Ns
             }
         }
     } else {
-#pragma unroll 4
-        for (int e = tid; e < numel; e += kThreads) {
-            const int row = row_of(e), col = e - row * cols;
-            if (P.src) put(row, col, load_low(P.src, src_low, (size_t)row * P.ld_src + col));
-            else { float vt = P.vel[e]; put(row, col, momentum(P.grad[e], vt)); P.vel[e] = vt; }
+        // eight elements a thread and trip, all loads first
+        constexpr int U = 8;
+        for (int e0 = tid; e0 < numel; e0 += kThreads * U) {
+            float g[U], v[U];
+            auto from = [&](int q) __attribute__((always_inline)) {
+                const int e = min(e0 + q * kThreads, numel - 1), row = row_of(e);
+                return (size_t)row * P.ld_src + (e - row * cols);
+            };
+            if (P.src && src_low) {
+#pragma unroll
+                for (int q = 0; q < U; ++q) g[q] = bf16_bits_to_float(reinterpret_cast<const unsigned short*>(P.src)[from(q)]);
+            } else if (P.src) {
+#pragma unroll
+                for (int q = 0; q < U; ++q) g[q] = reinterpret_cast<const float*>(P.src)[from(q)];
+            } else {
+#pragma unroll
+                for (int q = 0; q < U; ++q) {
+                    const int e = min(e0 + q * kThreads, numel - 1);
+                    g[q] = P.grad[e]; v[q] = P.vel[e];
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < U; ++q) {
+                const int e = e0 + q * kThreads;
+                if (e >= numel) continue;
+                const int row = row_of(e), col = e - row * cols;
+                if (P.src) put(row, col, g[q]);
+                else { float vt = v[q]; put(row, col, momentum(g[q], vt)); P.vel[e] = vt; }
+            }
         }
     }
 #pragma unroll
