@@ -7,8 +7,8 @@
 // Every row reads all of the weights from L2, so what bounds these kernels is how long a chain of such reads is: a lane has a class,
 // the waves of a row have a part of the channels each; for the gradients a group of threads has the channels and a part of
 // the classes or rows.  The rule that sends a problem here (ce_direct_waves) bounds the chains.  Loss and
-// gradients in fp32, host and all, tiled and here: 256 x 16 -> 10 67 and 45 us, 212 x 277 -> 112 70 and 47, 2 x 19 -> 2485 73 and 66; bf16
-// 911 x 28 -> 541 71 and 47.
+// gradients in fp32, host and all, tiled and here: 256 x 16 -> 10 67 and 38 us, 212 x 277 -> 112 70 and 42, 2 x 19 -> 2485 73 and 50; bf16
+// 911 x 28 -> 541 71 and 41.
 #include <algorithm>
 
 #include "lp_classes.h"
