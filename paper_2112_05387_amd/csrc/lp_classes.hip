@@ -634,12 +634,12 @@ __global__ __launch_bounds__(256) void ce_zero_kernel(float* p, size_t n) {
 
 // tiles: big and middle (one workgroup a compute unit), small (two), few samples
 template <bool AKR, bool BKR, bool M> using TBig = GemmTile<bf16_t, AKR, BKR, 2, 4, 4, 2, 2, M>;
-template <bool AKR, bool BKR, bool M> using TMid = GemmTile<bf16_t, AKR, BKR, 2, 2, 2, 2, 4, M, 1, true>;
-template <bool AKR, bool BKR, bool M> using TSmall = GemmTile<bf16_t, AKR, BKR, 2, 2, 1, 1, 4, M, 1, true>;
-template <bool AKR, bool BKR, bool M> using TFew = GemmTile<bf16_t, AKR, BKR, 4, 1, 1, 1, 3, M, 1, true>;
+template <bool AKR, bool BKR, bool M> using TMid = GemmTile<bf16_t, AKR, BKR, 2, 2, 2, 2, 4, M>;
+template <bool AKR, bool BKR, bool M> using TSmall = GemmTile<bf16_t, AKR, BKR, 2, 2, 1, 1, 4, M>;
+template <bool AKR, bool BKR, bool M> using TFew = GemmTile<bf16_t, AKR, BKR, 4, 1, 1, 1, 3, M>;
 // ... of three planes
-template <bool AKR, bool BKR, bool M> using TMid3 = GemmTile<bf16_t, AKR, BKR, 2, 2, 2, 2, 3, M, 3, true>;
-template <bool AKR, bool BKR, bool M> using TSmall3 = GemmTile<bf16_t, AKR, BKR, 2, 2, 1, 1, 3, M, 3, true>;
+template <bool AKR, bool BKR, bool M> using TMid3 = GemmTile<bf16_t, AKR, BKR, 2, 2, 2, 2, 3, M, 3>;
+template <bool AKR, bool BKR, bool M> using TSmall3 = GemmTile<bf16_t, AKR, BKR, 2, 2, 1, 1, 3, M, 3>;
 
 template <class K, class A> hipError_t launch(K kernel, OncePerDevice& once, dim3 grid, int threads, int lds, hipStream_t s, const A& args) {
     if (const hipError_t e = raise_lds_limit(once, {(const void*)kernel}, lds); e != hipSuccess) return e;

@@ -15,11 +15,9 @@
 // second [and of the third] in 128 [192] bytes, and a k-tile is 32 k of all.  From the fragments of two planes come three products, of
 // three planes six (the others are below the precision): half as much again, or twice as much, for the same loads and LDS reads.
 //
-// A k-tile is 128 (192) bytes of a row long, and its loads are spread between the products of the one before it.  Three shapes:
-//   eight waves (256 x 256, one workgroup a compute unit): two groups that take turns;
-//   four waves and four more that only load (LOADERS; tiles of 128 and less);
-//   four waves, each its share of the loads between its products.
-// In the latter two one barrier a k-tile, ahead of the products of its last 16 k, both frees its stage and shows the next.
+// A k-tile is 128 (192) bytes of a row long.  Eight waves (256 x 256 and 256 x 320, one workgroup a compute unit) are two groups that
+// take turns, the loads of the next k-tile between their products.  Four waves (tiles of 128 and less) have four more beside them
+// that only load; one barrier a k-tile, ahead of the products of its last 16 k, both frees its stage and shows the next.
 // What bounds it: power.  8192 x 8192 x 4096 in bf16 1105 (k contiguous), 1220 (one operand with rows along k), 1240 TFLOP/s
 // (both), DUAL 1440 of its three products, at 1.6 to 1.9 GHz; without the loads 1270 to 1570, the matrix cores busy for 85 % of
 // the clocks.  All eight waves in step: 1013, 1128, 1203, 1370; half as many waves of 128 x 128 each, a third fewer LDS
@@ -63,16 +61,18 @@ typedef __attribute__((address_space(3))) void* gemm_lds_t;
 typedef const __attribute__((address_space(4))) unsigned long long* GemmMask;      // read by scalar loads
 typedef __attribute__((ext_vector_type(4))) short gemm_s16x4;
 
-template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGES, bool MASKED = false, int PL = 1, bool LOADERS = false> struct GemmTile {
-    static constexpr int NW = WI * WJ, NT = NW * 64 * (LOADERS ? 2 : 1);
+template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGES, bool MASKED = false, int PL = 1> struct GemmTile {
+    static constexpr int NW = WI * WJ;
+    static constexpr bool TURNS = NW == 8, LOADERS = !TURNS;        // two waves a SIMD, one of either group; as many waves again that load (see run)
+    static constexpr int NT = NW * 64 * (LOADERS ? 2 : 1);
     static constexpr int TI = FI * 32, TJ = FJ * 32, BI = WI * TI, BJ = WJ * TJ;
     static constexpr bool DUAL = PL == 2, TRIPLE = PL == 3;         // planes beside each other
     static constexpr int KT = PL == 1 ? 64 : 32, KS = KT / 16, RK = KT * PL * 2;    // k of a k-tile; bytes of a row (k contiguous)
     static constexpr int A_BYTES = BI * RK, STAGE = (BI + BJ) * RK, LDS = STAGES * STAGE;
     static constexpr int NSA = A_BYTES / 1024 / NW, NSB = (STAGE - A_BYTES) / 1024 / NW, NL = NSA + NSB;      // wave-loads of a k-tile
-    static constexpr bool TURNS = NW == 8;                          // two waves a SIMD, one of either group (see run)
     static_assert(NW % 2 == 0 && NSA * NW * 1024 == A_BYTES && NL * NW * 1024 == STAGE, "every wave loads the same number of slabs");
-    static_assert(!TRIPLE || (LOADERS && !TURNS && NSA % 3 == 0 && NSB % 3 == 0), "loads of three slabs, by waves of their own");
+    static_assert(TURNS || NW == 4, "one or two multiplying waves a SIMD");
+    static_assert(!TRIPLE || (LOADERS && NSA % 3 == 0 && NSB % 3 == 0), "loads of three slabs, by waves of their own");
     typedef f32x16 Acc[FI][FJ];
 
     static constexpr unsigned kOOB = 0x80000000u;       // beyond any buffer of 2^31 - 1 bytes
@@ -267,12 +267,9 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 rb.arrived(PL * slot + p);
             }
         };
-        constexpr int NM = FI * FJ, NP = TRIPLE ? 6 * NM : DUAL ? 3 * NM : NM;   // products of a phase (a k-step) = places for loads
-        // The loads of a k-tile are issued between the products behind the barrier that frees its stage.  Two stages: as early as
-        // they go, one or more a place, as they have to land within the k-tile; more stages: evenly over a whole k-tile.
-        constexpr int PHASES = KS, PLACES = STAGES == 2 ? (NL < 2 * NP ? NL : 2 * NP) : PHASES * NP;
+        constexpr int NM = FI * FJ, NP = TRIPLE ? 6 * NM : DUAL ? 3 * NM : NM;   // products of a k-step
         // Several planes: the small terms first.  `ahead_of(n)` comes ahead of product n.
-        auto products = [&](int slot, int first, bool issue, auto ahead_of) __attribute__((always_inline)) {
+        auto products = [&](int slot, auto ahead_of) __attribute__((always_inline)) {
 #pragma unroll
             for (int p = 0; p < NP / NM; ++p) {
                 constexpr int pair_a[6] = {2, 0, 1, 1, 0, 0}, pair_b[6] = {0, 2, 1, 0, 1, 0};
@@ -285,16 +282,11 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                         if constexpr (TRIPLE) Mma<E, 32>::run(ra.get(3 * slot + pair_a[p], i), rb.get(3 * slot + pair_b[p], j), acc[i][j]);
                         else if constexpr (DUAL) Mma<E, 32>::run(ra.get(2 * slot + (p == 0), i), rb.get(2 * slot + (p == 1), j), acc[i][j]);
                         else Mma<E, 32>::run(ra.get(slot, i), rb.get(slot, j), acc[i][j]);
-                        if (issue) {
-#pragma unroll
-                            for (int q = 0; q < NL; ++q)
-                                if (q * PLACES / NL == first + p * NM + i * FJ + j) issue_one(q);
-                        }
                         __builtin_amdgcn_sched_barrier(0);
                     }
             }
         };
-        if (!LOADERS || loader) {
+        if (TURNS || loader) {
 #pragma unroll
             for (int s = 0; s < (TURNS ? 1 : STAGES); ++s) {
                 mask_ahead();
@@ -400,8 +392,8 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 if constexpr (M < FI) ra.template read_one<S, M>(stage);
                 else rb.template read_one<S, M - FI>(stage);
             };
-            auto step = [&](auto k, unsigned stage, int slot, int first, bool issue) __attribute__((always_inline)) {
-                products(slot, first, issue, [&](int n) __attribute__((always_inline)) {
+            auto step = [&](auto k, unsigned stage, int slot) __attribute__((always_inline)) {
+                products(slot, [&](int n) __attribute__((always_inline)) {
                     each(std::make_integer_sequence<int, NR>(), [&](auto q) __attribute__((always_inline)) {
                         constexpr int Q = decltype(q)::value;
                         if (n == (BETWEEN ? Q * SPAN / NR + 1 : TRIPLE ? Q / (FI + FJ) * NM : 0)) fragment(k, q, stage);
@@ -414,25 +406,18 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
             unsigned st = 0;
             int sn = 0;
             for (int t = 0; t < total; ++t) {
-                // (in the first iteration all of the stages' loads are under way)
-                step(k1, st, 0, NP, !LOADERS && t > 0);
+                step(k1, st, 0);
                 if constexpr (PL == 1) {
-                    step(k2, st, 1, 2 * NP, !LOADERS && t > 0);
-                    step(k3, st, 0, 3 * NP, !LOADERS && t > 0);
+                    step(k2, st, 1);
+                    step(k3, st, 0);
                 }                                              // this wave has read all of its stage
-                if constexpr (!LOADERS) wait_vmcnt<(STAGES - 2) * NL>();      // k-tile t + 1 landed (this wave's share)
                 asm volatile("" ::: "memory");
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
-                const int freed = sn;
                 if (++sn == STAGES) sn = 0;
                 st = (unsigned)(sn * STAGE);
-                if constexpr (!LOADERS) tile_begin(freed);
-                step(k0, st, 1, 0, !LOADERS);                  // (behind the last k-tile it reads zeros, not used)
+                step(k0, st, 1);                               // (behind the last k-tile it reads zeros, not used)
             }
-#pragma unroll
-            for (int q = 0; q < NL; ++q)                       // what would have been issued in the next iteration: zeros
-                if (!LOADERS && q * PLACES / NL >= NP) issue_one(q);
         }
         wait_vmcnt<0>();
         asm volatile("" ::: "memory");

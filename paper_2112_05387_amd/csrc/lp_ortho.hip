@@ -414,8 +414,8 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
 
 template <bool AKR> using NBig = GemmTile<f16_t, AKR, false, 2, 4, 4, 2, 2, false, 2>;
 template <bool AKR> using NWide = GemmTile<f16_t, AKR, false, 4, 2, 2, 5, 2, false, 2>;
-template <bool AKR> using NMid = GemmTile<f16_t, AKR, false, 2, 2, 2, 2, 4, false, 2, true>;
-template <bool AKR> using NSmall = GemmTile<f16_t, AKR, false, 2, 2, 1, 1, 4, false, 2, true>;
+template <bool AKR> using NMid = GemmTile<f16_t, AKR, false, 2, 2, 2, 2, 4, false, 2>;
+template <bool AKR> using NSmall = GemmTile<f16_t, AKR, false, 2, 2, 1, 1, 4, false, 2>;
 
 template <class T, int MODE> hipError_t launch_gemm(const NsArgs& a, hipStream_t s) {
     static OncePerDevice once;
