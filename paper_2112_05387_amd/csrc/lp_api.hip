@@ -3270,12 +3270,14 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     const int nl = low ? 1 : 2, nw = 2;
     const unsigned all = low ? 7u : 48u, few = low && p.N <= 32 ? 8u : 0u, small = low ? 4u : 32u;
 
-    // logits: by tiles that finish their rows, or cut along the channels, with the softmax as a pass of its own (some 8 us)
+    // logits: by tiles that finish their rows, or cut along the channels, with the softmax as a pass of its own
     double whole, cut;
     const int N1 = std::max(1, p.N);
     p.tl = best_plan(p.V, N1, p.K, nl, all | few, false, &whole);
     const TilePlan tc = best_plan(p.V, N1, p.K, nl, small | few, true, &cut);
-    p.cut = cut + 8.0 < whole && (size_t)tc.slices * N1 * p.V <= ((size_t)8 << 20);
+    // (some 8 us); and so where a few rows have few classes, any of them may be all but certain, and its gradient takes the sum of
+    // its other probabilities (1 x 2026 -> 234 with a loss of 0.003, dW off by 4e-4 by tiles, which have only its lse in fp32).
+    p.cut = (cut + 8.0 < whole || (N1 <= 32 && p.V <= 2048)) && (size_t)tc.slices * N1 * p.V <= ((size_t)8 << 20);
     if (p.cut) p.tl = tc;
     if ((long)p.tl.ti * p.tl.tj > (1l << 30)) return fail(LP_ERR_SHAPE, "%d rows x %d classes in one call", p.N, p.V);
     int bi, bj, wi, wj;

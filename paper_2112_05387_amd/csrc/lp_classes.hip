@@ -212,13 +212,18 @@ template <class T, int MODE, int NP, int WAVES> __global__ __launch_bounds__(T::
             const int y = n < a.N ? a.labels[n] : -1;
             const bool valid = is_class(y, a.V_all);
             const float shift = n < a.N ? a.lse[n] * kLog2e : 0.f;
+            // the label's class, where this lane has it: its one is taken off before the parts are formed
+            const int at = valid ? y - a.v0 - ib - 4 * h : -1;
 #pragma unroll
             for (int i = 0; i < FI; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     float p[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) p[e] = valid ? __builtin_amdgcn_exp2f(acc[i][j][4 * q + e] - shift) : 0.f;
+                    for (int e = 0; e < 4; ++e) {
+                        p[e] = valid ? __builtin_amdgcn_exp2f(acc[i][j][4 * q + e] - shift) : 0.f;
+                        if (at == i * 32 + 8 * q + e) p[e] -= 1.f;
+                    }
                     unsigned char* const d = E0 + lr * PITCH + (i * 32 + 8 * q + 4 * h) * 2;
 #pragma unroll
                     for (int k = 0; k < NP; ++k) {
@@ -228,19 +233,6 @@ template <class T, int MODE, int NP, int WAVES> __global__ __launch_bounds__(T::
                         p[2] -= __uint_as_float(hi << 16); p[3] -= __uint_as_float(hi & 0xffff0000u);
                     }
                 }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_s_waitcnt(0xc07f);
-            const int at = y - a.v0 - ib;                        // the label's class, where it is one of this wave's
-            if (h == 0 && valid && (unsigned)at < (unsigned)T::TI) {
-                unsigned short* const d = reinterpret_cast<unsigned short*>(E0 + lr * PITCH + at * 2);
-                float p = 0.f;
-#pragma unroll
-                for (int k = NP - 1; k >= 0; --k) p += bf16_up(d[k * (EP / 2)]);
-                unsigned b[NP];
-                split_bf16<NP>(p - 1.f, b);
-#pragma unroll
-                for (int k = 0; k < NP; ++k) d[k * (EP / 2)] = (unsigned short)b[k];
-            }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_s_waitcnt(0xc07f);
             const int v = ib + c * 8;
@@ -359,9 +351,9 @@ template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_k
                 float2 l = sliced(row + v, a.slice, a.nslices);
                 if (a.bias) { l.x += a.bias[v]; l.y += v + 1 < a.V ? a.bias[v + 1] : 0.f; }
                 if (v == y) own = l.x;
+                else join(m, s, l.x * kLog2e, 1.f);
                 if (v + 1 == y) own = l.y;
-                join(m, s, l.x * kLog2e, 1.f);
-                if (v + 1 < a.V) join(m, s, l.y * kLog2e, 1.f);
+                else if (v + 1 < a.V) join(m, s, l.y * kLog2e, 1.f);
             }
         } else {
             const float2* const row = a.partial + (size_t)n * a.parts;
@@ -403,10 +395,16 @@ template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_k
         }
     }
     if (n < a.N && part == 0) {
-        const float lse = (m + __builtin_amdgcn_logf(s)) * kLn2;       // log2
         if (!SLICES && valid && a.bias) own += a.bias[y];
-        // (not lse - own: of a row that is all but certain the logits cancel first)
-        loss = valid ? ((m - own * kLog2e) + __builtin_amdgcn_logf(s)) * kLn2 : 0.f;
+        const float o2 = own * kLog2e, mo = m, so = s;            // (SLICES: of the other classes, where there is a label)
+        if (SLICES && valid) join(m, s, o2, 1.f);
+        const float lse = (m + __builtin_amdgcn_logf(s)) * kLn2;       // log2
+        // Of a row that is all but certain the logits cancel first, and what the other classes have is not added to one (a logit at the
+        // end of fp32's range has none to base 2).
+        if (!valid) loss = 0.f;
+        else if (__builtin_isinf(o2)) loss = lse - own;
+        else if (SLICES && mo - o2 < 8.f) loss = log1pf(so * __builtin_amdgcn_exp2f(mo - o2));
+        else loss = ((m - o2) + __builtin_amdgcn_logf(s)) * kLn2;
         if (lane == 0) {
             a.lse[n] = lse;
             if (a.row_loss) a.row_loss[n] = loss;
@@ -442,21 +440,39 @@ template <int NP> __global__ __launch_bounds__(256) void ce_prob_kernel(const Ce
     const bool valid = is_class(y, a.V);
     const float shift = a.lse[n] * kLog2e;
     const float* const row = a.slices + (size_t)n * a.ldv;
-    for (int v = threadIdx.x * 2; v < a.ldv; v += 512) {
+    // the label's p - 1, where p is near one, as minus the sum of the others: 1 - p would lose what tells them apart
+    __shared__ float s_others[4];
+    float others = 0.f, mine[2] = {0.f, 0.f};
+    int at = -1;                                                  // this thread has the label's pair
+    auto store = [&](int v, const float (&p)[2]) __attribute__((always_inline)) {
         unsigned b[2][NP];
-        const float2 l = sliced(row + v, a.slice, a.nslices);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float p = 0.f;
-            if (valid && v + e < a.V) {
-                p = __builtin_amdgcn_exp2f(fmaf((e ? l.y : l.x) + (a.bias ? a.bias[v + e] : 0.f), kLog2e, -shift));
-                if (v + e == y) p -= 1.f;
-            }
-            split_bf16<NP>(p, b[e]);
-        }
+        for (int e = 0; e < 2; ++e) split_bf16<NP>(p[e], b[e]);
 #pragma unroll
         for (int k = 0; k < NP; ++k) *reinterpret_cast<unsigned*>(prob + (size_t)n * ldp + plane_at<NP>(v, k, pplane / 2)) = b[0][k] | (b[1][k] << 16);
+    };
+    for (int v = threadIdx.x * 2; v < a.ldv; v += 512) {
+        const float2 l = sliced(row + v, a.slice, a.nslices);
+        float p[2] = {0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (valid && v + e < a.V) {
+                p[e] = __builtin_amdgcn_exp2f(fmaf((e ? l.y : l.x) + (a.bias ? a.bias[v + e] : 0.f), kLog2e, -shift));
+                if (v + e != y) others += p[e];
+            }
+        if (valid && (v == y || v + 1 == y)) { at = v; mine[0] = p[0]; mine[1] = p[1]; }
+        else store(v, p);
     }
+    if (!valid) return;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) others += __shfl_xor(others, o);
+    if ((threadIdx.x & 63) == 0) s_others[threadIdx.x >> 6] = others;
+    __syncthreads();
+    if (at < 0) return;
+    others = (s_others[0] + s_others[1]) + (s_others[2] + s_others[3]);
+    float& p = y == at ? mine[0] : mine[1];
+    p = p > 0.5f ? -others : p - 1.f;
+    store(at, mine);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------

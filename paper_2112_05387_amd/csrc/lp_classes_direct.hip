@@ -93,17 +93,19 @@ template <class T, int NW> __global__ __launch_bounds__(NW * 64) void ce_direct_
     for (int w = 0; w < NW; ++w) m = fmaxf(m, s_r[w]);
     __syncthreads();
     const float m0 = m == -kInf ? 0.f : m;
-    float s = 0.f;
-    for (int v = tid; v < a.V; v += NW * 64) s += __builtin_amdgcn_exp2f((s_l[v] - m0) * kLog2e);
+    float s = 0.f;                                               // of the classes but the label's
+    for (int v = tid; v < a.V; v += NW * 64) s += v == y ? 0.f : __builtin_amdgcn_exp2f((s_l[v] - m0) * kLog2e);
     s = wave_sum(s);
     if (lane == 0) s_r[wave] = s;
     __syncthreads();
     if (tid != 0) return;
     s = 0.f;
     for (int w = 0; w < NW; ++w) s += s_r[w];
-    const float ls = __builtin_amdgcn_logf(s) * kLn2, lse = m + ls;
     const bool valid = is_class(y, a.V);
-    const float loss = valid ? (m - s_l[y]) + ls : 0.f;      // (not lse - l: of a row that is all but certain the logits cancel first)
+    const float own = valid ? s_l[y] : -kInf, all = s + __builtin_amdgcn_exp2f((own - m0) * kLog2e);
+    const float ls = __builtin_amdgcn_logf(all) * kLn2, lse = m + ls;
+    // of a row that is all but certain the logits cancel first, and what the other classes have is not added to one
+    const float loss = !valid ? 0.f : m - own < 5.f ? log1pf(s * __builtin_amdgcn_exp2f((m - own) * kLog2e)) : (m - own) + ls;
     a.lse_out[n] = lse;
     if (a.row_loss) a.row_loss[n] = loss;
     a.bsum[n] = loss;

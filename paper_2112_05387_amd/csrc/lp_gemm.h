@@ -21,8 +21,8 @@
 // What bounds it: power.  8192 x 8192 x 4096 in bf16 1105 (k contiguous), 1220 (one operand with rows along k), 1240 TFLOP/s
 // (both), DUAL 1440 of its three products, at 1.6 to 1.9 GHz; without the loads 1270 to 1570, the matrix cores busy for 85 % of
 // the clocks.  All eight waves in step: 1013, 1128, 1203, 1370; half as many waves of 128 x 128 each, a third fewer LDS
-// reads: 5 % less than that; fragments two k-steps ahead: the same.  DUAL in tiles of 128 x 128 (576 x 576 products of 64 and of
-// 256 workgroups): 145 and 186 us without loading waves, 118 and 173 with.  TRIPLE: 73623 x 8716 over 633 1170 TFLOP/s of its six
+// reads: 5 % less than that; fragments two k-steps ahead: the same.  DUAL in tiles of 128 x 128 over 8192, 64 and 256
+// workgroups: 145 and 186 us without loading waves, 118 and 173 with.  TRIPLE: 73623 x 8716 over 633 1170 TFLOP/s of its six
 // products, with the planes apart in 256 x 256 tiles 810; 230 workgroups of 128 x 128 over 1781 64 us, with planes apart 116.
 // Rows are unpadded; their 16-byte chunks (KR: 32-byte pairs) trade places so that a read touches every bank once:
 //   KR = false  chunk c of row r at c ^ (r >> 1 & 7)
@@ -214,7 +214,7 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
     // waves that have no share of the result
     __device__ static __forceinline__ bool idle() { return LOADERS && (int)threadIdx.x >= NW * 64; }
 
-    // Adds to acc the products of rows i0.. of A and j0.. of B over k in [kb, ke), kb a multiple of 64.  (DUAL: one pair, and operands
+    // Adds to acc the products of rows i0.. of A and j0.. of B over k in [kb, ke), kb a multiple of 64.  (Several planes: one pair, and operands
     // with k contiguous are zero behind ke up to a multiple of 32.)  mask (MASKED): bit k & 63
     // of word k >> 6 is set where A's row k counts.  Ends with every load landed and all waves past their last LDS read.
     __device__ static __forceinline__ void run(const GemmOperand& A, const GemmOperand& B, const GemmPairs& pairs, int i0, int j0, int kb, int ke,

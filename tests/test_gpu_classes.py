@@ -34,8 +34,9 @@ def _inputs(n, c, v, dtype, bias=True, ignored=0.0, seed=0, spread=6.0):
     return x.to(t), w.to(t), (r(v) if bias else None), y.to(torch.int32)
 
 
-def _reference(x, w, b, y, scale=1.0):
-    """Results in 64 bits and how far an element may be off."""
+def _reference(x, w, b, y, scale=1.0, certain=False):
+    """Results in 64 bits and how far an element may be off.  certain: the label's p - 1 as minus the sum of the others, and a loss that
+    is the logarithm of one and their sum, so off by what they are off by."""
     import torch
     low = x.dtype == torch.bfloat16
     v, c = w.shape
@@ -59,6 +60,12 @@ def _reference(x, w, b, y, scale=1.0):
     out = {"loss": (rows.sum()[None] / count, trows.sum()[None] / count + 4 * U32 * rows.sum()[None] / count), "row_loss": (rows, trows), "lse": (lse, tlse)}
     p = torch.exp(l - lse[:, None]) * valid[:, None]
     tp = p * (tl + tlse[:, None] + 8 * U32 * (l.abs() + lse.abs()[:, None]))
+    if certain:
+        others = tp.scatter(1, at, 0.0).sum(1, keepdim=True)
+        tp = tp.scatter(1, at, others)
+        trows = others[:, 0] + 8 * U32 * rows
+        out["row_loss"] = (rows, trows)
+        out["loss"] = (rows.sum()[None] / count, trows.sum()[None] / count + 4 * U32 * rows.sum()[None] / count)
     d = p.scatter_add(1, at, -valid.double()[:, None])
     g = abs(scale) / count
     part = 2.0 ** -16 if low else 4 * U32
@@ -236,6 +243,37 @@ def test_classes_switched_off(n, v):
     # every class off: the formula has no value, in that row alone there is none here (its bias is every row's, so all rows)
     got = _run(x, w, torch.full_like(b, float("-inf")), y)
     assert bool(got["lse"].eq(float("-inf")).all()) and bool(got["row_loss"].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,v", [(1, 64, 10), (3, 300, 90), (1, 2026, 234), (20, 1500, 700), (32, 2000, 2048)])
+def test_nearly_certain_rows(n, c, v, dtype):
+    """Few rows, each all but certain: loss and gradients keep their digits."""
+    x, w, b, y = _inputs(n, c, v, dtype, bias=False, seed=8)
+    x = (x.float() + 16 * w.float()[y.long()]).to(x.dtype)
+    want = _reference(x, w, None, y, certain=True)
+    assert float(want["row_loss"][0].max()) < 0.05
+    _compare(_run(x, w, None, y), want, f"nearly certain {n} x {c} -> {v} {dtype}")
+
+
+@pytest.mark.parametrize("dtype,n,c,v", [("f32", 12, 32, 40), ("f32", 64, 512, 1000), ("f32", 300, 32, 9000), ("bf16", 300, 32, 9000), ("bf16", 64, 2048, 1000)])
+def test_own_class_at_the_lowest_value(dtype, n, c, v):
+    """A row whose own class has the type's lowest value as its bias: that is its loss, finite (half a rounding of it, and the logit
+    is lost in it); everything else is what a bias of minus infinity gives."""
+    import torch
+    x, w, b, y = _inputs(n, c, v, dtype, seed=6)
+    y = torch.where(y == 3, 4, y).to(torch.int32)
+    y[0] = 3
+    lowest = torch.finfo(torch.float32).min
+    low, out = b.clone(), b.clone()
+    low[3], out[3] = lowest, float("-inf")
+    got, want = _run(x, w, low, y), _run(x, w, out, y)
+    assert abs(float(got["row_loss"][0]) / -lowest - 1.0) <= 4 * U32
+    assert abs(float(got["loss"][0]) * n / -lowest - 1.0) <= 8 * U32
+    assert float(want["row_loss"][0]) == float("inf")
+    assert torch.equal(got["row_loss"][1:], want["row_loss"][1:])
+    for k in ("lse", "dfeatures", "dweight", "dbias"):
+        assert torch.equal(got[k], want[k]) and bool(got[k].isfinite().all()), k
 
 
 @pytest.mark.parametrize("n,c,v", [(64, 48, 300), (700, 64, 9000)])
