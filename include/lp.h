@@ -320,10 +320,11 @@ typedef struct {
     int rows, cols;              /* >= 1, as lp_matrix where orthogonal; rows * cols elements */
     int dtype;                   /* lp_dtype of the parameter */
     int orthogonal;
-    size_t offset;               /* byte offset in params, a multiple of the element size */
-    size_t grad_offset;          /* byte offset in grads, velocity and master, a multiple of 4 */
+    size_t offset;               /* byte offset in params, a multiple of the element size, at most 2^48 */
+    size_t grad_offset;          /* byte offset in grads, velocity and master, a multiple of 4, at most 2^48 */
 } lp_muon_tensor;
-/* A packed set of tensors: params, grads, velocity and master 16-byte aligned.  No two tensors may share elements. */
+/* A packed set of tensors: params, grads, velocity and master 16-byte aligned.  No two tensors may share elements: the workspace
+ * query refuses a set in which they do (LP_ERR_INVALID_ARG), the update itself does not look. */
 lp_status lp_muon_step_workspace_bytes(int n, const lp_muon_tensor* tensors, size_t* bytes);
 lp_status lp_muon_step(void* stream, int n, const lp_muon_tensor* tensors, void* params, const float* grads, float* velocity,
                        float* master, const lp_muon_opts* opts, void* workspace, size_t workspace_bytes);

@@ -3707,12 +3707,30 @@ static void muon_rates(const lp_muon_opts* opts, OrthoPlan& o) {
     o.shrink = (float)(1.0 - (double)opts->lr * opts->weight_decay);
 }
 
+// two tensors of a packed set share elements (their offsets are in order)
+static bool muon_shared(int n, const lp_muon_tensor* t) {
+    std::vector<std::pair<size_t, size_t>> in(n), gr(n);
+    for (int i = 0; i < n; ++i) {
+        const size_t numel = (size_t)t[i].rows * t[i].cols;
+        in[i] = {t[i].offset, t[i].offset + numel * (t[i].dtype == LP_BF16 ? 2 : 4)};
+        gr[i] = {t[i].grad_offset, t[i].grad_offset + numel * 4};
+    }
+    for (auto* v : {&in, &gr}) {
+        std::sort(v->begin(), v->end());
+        for (int i = 1; i < n; ++i)
+            if ((*v)[i].first < (*v)[i - 1].second) return true;
+    }
+    return false;
+}
+
 static lp_status muon_tensors(int n, const lp_muon_tensor* t, void* params, const float* grads, float* velocity, float* master, const lp_muon_opts* opts, OrthoPlan& o) {
     if (n < 0 || n > LP_ORTHO_MAX_MATRICES || (n > 0 && !t)) return fail(LP_ERR_INVALID_ARG, "%d tensors, or their list is NULL", n);
     muon_rates(opts, o);
     o.sets.push_back(OrthoSet{{params, grads, velocity, master}});
     for (int i = 0; i < n; ++i) {
         if (t[i].offset % (t[i].dtype == LP_BF16 ? 2 : 4) || t[i].grad_offset % 4) return fail(LP_ERR_INVALID_ARG, "tensor %d: misaligned offset", i);
+        // (a negative offset that wrapped round: no buffer is that large)
+        if (t[i].offset > ((size_t)1 << 48) || t[i].grad_offset > ((size_t)1 << 48)) return fail(LP_ERR_INVALID_ARG, "tensor %d: offset %zu or %zu", i, t[i].offset, t[i].grad_offset);
         const lp_status st = muon_tensor(t[i].rows, t[i].cols, t[i].dtype, t[i].orthogonal, 0, t[i].offset, t[i].grad_offset, o);
         if (st != LP_OK) return st;
     }
@@ -3781,8 +3799,10 @@ lp_status lp_muon_step_workspace_bytes(int n, const lp_muon_tensor* tensors, siz
     return guarded([&] {
         OrthoPlan o;
         const lp_status st = muon_tensors(n, tensors, nullptr, nullptr, nullptr, nullptr, nullptr, o);
-        if (st == LP_OK) *bytes = o.bytes;
-        return st;
+        if (st != LP_OK) return st;
+        if (muon_shared(n, tensors)) return fail(LP_ERR_INVALID_ARG, "two tensors share elements");
+        *bytes = o.bytes;
+        return LP_OK;
     });
 }
 

@@ -13,6 +13,7 @@ import torch
 from . import binding as B
 
 _DTYPES = {torch.float32: B.LP_F32, torch.bfloat16: B.LP_BF16}
+_INT_MAX = 2 ** 31 - 1          # sizes are ints of the C ABI, which would take a larger one for another
 
 
 def _device(*tensors):
@@ -148,8 +149,10 @@ def _muon_table(table):
     for i, (shape, dtype, orthogonal, offset, grad_offset) in enumerate(table):
         n = math.prod(shape)
         rows = shape[0] if len(shape) > 1 else 1
-        if dtype not in ("f32", "bf16") or n < 1:
+        if dtype not in ("f32", "bf16") or n < 1 or max(rows, n // rows) > _INT_MAX:
             raise ValueError(f"tensor {i}: {dtype} {shape}")
+        if offset < 0 or grad_offset < 0:
+            raise ValueError(f"tensor {i}: offset {offset} or {grad_offset} in front of its buffer")
         arr[i] = B.lp_muon_tensor(rows, n // rows, B.LP_BF16 if dtype == "bf16" else B.LP_F32, int(orthogonal), offset, grad_offset)
         end, gend = max(end, offset + n * (2 if dtype == "bf16" else 4)), max(gend, grad_offset + 4 * n)
     return arr, B.lp_muon_step_workspace_bytes(arr), end, gend
@@ -160,7 +163,7 @@ def muon_update(table, params, grads, velocity, master=None, *, lr, momentum=0.9
 
     table: a tuple of (shape, "f32" or "bf16", orthogonal, byte offset in params, byte offset in the fp32 buffers), the layout
     lp_net_tensor_info describes; a tensor of several dimensions is read as a matrix of shape[0] rows.  params: uint8; grads,
-    velocity, master: float32, one-dimensional, contiguous.  rest_lr (default lr): learning rate of the tensors that are not
+    velocity, master: float32, one-dimensional, contiguous.  No two tensors may share elements.  rest_lr (default lr): learning rate of the tensors that are not
     orthogonalised."""
     arr, size, end, gend = _muon_table(tuple(table))
     dev = _device(params, grads, velocity, master)
