@@ -366,9 +366,9 @@ lp_status lp_net_set_fused_update(struct lp_net* net, int on, float lr, float mo
  * bf16, the probabilities are held as a sum of two bf16 for dweight and as one for dfeatures.  LP_F32: all fp32, products from
  * operands split into three bf16.  Results do not depend on the order in which workgroups run: the same bits on every call. */
 typedef struct {
-    int rows;              /* >= 0 */
+    int rows;              /* 0 .. 2^26 - 4 */
     int channels;          /* 1 .. 65536 */
-    int classes;           /* 1 .. 2^24 */
+    int classes;           /* 1 .. 2^24; the three together: what the launches of a call can hold (LP_ERR_SHAPE otherwise) */
     int dtype;             /* lp_dtype of features, weight and dfeatures */
     int64_t ld_features;   /* elements from a row to the next; 0: channels */
     int64_t ld_weight;

@@ -3190,6 +3190,9 @@ lp_status lp_sgd_update(struct lp_net* net, void* stream, int aux, uint32_t mask
 // ----------------------------------------------------------------------------------------------------
 namespace {
 
+// a launch has fewer than 2^32 threads
+static bool launchable(size_t blocks, int threads) { return blocks * threads < ((size_t)1 << 32); }
+
 // How a product of I x J outputs over K (pairs of planes included) is cut into workgroups.
 struct TilePlan { int cfg, ti, tj, slices, kchunk; };
 
@@ -3279,7 +3282,6 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     // its other probabilities (1 x 2026 -> 234 with a loss of 0.003, dW off by 4e-4 by tiles, which have only its lse in fp32).
     p.cut = (cut + 8.0 < whole || (N1 <= 32 && p.V <= 2048)) && (size_t)tc.slices * N1 * p.V <= ((size_t)8 << 20);
     if (p.cut) p.tl = tc;
-    if ((long)p.tl.ti * p.tl.tj > (1l << 30)) return fail(LP_ERR_SHAPE, "%d rows x %d classes in one call", p.N, p.V);
     int bi, bj, wi, wj;
     ce_tile_size(p.tl.cfg, &bi, &bj, &wi, &wj);
     p.parts = p.tl.ti * wi;
@@ -3296,6 +3298,15 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
         p.ldv = div_up(p.piece, round) * round;
     }
     p.ldp = low ? p.ldv : 3 * p.ldv;
+    if (backward) {
+        p.tx = best_plan(p.C, N1, p.piece, nl, all | few, true);
+        p.tw = best_plan(p.C, p.piece, N1, nw, all, true);
+    }
+    // workgroups of the products (512 threads; one more beside the probabilities) and of a row's end (256)
+    auto tiles = [](const TilePlan& t) { return (size_t)t.ti * t.tj; };
+    if (!launchable((size_t)div_up(p.piece, bi) * p.tl.tj + 1, 512) || !launchable(p.cut || p.N < 2048 ? N1 + 1 : (N1 + 3) / 4, 256) ||
+        (backward && (!launchable(tiles(p.tx), 512) || !launchable(tiles(p.tw), 512))))
+        return fail(LP_ERR_SHAPE, "%d rows, %d channels, %d classes in one call: more workgroups than a launch can have", p.N, p.C, p.V);
     WsAlloc ws;
     const size_t plane_rows = (size_t)p.nplanes * 2 * p.width;
     p.o_x = p.pack_x ? ws.take(plane_rows * N) : 0;
@@ -3307,8 +3318,6 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
         p.o_bcnt = ws.take(N * 4);
         p.o_ticket = ws.take(4);
     } else {
-        p.tx = best_plan(p.C, N1, p.piece, nl, all | few, true);
-        p.tw = best_plan(p.C, p.piece, N1, nw, all, true);
         p.o_mask = ws.take((N + 63) / 64 * 8);
         p.o_count = ws.take(4);
         p.o_prob = ws.take((size_t)p.nprob * 2 * N * p.ldv);
@@ -3576,7 +3585,7 @@ static lp_status ortho_plan(OrthoPlan& o) {
         for (int k = 0; k < kNsLaunches; ++k) { o.start[k][i] = (int)total[k]; total[k] += here[k]; }
     }
     for (int k = 0; k < kNsLaunches; ++k) {
-        if (total[k] > (1l << 30)) return fail(LP_ERR_SHAPE, "too many elements in one call");
+        if (!launchable((size_t)total[k], k == 1 || k == 2 ? 256 : 512)) return fail(LP_ERR_SHAPE, "too many elements in one call");
         o.start[k][n] = (int)total[k];
     }
     o.o_norm = ws.take((size_t)total[1] * sizeof(double));

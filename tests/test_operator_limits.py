@@ -48,3 +48,24 @@ def test_packed_tensors_beyond_the_integers():
         with pytest.raises(ValueError, match="tensor 0"):
             ops._muon_table(((shape, "f32", False, 0, 0),))
     assert ops._muon_table((((1, (1 << 31) - 1), "f32", False, 0, 0),))[2] == 4 * ((1 << 31) - 1)
+
+
+def test_classifier_launches():
+    """A launch has fewer than 2^32 threads: the workspace query says so, not the launch behind the first kernels."""
+    d = lambda n, c, v, t=B.LP_BF16: B.lp_linear_ce_desc(n, c, v, t, 0, 0, 0)
+    _refused(B.LP_ERR_SHAPE, lambda: B.lp_linear_ce_workspace_bytes(d(65536, 64, 1 << 24), False))      # 2^24 tiles of 512 threads
+    assert B.lp_linear_ce_workspace_bytes(d(65536, 64, 1 << 24), True) > 0                              # piece by piece
+    assert B.lp_linear_ce_workspace_bytes(d(65536, 64, 1 << 22), False) > 0
+    for backward in (False, True):
+        _refused(B.LP_ERR_SHAPE, lambda: B.lp_linear_ce_workspace_bytes(d(1 << 26, 8, 4), backward))    # 2^24 workgroups of 256 for the rows
+        assert B.lp_linear_ce_workspace_bytes(d((1 << 26) - 4, 8, 4), backward) > 0
+    _refused(B.LP_ERR_SHAPE, lambda: B.lp_linear_ce_workspace_bytes(d(1 << 25, 65536, 4), True))        # dfeatures: 2^25 tiles and more
+
+
+def test_orthogonalisation_launches():
+    mats = lambda n, r, c: (B.lp_matrix * n)(*[B.lp_matrix(r, c, B.LP_F32, B.LP_F32, 0x10000000, 0x10000000, 0, 0) for _ in range(n)])
+    assert B.lp_orthogonalize_workspace_bytes(mats(3, 1 << 20, 16384)) > 0
+    _refused(B.LP_ERR_SHAPE, lambda: B.lp_orthogonalize_workspace_bytes(mats(4, 1 << 20, 16384)))       # 2^24 pieces, 256 threads each
+    plain = lambda rows, cols: B.lp_muon_step_workspace_bytes(_tensors((rows, cols, B.LP_F32, 0, 0, 0)))
+    assert plain((1 << 20) - 1, 1 << 15) > 0
+    _refused(B.LP_ERR_SHAPE, lambda: plain(1 << 20, 1 << 15))                                           # 2^23 pieces of 4096 elements, 512 threads each
