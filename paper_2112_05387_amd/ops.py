@@ -45,10 +45,8 @@ def _ce_workspace(rows, channels, classes, dtype, ld_features, ld_weight, backwa
     return B.lp_linear_ce_workspace_bytes(B.lp_linear_ce_desc(rows, channels, classes, dtype, ld_features, ld_weight, 0), backward)
 
 
-def _rows(t, name):
+def _rows(t):
     """A matrix whose rows lie as the library reads them: consecutive elements, any row stride, 16-byte aligned."""
-    if t.dim() != 2:
-        raise ValueError(f"{name}: expected a matrix, got {tuple(t.shape)}")
     if t.shape[0] and t.shape[1] and (t.data_ptr() % 16 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
         return t.clone(memory_format=torch.contiguous_format)
     return t
@@ -62,15 +60,19 @@ def _ce_args(features, weight, labels, bias):
     dev = _device(features, weight, labels, bias)
     if features.dtype not in _DTYPES or weight.dtype != features.dtype:
         raise ValueError(f"features {features.dtype} and weight {weight.dtype}: both float32 or both bfloat16")
-    features, weight = _rows(features, "features"), _rows(weight, "weight")
+    if features.dim() != 2 or weight.dim() != 2:
+        raise ValueError(f"features {tuple(features.shape)} and weight {tuple(weight.shape)}: expected matrices")
     n, c = features.shape
     v = weight.shape[0]
+    if max(n, c, v) > _INT_MAX:
+        raise ValueError(f"features {tuple(features.shape)} and weight {tuple(weight.shape)}: more rows or columns than an int holds")
     if weight.shape[1] != c:
         raise ValueError(f"features {tuple(features.shape)} and weight {tuple(weight.shape)} do not fit")
     if labels.shape != (n,) or labels.dtype != torch.int32:
         raise ValueError(f"labels: expected int32 [{n}], got {labels.dtype} {tuple(labels.shape)}")
     if bias is not None and (bias.shape != (v,) or bias.dtype != torch.float32):
         raise ValueError(f"bias: expected float32 [{v}], got {bias.dtype} {tuple(bias.shape)}")
+    features, weight = _rows(features), _rows(weight)
     d = B.lp_linear_ce_desc(n, c, v, _DTYPES[features.dtype], _ld(features), _ld(weight), 0)
     return dev, d, features, weight, labels.contiguous(), None if bias is None else bias.contiguous()
 
@@ -124,8 +126,8 @@ def orthogonalize(matrices, steps=5, out_dtype=None):
     outs, keep = [], []
     for i, m in enumerate(matrices):
         o = out_dtype or m.dtype
-        if m.dim() != 2 or m.dtype not in _DTYPES or o not in _DTYPES:
-            raise ValueError(f"matrix {i}: expected a float32 or bfloat16 matrix, got {m.dtype} {tuple(m.shape)}, result {o}")
+        if m.dim() != 2 or m.dtype not in _DTYPES or o not in _DTYPES or max(m.shape) > _INT_MAX:
+            raise ValueError(f"matrix {i}: expected a float32 or bfloat16 matrix of at most 2^20 rows and columns, got {m.dtype} {tuple(m.shape)}, result {o}")
         if m.numel() and ((m.shape[1] > 1 and m.stride(1) != 1) or (m.shape[0] > 1 and m.stride(0) < m.shape[1])):
             m = m.clone(memory_format=torch.contiguous_format)
             keep.append(m)

@@ -69,3 +69,19 @@ def test_orthogonalisation_launches():
     plain = lambda rows, cols: B.lp_muon_step_workspace_bytes(_tensors((rows, cols, B.LP_F32, 0, 0, 0)))
     assert plain((1 << 20) - 1, 1 << 15) > 0
     _refused(B.LP_ERR_SHAPE, lambda: plain(1 << 20, 1 << 15))                                           # 2^23 pieces of 4096 elements, 512 threads each
+
+
+def test_matrices_beyond_the_integers(monkeypatch):
+    """2^32 + 4 rows are not 4 rows."""
+    import torch
+    monkeypatch.setattr(ops, "_device", lambda *t: torch.device("cuda", 0))
+    many = (1 << 32) + 4
+    meta = lambda *s, t=torch.float32: torch.empty(s, dtype=t, device="meta")
+    for n, v in ((many, 10), (4, many)):
+        with pytest.raises(ValueError, match="rows"):
+            ops.linear_ce_forward(meta(n, 8), meta(v, 8), meta(n, t=torch.int32))
+        with pytest.raises(ValueError, match="rows"):
+            ops.linear_ce_backward(meta(n, 8), meta(v, 8), meta(n, t=torch.int32), meta(n))
+    for shape in ((many, 4), (4, many)):
+        with pytest.raises(ValueError, match="matrix 0"):
+            ops.orthogonalize([meta(*shape)])
