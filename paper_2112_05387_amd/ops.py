@@ -3,6 +3,9 @@
 Every call enqueues its work on the current stream of the tensors' device and returns; outputs and workspaces come from
 torch's allocator on that stream, so calls on several streams, and calls captured into HIP graphs, do not share any.  As with
 any torch operator, a tensor that another stream produced has to be waited for by the caller.
+
+Nothing here records a graph: the gradients are a call of their own (linear_ce_backward), and the update works in place.  So tensors
+that require a gradient are refused unless autograd is off (torch.no_grad), as their results would be cut off from them unseen.
 """
 import contextlib
 import functools
@@ -21,6 +24,8 @@ def _device(*tensors):
     for t in tensors:
         if t is None:
             continue
+        if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError("a tensor requires a gradient, and no graph is recorded here: call under torch.no_grad()")
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise ValueError("expected tensors on the GPU (there is no CPU fallback)")
         if dev is None:
