@@ -20,12 +20,12 @@ _INT_MAX = 2 ** 31 - 1          # sizes are ints of the C ABI, which would take 
 
 
 def _device(*tensors):
+    if torch.is_grad_enabled() and any(t.requires_grad for t in tensors if isinstance(t, torch.Tensor)):
+        raise ValueError("a tensor requires a gradient, and no graph is recorded here: call under torch.no_grad()")
     dev = None
     for t in tensors:
         if t is None:
             continue
-        if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
-            raise ValueError("a tensor requires a gradient, and no graph is recorded here: call under torch.no_grad()")
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise ValueError("expected tensors on the GPU (there is no CPU fallback)")
         if dev is None:
@@ -61,8 +61,8 @@ def _ld(t):
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def _ce_args(features, weight, labels, bias):
-    dev = _device(features, weight, labels, bias)
+def _ce_args(features, weight, labels, bias, lse=None):
+    dev = _device(features, weight, labels, bias, lse)
     if features.dtype not in _DTYPES or weight.dtype != features.dtype:
         raise ValueError(f"features {features.dtype} and weight {weight.dtype}: both float32 or both bfloat16")
     if features.dim() != 2 or weight.dim() != 2:
@@ -106,8 +106,7 @@ def linear_ce_forward(features, weight, labels, bias=None):
 def linear_ce_backward(features, weight, labels, lse, bias=None, scale=1.0):
     """Gradients of scale * loss (lp_linear_ce_backward), from lse as linear_ce_forward returned it for the same operands:
     (dfeatures [N, C] in the type of features, dweight [V, C] float32, dbias [V] float32 or None without a bias)."""
-    dev, d, features, weight, labels, bias = _ce_args(features, weight, labels, bias)
-    _device(features, lse)
+    dev, d, features, weight, labels, bias = _ce_args(features, weight, labels, bias, lse)
     if lse.shape != (d.rows,) or lse.dtype != torch.float32:
         raise ValueError(f"lse: expected float32 [{d.rows}], got {lse.dtype} {tuple(lse.shape)}")
     lse = lse.contiguous()
