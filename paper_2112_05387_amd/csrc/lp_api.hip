@@ -3268,9 +3268,9 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     auto direct = [&](long ld) { return low && p.C % 8 == 0 && ld % 8 == 0 && ld <= (1l << 20); };
     p.pack_x = !direct(p.ldx); p.pack_w = !direct(p.ldw);
     p.width = low ? p.K : (p.C + 31) & ~31;
-    p.logits = GemmPairs{1, 0, 0}; p.dx = p.logits; p.dw = low ? GemmPairs{2, 0, 0x10} : p.logits;
+    p.logits = GemmPairs{1, 0, 0}; p.dx = p.dw = low ? GemmPairs{2, 0, 0x10} : p.logits;
     // k-tiles of 64 k: three planes lie beside each other, 32 k a tile
-    const int nl = low ? 1 : 2, nw = 2;
+    const int nl = low ? 1 : 2, ng = 2;
     const unsigned all = low ? 7u : 48u, few = low && p.N <= 32 ? 8u : 0u, small = low ? 4u : 32u;
 
     // logits: by tiles that finish their rows, or cut along the channels, with the softmax as a pass of its own
@@ -3299,8 +3299,8 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     }
     p.ldp = low ? p.ldv : 3 * p.ldv;
     if (backward) {
-        p.tx = best_plan(p.C, N1, p.piece, nl, all | few, true);
-        p.tw = best_plan(p.C, p.piece, N1, nw, all, true);
+        p.tx = best_plan(p.C, N1, p.piece, ng, all | few, true);
+        p.tw = best_plan(p.C, p.piece, N1, ng, all, true);
     }
     // workgroups of the products (512 threads; one more beside the probabilities) and of a row's end (256)
     auto tiles = [](const TilePlan& t) { return (size_t)t.ti * t.tj; };

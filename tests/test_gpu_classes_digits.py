@@ -1,0 +1,38 @@
+"""Cross-entropy of a linear classifier where digits are easily lost: gradients in bf16 whose sums cancel, probabilities that have to be held to
+fp32's 24 bits, rows that are all but certain, classes at the type's lowest value, pieces of the classes, differences of the loss.
+
+Tolerances as in test_gpu_classes; where they are tighter the arithmetic stands with the test."""
+import math
+
+import pytest
+
+from tests.gpu_common import say
+from tests.test_gpu_classes import U32, _compare, _inputs, _reference, _run, _steps
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n,c,v", [(700, 16, 9000), (64, 512, 1000), (3000, 40, 60), (5, 64, 20000), (2000, 136, 300)])
+def test_what_all_classes_have_in_common(n, c, v):
+    """sum_v d_nv is zero, so what the rows of the weights have in common does not reach the gradient of the features.  A channel that is zero in
+    all features and 64 in all weights: its logits are untouched, its gradient is 64 times the sum of d, off by what d is off by: the
+    error of p (logits and lse) and 2^-16 of |d| for what is held of it; the features are small, so that the logits are exact
+    to far less than bf16's 2^-9."""
+    import torch
+    x, w, b, y = _inputs(n, c, v, "bf16", seed=21)
+    x = (x.float() / 16).bfloat16()
+    x[:, 0] = 0
+    w[:, 0] = 64
+    got = _run(x, w, b, y, scale=float(n))["dfeatures"][:, 0].double()
+    l = x.double() @ w.double().t() + b.double()
+    # the channel of zeros adds nothing to any rounding
+    tl = _steps(c) * (x.double().abs() @ w.double().abs().t() + b.double().abs()) + 4 * U32 * l.abs()
+    lse = l.logsumexp(1, keepdim=True)
+    p = torch.exp(l - lse)
+    tp = p * (tl + tl.max(1, keepdim=True).values + 8 * U32 * (2 * lse.abs() + l.abs() + 1))
+    d = p.scatter_add(1, y.long()[:, None], torch.full((n, 1), -1.0, dtype=torch.float64, device="cuda"))
+    tol = 64 * ((tp + 2.0 ** -16 * d.abs()).sum(1) + 2 * _steps(v) * d.abs().sum(1))
+    exact = 64 * d.sum(1)
+    worst = float(((got - exact).abs() / tol).max())
+    say(f"{n} x {c} -> {v}: largest share of the tolerance {worst:.2f}")
+    assert worst <= 1.0
