@@ -363,7 +363,7 @@ lp_status lp_net_set_fused_update(struct lp_net* net, int on, float lr, float mo
  * A row counts when its label is in [0, classes); any other label (-1, say) leaves it out: row_loss 0, gradient 0, and
  * nothing of what its features hold reaches a sum (its lse is still written).  A class is switched off by a bias of minus infinity.
  * Sums, statistics, loss and the gradients of weight and bias are fp32.  LP_BF16: features, weight and dfeatures are
- * bf16, the probabilities are held as a sum of two bf16.  LP_F32: all fp32, products from
+ * bf16, the probabilities are held as a sum of three bf16, of which dfeatures reads two.  LP_F32: all fp32, products from
  * operands split into three bf16.  Results do not depend on the order in which workgroups run: the same bits on every call. */
 typedef struct {
     int rows;              /* 0 .. 2^26 - 4 */

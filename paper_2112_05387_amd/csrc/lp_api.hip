@@ -3229,7 +3229,7 @@ static TilePlan best_plan(int I, int J, int K, int pairs, unsigned tiles, bool m
 }
 
 struct CePlan {
-    int N, C, V, K, nplanes, nprob;          // K: channels rounded up to eight; planes of the operands, of the probabilities
+    int N, C, V, K, nplanes;                 // K: channels rounded up to eight; planes of the operands: one, or three beside each other
     bool pack_x, pack_w, cut;                // cut: partial logits instead of tiles that finish their rows
     long ldx, ldw, lddx;
     GemmPairs logits, dx, dw;
@@ -3241,7 +3241,8 @@ struct CePlan {
     int direct;                              // waves a row of the kernels for small problems, or 0
 };
 
-constexpr size_t kProbBytes = (size_t)512 << 20;
+// what the probabilities of a piece of the classes may take (or 256 classes), and bytes of one of them: three bf16
+constexpr size_t kProbBytes = (size_t)512 << 20, kProbSize = 6;
 
 static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     if (!d) return fail(LP_ERR_INVALID_ARG, "descriptor is NULL");
@@ -3263,14 +3264,15 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
         return LP_OK;
     }
     const bool low = d->dtype == LP_BF16;
-    p.nplanes = low ? 1 : 3; p.nprob = low ? 2 : 3;
+    p.nplanes = low ? 1 : 3;
     // bf16 rows of whole 16-byte vectors are read where they are (the strides of a tile's rows within 32 bits)
     auto direct = [&](long ld) { return low && p.C % 8 == 0 && ld % 8 == 0 && ld <= (1l << 20); };
     p.pack_x = !direct(p.ldx); p.pack_w = !direct(p.ldw);
     p.width = low ? p.K : (p.C + 31) & ~31;
-    p.logits = GemmPairs{1, 0, 0}; p.dx = p.dw = low ? GemmPairs{2, 0, 0x10} : p.logits;
+    // bf16: parts of the probabilities that a gradient reads, the smallest first
+    p.logits = GemmPairs{1, 0, 0}; p.dx = low ? GemmPairs{2, 0, 0x01} : p.logits; p.dw = low ? GemmPairs{3, 0, 0x012} : p.logits;
     // k-tiles of 64 k: three planes lie beside each other, 32 k a tile
-    const int nl = low ? 1 : 2, ng = 2;
+    const int nl = low ? 1 : 2, nx = 2, nw = low ? 3 : 2;
     const unsigned all = low ? 7u : 48u, few = low && p.N <= 32 ? 8u : 0u, small = low ? 4u : 32u;
 
     // logits: by tiles that finish their rows, or cut along the channels, with the softmax as a pass of its own
@@ -3290,8 +3292,8 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     const size_t N = p.N, V8 = (size_t)div_up(p.V, round) * round;
     p.pieces = 1; p.piece = p.V; p.ldv = (int)V8;
     // (the rows of a tile within 32 bits: at most 2^20 classes a piece)
-    if (backward && !p.cut && ((size_t)p.nprob * 2 * N * V8 > kProbBytes || p.V > (1 << 20))) {
-        p.piece = (int)std::min<size_t>(1 << 20, std::max<size_t>(256, kProbBytes / (p.nprob * 2 * std::max<size_t>(N, 1)) / 256 * 256));
+    if (backward && !p.cut && (kProbSize * N * V8 > kProbBytes || p.V > (1 << 20))) {
+        p.piece = (int)std::min<size_t>(1 << 20, std::max<size_t>(256, kProbBytes / (kProbSize * std::max<size_t>(N, 1)) / 256 * 256));
         p.pieces = div_up(p.V, p.piece);
         p.piece = std::min(p.V, div_up(div_up(p.V, p.pieces), 256) * 256);
         p.pieces = div_up(p.V, p.piece);
@@ -3299,8 +3301,8 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     }
     p.ldp = low ? p.ldv : 3 * p.ldv;
     if (backward) {
-        p.tx = best_plan(p.C, N1, p.piece, ng, all | few, true);
-        p.tw = best_plan(p.C, p.piece, N1, ng, all, true);
+        p.tx = best_plan(p.C, N1, p.piece, nx, all | few, true);
+        p.tw = best_plan(p.C, p.piece, N1, nw, all, true);
     }
     // workgroups of the products (512 threads; one more beside the probabilities) and of a row's end (256)
     auto tiles = [](const TilePlan& t) { return (size_t)t.ti * t.tj; };
@@ -3320,7 +3322,7 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     } else {
         p.o_mask = ws.take((N + 63) / 64 * 8);
         p.o_count = ws.take(4);
-        p.o_prob = ws.take((size_t)p.nprob * 2 * N * p.ldv);
+        p.o_prob = ws.take(kProbSize * N * p.ldv);
         p.o_dx = ws.take((size_t)p.tx.slices * N * p.K * 4);
         p.o_dw = p.tw.slices > 1 ? ws.take((size_t)p.tw.slices * p.piece * p.K * 4) : 0;
         p.o_colsum = p.cut ? 0 : ws.take((size_t)p.colparts * p.ldv * 4);
@@ -3461,7 +3463,7 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
     auto parts_log = [](int slices) { int lg = 0; while (lg < 6 && (8 << lg) < slices) ++lg; return lg; };
     f.labels = labels; f.count = count; f.scale = loss_scale; f.N = p.N; f.V_all = p.V;
     f.colsum = p.cut ? nullptr : (float*)(ws + p.o_colsum); f.parts = p.colparts; f.ld_colsum = p.ldv;
-    f.prob = (const unsigned short*)prob; f.pplane = pplane; f.nplanes = p.nprob; f.ldp = p.ldp;
+    f.prob = (const unsigned short*)prob; f.pplane = pplane; f.beside = p.nplanes == 3; f.ldp = p.ldp;
     for (int v0 = 0, piece = 0; piece < p.pieces; ++piece, v0 += p.piece) {
         const int V = std::min(p.piece, p.V - v0);
         CeLogits a = ce_logits(p, X, W, bias, v0, V);
@@ -3473,7 +3475,7 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
             r.N = p.N; r.V = p.V; r.labels = labels; r.bias = bias; r.slices = a.slices; r.slice = a.slice; r.nslices = p.tl.slices; r.ldv = a.ldv;
             r.lse = const_cast<float*>(lse); r.mask = mask; r.count = count;
             st = hip_status(launch_ce_slices(a, p.tl.slices, p.tl.cfg, s));
-            if (st == LP_OK) st = hip_status(launch_ce_prob(r, (unsigned short*)prob, pplane, p.ldp, p.nprob, s));
+            if (st == LP_OK) st = hip_status(launch_ce_prob(r, (unsigned short*)prob, pplane, p.ldp, p.nplanes == 3, s));
         } else {
             a.colsum = dbias ? (float*)(ws + p.o_colsum) : nullptr; a.ld_colsum = p.ldv;
             st = hip_status(launch_ce_prob_tiles(a, p.tl.cfg, s));

@@ -23,7 +23,7 @@ struct CeLogits {
     float* slices; size_t slice;        // partial logits: [slices][N][ldv]
     int ldv, ldp;                       // classes of a row of slices / prob, a multiple of 8 (three planes: 32); elements of a row of prob
     const float* lse; const int* labels;
-    char* prob; size_t pplane;          // probabilities: two planes of bf16 [N][ldv], or three beside each other [N][ldp]
+    char* prob; size_t pplane;          // probabilities: three planes of bf16 [N][ldv], or beside each other [N][ldp]
     float* colsum; int ld_colsum;       // their sums over the samples of every wave's tile, or null
 };
 struct CeRows {
@@ -58,7 +58,7 @@ struct CeFinish {
     const int* labels; const int* count; float scale;
     int N, V, V_all;                    // V: classes of the bias here
     const float* colsum; int parts, ld_colsum;
-    const unsigned short* prob; size_t pplane; int nplanes, ldp;
+    const unsigned short* prob; size_t pplane; int beside, ldp;
     float* dbias;
 };
 
@@ -85,7 +85,7 @@ hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s);
 hipError_t launch_ce_prob_tiles(const CeLogits& a, int cfg, hipStream_t s);
 hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t s);
 hipError_t launch_ce_rows(const CeRows& a, hipStream_t s);
-hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int ldp, int planes, hipStream_t s);
+hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int ldp, bool beside, hipStream_t s);
 hipError_t launch_ce_dx(const CeGrad& a, int slices, int cfg, hipStream_t s);
 hipError_t launch_ce_dw(const CeGrad& a, int slices, int cfg, hipStream_t s);
 hipError_t launch_ce_finish(const CeFinish& a, int dtype, hipStream_t s);

@@ -9,10 +9,10 @@
 // probabilities; they go to memory, piece of the classes by piece, and are read from there by the two gradient products.  Keeping
 // the logits would save one product of four and cost 4 bytes a logit.
 //
-// Precision.  bf16: products of bf16 are exact, sums are fp32.  The probabilities are kept as two bf16 (16 bits).  dX reads both, though
-// it is rounded to bf16 itself: sum_v d_nv is zero, so what the rows of W have in common cancels in dX, and with one part of 8
-// bits it does not (64 x 256 -> 4000 with 0.5 added to every weight: 8e-3 off instead of 1.7e-3).  p - 1 of the label is formed in
-// fp32 before it is split, so a small p beside it is kept by the second part.
+// Precision.  bf16: products of bf16 are exact, sums are fp32.  The probabilities are kept as three bf16 (24 bits), all of which dW and
+// the bias read, which are fp32 (with two dW is off by 1.8e-6, with three by the 2e-7 of its sums).  dX, rounded to bf16 itself,
+// reads two: sum_v d_nv is zero, so what the rows of W have in common cancels in dX, and with one part of 8 bits it does not (64 x 256
+// -> 4000 with 0.5 added to every weight: 8e-3 off instead of 1.7e-3).
 // fp32: every operand as three bf16 (24 bits) that lie beside each other, six of the nine products (the others are below 2^-25).
 // 73623 classes x 8716 rows of 633 channels: a product in 4.2 ms, 195 TFLOP/s of fp32; the card's fp32 matrix product reaches 151.
 //
@@ -51,9 +51,9 @@ template <int NP> __device__ __forceinline__ void split_bf16(float x, unsigned (
     }
 }
 
-// Element c of plane k in a row of NP planes: two lie `plane` elements apart, three beside each other, 32 of each in turn
-template <int NP> __device__ __forceinline__ size_t plane_at(int c, int k, size_t plane) {
-    if constexpr (NP == 3) return (size_t)(c >> 5) * 96 + k * 32 + (c & 31);
+// Element c of plane k in a row of three planes: they lie beside each other, 32 of each in turn, or `plane` elements apart
+template <bool BESIDE> __device__ __forceinline__ size_t plane_at(int c, int k, size_t plane) {
+    if constexpr (BESIDE) return (size_t)(c >> 5) * 96 + k * 32 + (c & 31);
     else return k * plane + c;
 }
 
@@ -93,7 +93,7 @@ template <class T, int NP> __global__ __launch_bounds__(256) void ce_pack_kernel
         }
 #pragma unroll
         for (int p = 0; p < NP; ++p)
-            *reinterpret_cast<u32x2*>(dst + (size_t)r * (NP * a.width) + plane_at<NP>(c, p, 0)) = u32x2{out[p][0] | ((unsigned)out[p][1] << 16), out[p][2] | ((unsigned)out[p][3] << 16)};
+            *reinterpret_cast<u32x2*>(dst + (size_t)r * (NP * a.width) + (NP == 3 ? plane_at<true>(c, p, 0) : c)) = u32x2{out[p][0] | ((unsigned)out[p][1] << 16), out[p][2] | ((unsigned)out[p][3] << 16)};
     }
 }
 
@@ -124,7 +124,10 @@ __device__ __forceinline__ void ce_labels(const int* __restrict__ labels, int N,
 // ---------------------------------------------------------------------------------------------------------------------------------
 enum LogitsMode { LM_STATS, LM_PROB, LM_SLICE };
 
-template <class T, int MODE, int NP, int WAVES> __global__ __launch_bounds__(T::NT, WAVES) void ce_logits_kernel(const CeLogits a) {
+// parts of 32 samples' probabilities that fit into LDS for all waves at once
+template <class T> constexpr int prob_parts() { return 3 * T::NW * 32 * (T::TI * 2 + 16) <= 160 * 1024 ? 3 : 2; }
+
+template <class T, int MODE, int WAVES> __global__ __launch_bounds__(T::NT, WAVES) void ce_logits_kernel(const CeLogits a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     if constexpr (MODE == LM_PROB)
         if ((int)blockIdx.x == a.tiles_i * a.tiles_j) { ce_labels(a.labels, a.N, a.V_all, a.mask, a.count, reinterpret_cast<int*>(smem)); return; }
@@ -200,9 +203,11 @@ template <class T, int MODE, int NP, int WAVES> __global__ __launch_bounds__(T::
             if (h == 0 && n < a.N) a.partial[(size_t)n * a.parts + ti * (T::BI / T::TI) + wi] = make_float2(m, t);
         }
     } else {
-        // probabilities: 32 samples of the wave at a time through LDS, from where they go out as 16-byte pieces of rows
-        constexpr int PITCH = T::TI * 2 + 16, EP = 32 * PITCH, CPR = T::TI / 8, RPL = 64 / CPR;
-        unsigned char* const E0 = smem + wave * (NP * EP);
+        // probabilities: 32 samples of the wave at a time through LDS, from where they go out as 16-byte pieces of rows; as many of
+        // their parts at once as LDS holds, what is left of a probability stays in its accumulator
+        constexpr int NP = 3, PITCH = T::TI * 2 + 16, EP = 32 * PITCH, CPR = T::TI / 8, RPL = 64 / CPR, AT_ONCE = prob_parts<T>();
+        constexpr int UNROLL = FI > 2 ? 1 : 8;                     // (256 x 256: the addresses of all rows do not fit into the registers beside the accumulators)
+        unsigned char* const E0 = smem + wave * (AT_ONCE * EP);
         const int c = lane % CPR, jr = lane / CPR;
         float cs[8];
 #pragma unroll
@@ -218,41 +223,51 @@ template <class T, int MODE, int NP, int WAVES> __global__ __launch_bounds__(T::
 #pragma unroll
             for (int i = 0; i < FI; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float p[4];
+                for (int r = 0; r < 16; ++r) {
+                    float p = valid ? __builtin_amdgcn_exp2f(acc[i][j][r] - shift) : 0.f;
+                    if (at == i * 32 + 8 * (r >> 2) + (r & 3)) p -= 1.f;
+                    acc[i][j][r] = p;
+                }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        p[e] = valid ? __builtin_amdgcn_exp2f(acc[i][j][4 * q + e] - shift) : 0.f;
-                        if (at == i * 32 + 8 * q + e) p[e] -= 1.f;
+            for (int k0 = 0; k0 < NP; k0 += AT_ONCE) {
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        unsigned char* const d = E0 + lr * PITCH + (i * 32 + 8 * q + 4 * h) * 2;
+                        float p[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) p[e] = acc[i][j][4 * q + e];
+#pragma unroll
+                        for (int k = k0; k < NP && k < k0 + AT_ONCE; ++k) {
+                            const unsigned lo = pack_bf16x2(p[0], p[1]), hi = pack_bf16x2(p[2], p[3]);
+                            *reinterpret_cast<u32x2*>(d + (k - k0) * EP) = u32x2{lo, hi};
+                            p[0] -= __uint_as_float(lo << 16); p[1] -= __uint_as_float(lo & 0xffff0000u);
+                            p[2] -= __uint_as_float(hi << 16); p[3] -= __uint_as_float(hi & 0xffff0000u);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = p[e];
                     }
-                    unsigned char* const d = E0 + lr * PITCH + (i * 32 + 8 * q + 4 * h) * 2;
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_s_waitcnt(0xc07f);
+                const int v = ib + c * 8;
+#pragma unroll UNROLL
+                for (int t = 0; t < 32 / RPL; ++t) {
+                    const int row = t * RPL + jr, no = jb + j * 32 + row;
 #pragma unroll
-                    for (int k = 0; k < NP; ++k) {
-                        const unsigned lo = pack_bf16x2(p[0], p[1]), hi = pack_bf16x2(p[2], p[3]);
-                        *reinterpret_cast<u32x2*>(d + k * EP) = u32x2{lo, hi};
-                        p[0] -= __uint_as_float(lo << 16); p[1] -= __uint_as_float(lo & 0xffff0000u);
-                        p[2] -= __uint_as_float(hi << 16); p[3] -= __uint_as_float(hi & 0xffff0000u);
+                    for (int k = k0; k < NP && k < k0 + AT_ONCE; ++k) {
+                        const u32x4 w = *reinterpret_cast<const u32x4*>(E0 + (k - k0) * EP + row * PITCH + c * 16);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            cs[2 * e] += __uint_as_float(w[e] << 16);
+                            cs[2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
+                        }
+                        if (no < a.N && v < a.ldv) *reinterpret_cast<u32x4*>(a.prob + ((size_t)no * a.ldp + plane_at<T::TRIPLE>(v, k, a.pplane / 2)) * 2) = w;
                     }
                 }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_s_waitcnt(0xc07f);
-            const int v = ib + c * 8;
-#pragma unroll
-            for (int t = 0; t < 32 / RPL; ++t) {
-                const int row = t * RPL + jr, no = jb + j * 32 + row;
-#pragma unroll
-                for (int k = 0; k < NP; ++k) {
-                    const u32x4 w = *reinterpret_cast<const u32x4*>(E0 + k * EP + row * PITCH + c * 16);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        cs[2 * e] += __uint_as_float(w[e] << 16);
-                        cs[2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
-                    }
-                    if (no < a.N && v < a.ldv) *reinterpret_cast<u32x4*>(a.prob + ((size_t)no * a.ldp + plane_at<NP>(v, k, a.pplane / 2)) * 2) = w;
-                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                __builtin_amdgcn_s_waitcnt(0xc07f);              // read before the next ones overwrite it
             }
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            __builtin_amdgcn_s_waitcnt(0xc07f);                  // read before the next 32 samples overwrite it
         }
         if (a.colsum) {
 #pragma unroll
@@ -282,7 +297,7 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
 
 // eight elements of a row of one plane or of three
 __device__ __forceinline__ void whole_eight(const unsigned short* row, int c, int nplanes, float (&f)[8]) {
-    const unsigned short* const p = nplanes == 3 ? row + plane_at<3>(c, 0, 0) : row + c;
+    const unsigned short* const p = nplanes == 3 ? row + plane_at<true>(c, 0, 0) : row + c;
 #pragma unroll
     for (int k = 0; k < 3; ++k)
         if (k < nplanes) {
@@ -433,7 +448,8 @@ template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_k
 }
 
 // Probabilities from partial logits (few tiles): a workgroup a row
-template <int NP> __global__ __launch_bounds__(256) void ce_prob_kernel(const CeRows a, unsigned short* __restrict__ prob, size_t pplane, int ldp) {
+template <bool BESIDE> __global__ __launch_bounds__(256) void ce_prob_kernel(const CeRows a, unsigned short* __restrict__ prob, size_t pplane, int ldp) {
+    constexpr int NP = 3;
     __shared__ int s_cnt[4];
     const int n = blockIdx.x;
     if (n == a.N) { ce_labels(a.labels, a.N, a.V, a.mask, a.count, s_cnt); return; }
@@ -450,7 +466,7 @@ template <int NP> __global__ __launch_bounds__(256) void ce_prob_kernel(const Ce
 #pragma unroll
         for (int e = 0; e < 2; ++e) split_bf16<NP>(p[e], b[e]);
 #pragma unroll
-        for (int k = 0; k < NP; ++k) *reinterpret_cast<unsigned*>(prob + (size_t)n * ldp + plane_at<NP>(v, k, pplane / 2)) = b[0][k] | (b[1][k] << 16);
+        for (int k = 0; k < NP; ++k) *reinterpret_cast<unsigned*>(prob + (size_t)n * ldp + plane_at<BESIDE>(v, k, pplane / 2)) = b[0][k] | (b[1][k] << 16);
     };
     for (int v = threadIdx.x * 2; v < a.ldv; v += 512) {
         const float2 l = sliced(row + v, a.slice, a.nslices);
@@ -622,8 +638,8 @@ template <class T> __global__ __launch_bounds__(256) void ce_finish_kernel(const
     __shared__ float s_p[4][8];
     const int v0 = (b - a.blocks_x - a.blocks_w) * 8;
     float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < a.nplanes; ++p) {
-        const unsigned short* const q = a.prob + (a.nplanes == 3 ? plane_at<3>(v0, p, 0) : p * (a.pplane / 2) + v0);
+    for (int p = 0; p < 3; ++p) {
+        const unsigned short* const q = a.prob + (a.beside ? plane_at<true>(v0, p, 0) : plane_at<false>(v0, p, a.pplane / 2));
 #pragma unroll 4
         for (int n = threadIdx.x; n < a.N; n += 256) {
             const u32x4 u = *reinterpret_cast<const u32x4*>(q + (size_t)n * a.ldp);
@@ -664,10 +680,10 @@ template <class K, class A> hipError_t launch(K kernel, OncePerDevice& once, dim
     return hipGetLastError();
 }
 
-template <class T, int MODE, int NP, int WAVES> hipError_t launch_logits_t(const CeLogits& a, int slices, hipStream_t s) {
+template <class T, int MODE, int WAVES> hipError_t launch_logits_t(const CeLogits& a, int slices, hipStream_t s) {
     static OncePerDevice once;
-    constexpr int EP = MODE == LM_PROB ? T::NW * NP * 32 * (T::TI * 2 + 16) : 0;
-    return launch(ce_logits_kernel<T, MODE, NP, WAVES>, once, dim3(a.tiles_i * a.tiles_j + (MODE == LM_PROB ? 1 : 0), slices), T::NT, std::max(T::LDS, EP), s, a);
+    constexpr int EP = MODE == LM_PROB ? T::NW * prob_parts<T>() * 32 * (T::TI * 2 + 16) : 0;
+    return launch(ce_logits_kernel<T, MODE, WAVES>, once, dim3(a.tiles_i * a.tiles_j + (MODE == LM_PROB ? 1 : 0), slices), T::NT, std::max(T::LDS, EP), s, a);
 }
 template <class T, int WAVES> hipError_t launch_grad_t(const CeGrad& a, int slices, hipStream_t s) {
     static OncePerDevice once;
@@ -702,29 +718,29 @@ hipError_t launch_ce_pack(CePack x, CePack w, int dtype, hipStream_t s) {
 }
 hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s) {
     switch (cfg) {
-        case 0: return launch_logits_t<TBig<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
-        case 1: return launch_logits_t<TMid<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
-        case 2: return launch_logits_t<TSmall<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
-        case 3: return launch_logits_t<TFew<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
-        case 4: return launch_logits_t<TMid3<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
-        default: return launch_logits_t<TSmall3<false, false, false>, LM_STATS, 1, 2>(a, 1, s);
+        case 0: return launch_logits_t<TBig<false, false, false>, LM_STATS, 2>(a, 1, s);
+        case 1: return launch_logits_t<TMid<false, false, false>, LM_STATS, 2>(a, 1, s);
+        case 2: return launch_logits_t<TSmall<false, false, false>, LM_STATS, 2>(a, 1, s);
+        case 3: return launch_logits_t<TFew<false, false, false>, LM_STATS, 2>(a, 1, s);
+        case 4: return launch_logits_t<TMid3<false, false, false>, LM_STATS, 2>(a, 1, s);
+        default: return launch_logits_t<TSmall3<false, false, false>, LM_STATS, 2>(a, 1, s);
     }
 }
 hipError_t launch_ce_prob_tiles(const CeLogits& a, int cfg, hipStream_t s) {
     switch (cfg) {
-        case 0: return launch_logits_t<TBig<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
-        case 1: return launch_logits_t<TMid<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
-        case 2: return launch_logits_t<TSmall<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
-        case 3: return launch_logits_t<TFew<false, false, false>, LM_PROB, 2, 2>(a, 1, s);
-        case 4: return launch_logits_t<TMid3<false, false, false>, LM_PROB, 3, 2>(a, 1, s);
-        default: return launch_logits_t<TSmall3<false, false, false>, LM_PROB, 3, 2>(a, 1, s);
+        case 0: return launch_logits_t<TBig<false, false, false>, LM_PROB, 2>(a, 1, s);
+        case 1: return launch_logits_t<TMid<false, false, false>, LM_PROB, 2>(a, 1, s);
+        case 2: return launch_logits_t<TSmall<false, false, false>, LM_PROB, 2>(a, 1, s);
+        case 3: return launch_logits_t<TFew<false, false, false>, LM_PROB, 2>(a, 1, s);
+        case 4: return launch_logits_t<TMid3<false, false, false>, LM_PROB, 2>(a, 1, s);
+        default: return launch_logits_t<TSmall3<false, false, false>, LM_PROB, 2>(a, 1, s);
     }
 }
 hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t s) {
     switch (cfg) {
-        case 2: return launch_logits_t<TSmall<false, false, false>, LM_SLICE, 1, 2>(a, slices, s);
-        case 3: return launch_logits_t<TFew<false, false, false>, LM_SLICE, 1, 2>(a, slices, s);
-        default: return launch_logits_t<TSmall3<false, false, false>, LM_SLICE, 1, 2>(a, slices, s);
+        case 2: return launch_logits_t<TSmall<false, false, false>, LM_SLICE, 2>(a, slices, s);
+        case 3: return launch_logits_t<TFew<false, false, false>, LM_SLICE, 2>(a, slices, s);
+        default: return launch_logits_t<TSmall3<false, false, false>, LM_SLICE, 2>(a, slices, s);
     }
 }
 hipError_t launch_ce_rows(const CeRows& a, hipStream_t s) {
@@ -744,9 +760,9 @@ hipError_t launch_ce_total(const float* sums, const int* counts, int n, float* l
     hipLaunchKernelGGL(ce_total_kernel, dim3(1), dim3(256), 0, s, sums, counts, n, loss);
     return hipGetLastError();
 }
-hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int ldp, int planes, hipStream_t s) {
-    if (planes == 2) hipLaunchKernelGGL(ce_prob_kernel<2>, dim3(a.N + 1), dim3(256), 0, s, a, prob, pplane, ldp);
-    else hipLaunchKernelGGL(ce_prob_kernel<3>, dim3(a.N + 1), dim3(256), 0, s, a, prob, pplane, ldp);
+hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int ldp, bool beside, hipStream_t s) {
+    if (!beside) hipLaunchKernelGGL(ce_prob_kernel<false>, dim3(a.N + 1), dim3(256), 0, s, a, prob, pplane, ldp);
+    else hipLaunchKernelGGL(ce_prob_kernel<true>, dim3(a.N + 1), dim3(256), 0, s, a, prob, pplane, ldp);
     return hipGetLastError();
 }
 hipError_t launch_ce_dx(const CeGrad& a, int slices, int cfg, hipStream_t s) {

@@ -36,3 +36,41 @@ def test_what_all_classes_have_in_common(n, c, v):
     worst = float(((got - exact).abs() / tol).max())
     say(f"{n} x {c} -> {v}: largest share of the tolerance {worst:.2f}")
     assert worst <= 1.0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,v", [(256, 300), (64, 20000), (128, 1100), (512, 9000), (1040, 130)])
+def test_probabilities_to_24_bits(n, v, dtype):
+    """Features are the identity and the weights zero: the logits are the bias, and the gradient of the weights is d itself, transposed, every sum
+    of one term.  p = exp(l - lse) from lse in fp32: the difference, its product with log2 e and that constant are off by
+    3 |l - lse| 2^-24, exp2 and the scale by 2^-23 each, the parts in which d is held by 2^-24; p - 1 rounds once more.  The
+    gradient of the bias is summed over four rows that count, three additions and exact zeros."""
+    import torch
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(v)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x = torch.eye(n, device="cuda").to(t)
+    w = torch.zeros(v, n, dtype=t, device="cuda")
+    b = torch.rand(v, generator=gen, device="cuda") - 0.5
+    y = torch.randint(0, v, (n,), generator=gen, device="cuda").to(torch.int32)
+    from paper_2112_05387_amd import ops
+    lse = ops.linear_ce_forward(x, w, y, bias=b)[2]
+    l = b.double().expand(n, v)
+    off = l - lse.double()[:, None]
+    p = off.exp()
+    rel = (3 * off.abs() + 8) * U32
+    for few in (False, True):
+        if few:
+            y = torch.where(torch.arange(n, device="cuda") % (n // 4) == 3, y, -1).to(torch.int32)
+        keep = (y >= 0).double()[:, None]
+        at = y.clamp(min=0).long()[:, None]
+        d = p.scatter_add(1, at, torch.full((n, 1), -1.0, dtype=torch.float64, device="cuda")) * keep
+        tol = (p * rel + 2 * U32 * d.abs()) * keep
+        count = int(keep.sum())
+        _, dw, db = ops.linear_ce_backward(x, w, y, lse, bias=b, scale=float(count))
+        worst = float(((dw.double().t() - d).abs() / (tol + 1e-37)).max())
+        say(f"{n} -> {v} {dtype}, {count} rows: dweight {worst:.2f} of the tolerance")
+        assert worst <= 1.0
+    worst = float(((db.double() - d.sum(0)).abs() / (tol.sum(0) + 4 * U32 * d.abs().sum(0))).max())
+    say(f"{n} -> {v} {dtype}: dbias {worst:.2f} of the tolerance")
+    assert worst <= 1.0
