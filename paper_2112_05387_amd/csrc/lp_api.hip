@@ -3236,7 +3236,7 @@ struct CePlan {
     TilePlan tl, tx, tw;
     int piece, pieces, ldv, ldp;             // classes of a piece of the probabilities; of a row of them, and its elements
     int width;                               // channels of a row of a laid-out operand
-    size_t o_x, o_w, o_partial, o_slices, o_bsum, o_bcnt, o_mask, o_count, o_prob, o_dx, o_dw, o_colsum, o_ticket, bytes;
+    size_t o_x, o_w, o_partial, o_own, o_slices, o_bsum, o_bcnt, o_mask, o_count, o_prob, o_dx, o_dw, o_colsum, o_ticket, bytes;
     int parts, colparts;
     int direct;                              // waves a row of the kernels for small problems, or 0
 };
@@ -3280,9 +3280,9 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     const int N1 = std::max(1, p.N);
     p.tl = best_plan(p.V, N1, p.K, nl, all | few, false, &whole);
     const TilePlan tc = best_plan(p.V, N1, p.K, nl, small | few, true, &cut);
-    // (some 8 us); and so where a few rows have few classes, any of them may be all but certain, and its gradient takes the sum of
-    // its other probabilities (1 x 2026 -> 234 with a loss of 0.003, dW off by 4e-4 by tiles, which have only its lse in fp32).
-    p.cut = (cut + 8.0 < whole || (N1 <= 32 && p.V <= 2048)) && (size_t)tc.slices * N1 * p.V <= ((size_t)8 << 20);
+    // (some 8 us); and so the gradient where a few rows have few classes, any of them may be all but certain, and its gradient takes the sum
+    // of its other probabilities (1 x 2026 -> 234 with a loss of 0.003, dW off by 4e-4 by tiles, which have only its lse in fp32).
+    p.cut = (cut + 8.0 < whole || (backward && N1 <= 32 && p.V <= 2048)) && (size_t)tc.slices * N1 * p.V <= ((size_t)8 << 20);
     if (p.cut) p.tl = tc;
     int bi, bj, wi, wj;
     ce_tile_size(p.tl.cfg, &bi, &bj, &wi, &wj);
@@ -3316,6 +3316,7 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     p.o_slices = p.cut ? ws.take((size_t)p.tl.slices * N * V8 * 4) : 0;
     if (!backward) {
         p.o_partial = p.cut ? 0 : ws.take(N * p.parts * sizeof(float2));
+        p.o_own = p.cut ? 0 : ws.take(N * 4);
         p.o_bsum = ws.take(N * 4);
         p.o_bcnt = ws.take(N * 4);
         p.o_ticket = ws.take(4);
@@ -3414,12 +3415,12 @@ lp_status lp_linear_ce_forward(const lp_linear_ce_desc* d, void* stream, const v
         r.slices = a.slices; r.slice = a.slice; r.nslices = p.tl.slices; r.ldv = a.ldv;
         st = hip_status(launch_ce_slices(a, p.tl.slices, p.tl.cfg, s));
     } else {
-        a.partial = (float2*)(ws + p.o_partial); a.parts = p.parts;
-        r.partial = a.partial; r.parts = p.parts;
+        a.partial = (float2*)(ws + p.o_partial); a.parts = p.parts; a.labels = labels; a.own = (float*)(ws + p.o_own);
+        r.partial = a.partial; r.parts = p.parts; r.own = a.own;
         st = hip_status(launch_ce_stats(a, p.tl.cfg, s));
     }
     if (st != LP_OK) return st;
-    r.N = p.N; r.V = p.V; r.K = p.K; r.labels = labels; r.bias = bias; r.w = W; r.x = X; r.nplanes = p.nplanes;
+    r.N = p.N; r.V = p.V; r.labels = labels; r.bias = bias;
     r.lse = lse; r.row_loss = row_loss; r.loss = loss;
     r.bsum = (float*)(ws + p.o_bsum); r.bcnt = (int*)(ws + p.o_bcnt);
     return hip_status(launch_ce_rows(r, s));

@@ -19,7 +19,8 @@ struct CeLogits {
     const float* bias;                  // of the piece, or null
     unsigned long long* mask; int* count;    // probabilities: which rows count, and how many do, are found beside them
     int* ticket;                        // statistics, partial logits: set to zero for the kernel behind, or null
-    float2* partial; int parts;         // statistics: [N][parts] (maximum, sum), base 2
+    float2* partial; int parts;         // statistics: [N][parts] (maximum, sum) without the label's class
+    float* own;                         // statistics: the label's logit of every row that has one
     float* slices; size_t slice;        // partial logits: [slices][N][ldv]
     int ldv, ldp;                       // classes of a row of slices / prob, a multiple of 8 (three planes: 32); elements of a row of prob
     const float* lse; const int* labels;
@@ -27,12 +28,11 @@ struct CeLogits {
     float* colsum; int ld_colsum;       // their sums over the samples of every wave's tile, or null
 };
 struct CeRows {
-    int N, V, K;
+    int N, V;
     const int* labels;
     const float* bias;
-    const float2* partial; int parts;
+    const float2* partial; int parts; const float* own;
     const float* slices; size_t slice; int nslices, ldv;
-    GemmOperand w, x; int nplanes;
     float *lse, *row_loss, *loss;
     float* bsum; int* bcnt;             // of every workgroup
     int* ticket;                        // workgroups that are done, zero before; or null: somebody else adds up

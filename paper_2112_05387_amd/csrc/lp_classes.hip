@@ -4,8 +4,8 @@
 //   d_nv = (exp(l_nv - lse_n) - [v = y(n)]) / count,   dX = d W,   dW = d^T X,   db_v = sum_n d_nv
 //
 // Four products, each on the matrix cores with what follows it as its epilogue.  Forward: l = X W^T, of which a workgroup keeps the
-// maximum and the sum of exponentials of its classes for every row (the statistics of all tiles are joined by a small kernel that
-// also takes the label's own logit, a dot product).  Backward: the same product once more, whose epilogue turns a tile into
+// maximum and the sum of exponentials of its classes for every row (the statistics of all tiles are joined by a small kernel; the label's
+// class is kept apart until then).  Backward: the same product once more, whose epilogue turns a tile into
 // probabilities; they go to memory, piece of the classes by piece, and are read from there by the two gradient products.  Keeping
 // the logits would save one product of four and cost 4 bytes a logit.
 //
@@ -168,23 +168,34 @@ template <class T, int MODE, int WAVES> __global__ __launch_bounds__(T::NT, WAVE
         }
         return;
     }
-    // to base 2, with the bias; classes beyond the last: minus infinity
+    // with the bias; classes beyond the last: minus infinity
     const bool ragged = i0 + T::BI > a.V;
 #pragma unroll
     for (int i = 0; i < FI; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int v = ib + i * 32 + T::row(r, lane);
-            const float b = a.bias ? a.bias[min(v, a.V - 1)] * kLog2e : 0.f;
+            const float b = a.bias ? a.bias[min(v, a.V - 1)] : 0.f;
 #pragma unroll
             for (int j = 0; j < FJ; ++j) {
-                acc[i][j][r] = fmaf(acc[i][j][r], kLog2e, b);
+                acc[i][j][r] += b;
                 if (ragged && v >= a.V) acc[i][j][r] = -kInf;
             }
         }
     if constexpr (MODE == LM_STATS) {
 #pragma unroll
         for (int j = 0; j < FJ; ++j) {
+            const int n = jb + j * 32 + lr;
+            // the label's logit is handed on and left out here, by the lane that has it (few waves have one): what the other classes
+            // have beside it is then never the difference of two numbers that are nearly one
+            const int y = n < a.N ? a.labels[n] : -1, at = is_class(y, a.V) ? y - ib - 4 * h : -1;
+            if (__any(at >= 0 && at < T::TI)) {
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (at == i * 32 + 8 * (r >> 2) + (r & 3)) { a.own[n] = acc[i][j][r]; acc[i][j][r] = -kInf; }
+            }
             float m = -kInf;
 #pragma unroll
             for (int i = 0; i < FI; ++i)
@@ -196,10 +207,9 @@ template <class T, int MODE, int WAVES> __global__ __launch_bounds__(T::NT, WAVE
 #pragma unroll
             for (int i = 0; i < FI; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r & 3] += __builtin_amdgcn_exp2f(acc[i][j][r] - m0);
+                for (int r = 0; r < 16; ++r) s[r & 3] += __builtin_amdgcn_exp2f((acc[i][j][r] - m0) * kLog2e);
             float t = (s[0] + s[1]) + (s[2] + s[3]);
             t += __shfl_xor(t, 32);
-            const int n = jb + j * 32 + lr;
             if (h == 0 && n < a.N) a.partial[(size_t)n * a.parts + ti * (T::BI / T::TI) + wi] = make_float2(m, t);
         }
     } else {
@@ -217,14 +227,14 @@ template <class T, int MODE, int WAVES> __global__ __launch_bounds__(T::NT, WAVE
             const int n = jb + j * 32 + lr;
             const int y = n < a.N ? a.labels[n] : -1;
             const bool valid = is_class(y, a.V_all);
-            const float shift = n < a.N ? a.lse[n] * kLog2e : 0.f;
+            const float lse = n < a.N ? a.lse[n] : 0.f;
             // the label's class, where this lane has it: its one is taken off before the parts are formed
             const int at = valid ? y - a.v0 - ib - 4 * h : -1;
 #pragma unroll
             for (int i = 0; i < FI; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    float p = valid ? __builtin_amdgcn_exp2f(acc[i][j][r] - shift) : 0.f;
+                    float p = valid ? __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * kLog2e) : 0.f;
                     if (at == i * 32 + 8 * (r >> 2) + (r & 3)) p -= 1.f;
                     acc[i][j][r] = p;
                 }
@@ -285,30 +295,14 @@ template <class T, int MODE, int WAVES> __global__ __launch_bounds__(T::NT, WAVE
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// The end of the forward pass.  (m, s) of the tiles (or the partial logits themselves) to lse, the label's logit, the row's loss and
-// every workgroup's sum of them; a last small kernel (or the only workgroup) adds those up.  WPR waves a row: one, or four where rows
+// The end of the forward pass.  (m, s) of the tiles (or the partial logits themselves), all of it without the label's class, and the
+// label's logit to lse, the row's loss and every workgroup's sum of them; a last small kernel (or the only workgroup) adds those up.  WPR waves a row: one, or four where rows
 // are few or their logits come in slices.
 // ---------------------------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     const float t = fmaxf(m, m2), t0 = t == -kInf ? 0.f : t;
-    s = s * __builtin_amdgcn_exp2f(m - t0) + s2 * __builtin_amdgcn_exp2f(m2 - t0);
+    s = s * __builtin_amdgcn_exp2f((m - t0) * kLog2e) + s2 * __builtin_amdgcn_exp2f((m2 - t0) * kLog2e);
     m = t;
-}
-
-// eight elements of a row of one plane or of three
-__device__ __forceinline__ void whole_eight(const unsigned short* row, int c, int nplanes, float (&f)[8]) {
-    const unsigned short* const p = nplanes == 3 ? row + plane_at<true>(c, 0, 0) : row + c;
-#pragma unroll
-    for (int k = 0; k < 3; ++k)
-        if (k < nplanes) {
-            const u32x4 u = *reinterpret_cast<const u32x4*>(p + k * 32);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float lo = __uint_as_float(u[e] << 16), hi = __uint_as_float(u[e] & 0xffff0000u);
-                f[2 * e] = k ? f[2 * e] + lo : lo;
-                f[2 * e + 1] = k ? f[2 * e + 1] + hi : hi;
-            }
-        }
 }
 
 // sums of the slices of two logits, eight slices requested at once
@@ -367,9 +361,9 @@ template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_k
                 float2 l = sliced(row + v, a.slice, a.nslices);
                 if (a.bias) { l.x += a.bias[v]; l.y += v + 1 < a.V ? a.bias[v + 1] : 0.f; }
                 if (v == y) own = l.x;
-                else join(m, s, l.x * kLog2e, 1.f);
+                else join(m, s, l.x, 1.f);
                 if (v + 1 == y) own = l.y;
-                else if (v + 1 < a.V) join(m, s, l.y * kLog2e, 1.f);
+                else if (v + 1 < a.V) join(m, s, l.y, 1.f);
             }
         } else {
             const float2* const row = a.partial + (size_t)n * a.parts;
@@ -382,17 +376,7 @@ template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_k
                 for (int q = 0; q < 4; ++q) join(m, s, v[q].x, v[q].y);
             }
             for (; t < a.parts; t += STEP) { const float2 v = row[t]; join(m, s, v.x, v.y); }
-            if (valid) {  // the label's logit: three planes add up to the fp32 they were made of
-                const unsigned short* const x = reinterpret_cast<const unsigned short*>(a.x.base) + (size_t)n * a.x.ld;
-                const unsigned short* const w = reinterpret_cast<const unsigned short*>(a.w.base) + (size_t)y * a.w.ld;
-                for (int c = l0 * 8; c < a.K; c += 8 * STEP) {
-                    float xf[8], wf[8];
-                    whole_eight(x, c, a.nplanes, xf);
-                    whole_eight(w, c, a.nplanes, wf);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) own = fmaf(xf[e], wf[e], own);
-                }
-            }
+            if (valid && l0 == 0) own = a.own[n];
         }
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -411,16 +395,15 @@ template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_k
         }
     }
     if (n < a.N && part == 0) {
-        if (!SLICES && valid && a.bias) own += a.bias[y];
-        const float o2 = own * kLog2e, mo = m, so = s;            // (SLICES: of the other classes, where there is a label)
-        if (SLICES && valid) join(m, s, o2, 1.f);
-        const float lse = (m + __builtin_amdgcn_logf(s)) * kLn2;       // log2
-        // Of a row that is all but certain the logits cancel first, and what the other classes have is not added to one (a logit at the
-        // end of fp32's range has none to base 2).
+        const float mo = m, so = s;                              // of the other classes, where there is a label
+        if (valid) join(m, s, own, 1.f);
+        const float ls = __builtin_amdgcn_logf(s) * kLn2, lse = m + ls;      // (log2)
+        // Of a row that is all but certain the logits cancel first, and what the other classes have is not added to one: its loss is
+        // never negative and has all its digits.  (Classes at the type's lowest value have logits that only differences can hold.)
         if (!valid) loss = 0.f;
-        else if (__builtin_isinf(o2)) loss = lse - own;
-        else if (SLICES && mo - o2 < 8.f) loss = log1pf(so * __builtin_amdgcn_exp2f(mo - o2));
-        else loss = ((m - o2) + __builtin_amdgcn_logf(s)) * kLn2;
+        else if (lse != lse) loss = lse;
+        else if (mo - own < 5.f) loss = log1pf(so * __builtin_amdgcn_exp2f((mo - own) * kLog2e));
+        else loss = (m - own) + ls;
         if (lane == 0) {
             a.lse[n] = lse;
             if (a.row_loss) a.row_loss[n] = loss;
@@ -455,7 +438,7 @@ template <bool BESIDE> __global__ __launch_bounds__(256) void ce_prob_kernel(con
     if (n == a.N) { ce_labels(a.labels, a.N, a.V, a.mask, a.count, s_cnt); return; }
     const int y = a.labels[n];
     const bool valid = is_class(y, a.V);
-    const float shift = a.lse[n] * kLog2e;
+    const float lse = a.lse[n];
     const float* const row = a.slices + (size_t)n * a.ldv;
     // the label's p - 1, where p is near one, as minus the sum of the others: 1 - p would lose what tells them apart
     __shared__ float s_others[4];
@@ -474,7 +457,7 @@ template <bool BESIDE> __global__ __launch_bounds__(256) void ce_prob_kernel(con
 #pragma unroll
         for (int e = 0; e < 2; ++e)
             if (valid && v + e < a.V) {
-                p[e] = __builtin_amdgcn_exp2f(fmaf((e ? l.y : l.x) + (a.bias ? a.bias[v + e] : 0.f), kLog2e, -shift));
+                p[e] = __builtin_amdgcn_exp2f(((e ? l.y : l.x) + (a.bias ? a.bias[v + e] : 0.f) - lse) * kLog2e);
                 if (v + e != y) others += p[e];
             }
         if (valid && (v == y || v + 1 == y)) { at = v; mine[0] = p[0]; mine[1] = p[1]; }

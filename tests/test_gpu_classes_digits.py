@@ -74,3 +74,42 @@ def test_probabilities_to_24_bits(n, v, dtype):
     worst = float(((db.double() - d.sum(0)).abs() / (tol.sum(0) + 4 * U32 * d.abs().sum(0))).max())
     say(f"{n} -> {v} {dtype}: dbias {worst:.2f} of the tolerance")
     assert worst <= 1.0
+
+
+CERTAIN = [(33, 2026, 234), (256, 640, 100), (300, 512, 4000), (1, 2026, 3000), (33, 2048, 2048), (32, 2048, 2049), (20, 300, 9000), (2600, 200, 3000), (5000, 96, 64),
+           (777, 333, 2345), (1, 2048, 60000)]
+
+
+def _certain(n, c, v, dtype):
+    """As rows are at the end of a training: the score of the right class stands out by 16 to 22 lengths of its weights."""
+    x, w, b, y = _inputs(n, c, v, dtype, bias=n % 2 == 0, ignored=0.1 if n > 3 else 0.0, seed=18)
+    x = (x.float() + 16 * w.float()[y.clamp(min=0).long()] * (y >= 0)[:, None]).to(x.dtype)
+    want = _reference(x, w, b, y, certain=True)
+    assert float(want["row_loss"][0].median()) < 0.05
+    return x, w, b, y, want
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,v", CERTAIN)
+def test_losses_of_nearly_certain_rows(n, c, v, dtype):
+    """A row's loss keeps its digits, however many rows and classes there are, and is never negative."""
+    from paper_2112_05387_amd import ops
+    x, w, b, y, want = _certain(n, c, v, dtype)
+    got = dict(zip(("loss", "row_loss", "lse"), ops.linear_ce_forward(x, w, y, bias=b)))
+    assert bool((got["row_loss"] >= 0).all())
+    _compare(got, want, f"losses of nearly certain rows {n} x {c} -> {v} {dtype}")
+
+
+@pytest.mark.parametrize("dtype,n,c,v", [("f32", 12, 32, 40), ("f32", 64, 512, 1000), ("f32", 300, 32, 9000), ("bf16", 300, 32, 9000), ("bf16", 64, 2048, 1000), ("bf16", 3000, 64, 300)])
+def test_every_class_at_the_lowest_value(dtype, n, c, v):
+    """The logits are lost in the bias, and all of them are the same: log v a row, and an lse that is the lowest value (log v is lost in it, so that the
+    gradient, which starts from it, has no meaning)."""
+    import torch
+    from paper_2112_05387_amd import ops
+    x, w, b, y = _inputs(n, c, v, dtype, ignored=0.2, seed=6)
+    lowest = torch.finfo(torch.float32).min
+    loss, rows, lse = ops.linear_ce_forward(x, w, y, bias=torch.full_like(b, lowest))
+    keep = y >= 0
+    assert bool((lse == lowest).all()) and bool((rows[~keep] == 0).all())
+    assert float((rows[keep] / math.log(v) - 1).abs().max()) <= 8 * U32 + _steps(v)
+    assert abs(float(loss[0]) / math.log(v) - 1) <= 16 * U32 + _steps(v)
