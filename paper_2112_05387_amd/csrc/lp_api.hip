@@ -3198,6 +3198,12 @@ struct TilePlan { int cfg, ti, tj, slices, kchunk; };
 
 static int div_up(int a, int b) { return (a + b - 1) / b; }
 
+// waves along the rows of a tile
+static int wave_rows(int cfg) {
+    int bi, bj, wi, wj;
+    ce_tile_size(cfg, &bi, &bj, &wi, &wj);
+    return wi;
+}
 static TilePlan tile_plan(int cfg, int I, int J, int K, int slices) {
     int bi, bj, wi, wj;
     ce_tile_size(cfg, &bi, &bj, &wi, &wj);
@@ -3236,13 +3242,19 @@ struct CePlan {
     TilePlan tl, tx, tw;
     int piece, pieces, ldv, ldp;             // classes of a piece of the probabilities; of a row of them, and its elements
     int width;                               // channels of a row of a laid-out operand
-    size_t o_x, o_w, o_partial, o_own, o_slices, o_bsum, o_bcnt, o_mask, o_count, o_prob, o_dx, o_dw, o_colsum, o_ticket, bytes;
+    size_t o_x, o_w, o_partial, o_own, o_slices, o_bsum, o_bcnt, o_mask, o_count, o_prob, o_dx, o_dw, o_colsum, o_others, o_dlabel, o_ticket, bytes;
     int parts, colparts;
     int direct;                              // waves a row of the kernels for small problems, or 0
 };
 
-// what the probabilities of a piece of the classes may take (or 256 classes), and bytes of one of them: three bf16
-constexpr size_t kProbBytes = (size_t)512 << 20, kProbSize = 6;
+// Bytes of a probability (three bf16), and what those of a piece of the classes may take (or 256 classes): four times what the operands
+// and gradients of the call take, between 512 MiB and 2 GiB.  One piece needs no pass of its own for what the other classes of a row have in
+// all pieces (8192 x 2048 -> 32768 in four pieces 7.74 ms, in one 6.84).
+constexpr size_t kProbSize = 6;
+static size_t prob_bytes(size_t n, size_t c, size_t v, bool low) {
+    const size_t held = low ? 4 * n * c + 6 * v * c : 8 * n * c + 8 * v * c;
+    return std::min<size_t>(std::max<size_t>(4 * held, (size_t)512 << 20), (size_t)2 << 30);
+}
 
 static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     if (!d) return fail(LP_ERR_INVALID_ARG, "descriptor is NULL");
@@ -3280,26 +3292,26 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
     const int N1 = std::max(1, p.N);
     p.tl = best_plan(p.V, N1, p.K, nl, all | few, false, &whole);
     const TilePlan tc = best_plan(p.V, N1, p.K, nl, small | few, true, &cut);
-    // (some 8 us); and so the gradient where a few rows have few classes, any of them may be all but certain, and its gradient takes the sum
-    // of its other probabilities (1 x 2026 -> 234 with a loss of 0.003, dW off by 4e-4 by tiles, which have only its lse in fp32).
-    p.cut = (cut + 8.0 < whole || (backward && N1 <= 32 && p.V <= 2048)) && (size_t)tc.slices * N1 * p.V <= ((size_t)8 << 20);
+    // (some 8 us)
+    p.cut = cut + 8.0 < whole && (size_t)tc.slices * N1 * p.V <= ((size_t)8 << 20);
     if (p.cut) p.tl = tc;
     int bi, bj, wi, wj;
     ce_tile_size(p.tl.cfg, &bi, &bj, &wi, &wj);
-    p.parts = p.tl.ti * wi;
     p.colparts = p.tl.tj * wj;
     const int round = low ? 8 : 32;
     const size_t N = p.N, V8 = (size_t)div_up(p.V, round) * round;
     p.pieces = 1; p.piece = p.V; p.ldv = (int)V8;
     // (the rows of a tile within 32 bits: at most 2^20 classes a piece)
-    if (backward && !p.cut && (kProbSize * N * V8 > kProbBytes || p.V > (1 << 20))) {
-        p.piece = (int)std::min<size_t>(1 << 20, std::max<size_t>(256, kProbBytes / (kProbSize * std::max<size_t>(N, 1)) / 256 * 256));
+    const size_t room = prob_bytes(N, p.C, p.V, low);
+    if (backward && !p.cut && (kProbSize * N * V8 > room || p.V > (1 << 20))) {
+        p.piece = (int)std::min<size_t>(1 << 20, std::max<size_t>(256, room / (kProbSize * std::max<size_t>(N, 1)) / 256 * 256));
         p.pieces = div_up(p.V, p.piece);
         p.piece = std::min(p.V, div_up(div_up(p.V, p.pieces), 256) * 256);
         p.pieces = div_up(p.V, p.piece);
         p.ldv = div_up(p.piece, round) * round;
     }
     p.ldp = low ? p.ldv : 3 * p.ldv;
+    p.parts = div_up(p.piece, bi) * wi;
     if (backward) {
         p.tx = best_plan(p.C, N1, p.piece, nx, all | few, true);
         p.tw = best_plan(p.C, p.piece, N1, nw, all, true);
@@ -3326,6 +3338,8 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
         p.o_prob = ws.take(kProbSize * N * p.ldv);
         p.o_dx = ws.take((size_t)p.tx.slices * N * p.K * 4);
         p.o_dw = p.tw.slices > 1 ? ws.take((size_t)p.tw.slices * p.piece * p.K * 4) : 0;
+        p.o_others = p.cut ? 0 : ws.take(N * p.parts * 4);
+        p.o_dlabel = p.cut ? 0 : ws.take(N * 4);
         p.o_colsum = p.cut ? 0 : ws.take((size_t)p.colparts * p.ldv * 4);
     }
     p.bytes = std::max<size_t>(ws.off, 256);
@@ -3465,6 +3479,17 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
     f.labels = labels; f.count = count; f.scale = loss_scale; f.N = p.N; f.V_all = p.V;
     f.colsum = p.cut ? nullptr : (float*)(ws + p.o_colsum); f.parts = p.colparts; f.ld_colsum = p.ldv;
     f.prob = (const unsigned short*)prob; f.pplane = pplane; f.beside = p.nplanes == 3; f.ldp = p.ldp;
+    CeLabel lab;
+    memset(&lab, 0, sizeof(lab));
+    lab.N = p.N; lab.V = p.V; lab.parts = p.parts; lab.ldp = p.ldp; lab.labels = labels; lab.others = (float*)(ws + p.o_others);
+    lab.prob = (unsigned short*)prob; lab.pplane = pplane; lab.dlabel = (float*)(ws + p.o_dlabel);
+    if (p.pieces > 1)         // what the other classes of a row have in all pieces, ahead of the label's own in its piece
+        for (int v0 = 0; v0 < p.V; v0 += p.piece) {
+            CeLogits a = ce_logits(p, X, W, bias, v0, std::min(p.piece, p.V - v0));
+            a.lse = lse; a.labels = labels; a.others = (float*)(ws + p.o_others); a.parts = lab.parts = a.tiles_i * wave_rows(p.tl.cfg);
+            if ((st = hip_status(launch_ce_sums(a, p.tl.cfg, s))) != LP_OK || (st = hip_status(launch_ce_others(lab, v0 == 0, s))) != LP_OK) return st;
+        }
+    else if (!p.cut) f.dlabel = lab.dlabel;
     for (int v0 = 0, piece = 0; piece < p.pieces; ++piece, v0 += p.piece) {
         const int V = std::min(p.piece, p.V - v0);
         CeLogits a = ce_logits(p, X, W, bias, v0, V);
@@ -3479,7 +3504,10 @@ lp_status lp_linear_ce_backward(const lp_linear_ce_desc* d, void* stream, const 
             if (st == LP_OK) st = hip_status(launch_ce_prob(r, (unsigned short*)prob, pplane, p.ldp, p.nplanes == 3, s));
         } else {
             a.colsum = dbias ? (float*)(ws + p.o_colsum) : nullptr; a.ld_colsum = p.ldv;
+            if (p.pieces > 1) a.dlabel = lab.dlabel;
+            else { a.others = (float*)(ws + p.o_others); a.parts = p.parts; }
             st = hip_status(launch_ce_prob_tiles(a, p.tl.cfg, s));
+            if (st == LP_OK && p.pieces == 1) st = hip_status(launch_ce_label(lab, p.nplanes == 3, s));
         }
         if (st != LP_OK) return st;
         CeGrad g;

@@ -26,6 +26,15 @@ struct CeLogits {
     const float* lse; const int* labels;
     char* prob; size_t pplane;          // probabilities: three planes of bf16 [N][ldv], or beside each other [N][ldp]
     float* colsum; int ld_colsum;       // their sums over the samples of every wave's tile, or null
+    float* others;                      // their sums over the classes of every wave's tile but the label's, [N][parts], or null
+    const float* dlabel;                // the label's p - 1 where p > 1/2, or null: left at zero
+};
+struct CeLabel {
+    int N, V, parts, ldp;
+    const int* labels;
+    const float* others;
+    unsigned short* prob; size_t pplane;
+    float* dlabel;                      // -sum of the others where p > 1/2, or zero
 };
 struct CeRows {
     int N, V;
@@ -58,6 +67,7 @@ struct CeFinish {
     const int* labels; const int* count; float scale;
     int N, V, V_all;                    // V: classes of the bias here
     const float* colsum; int parts, ld_colsum;
+    const float* dlabel;                // what the labels' classes have besides, or null
     const unsigned short* prob; size_t pplane; int beside, ldp;
     float* dbias;
 };
@@ -83,6 +93,9 @@ double ce_tile_time(int cfg, long blocks, int ktiles);
 hipError_t launch_ce_pack(CePack x, CePack w, int dtype, hipStream_t s);
 hipError_t launch_ce_stats(const CeLogits& a, int cfg, hipStream_t s);
 hipError_t launch_ce_prob_tiles(const CeLogits& a, int cfg, hipStream_t s);
+hipError_t launch_ce_sums(const CeLogits& a, int cfg, hipStream_t s);
+hipError_t launch_ce_label(const CeLabel& a, bool beside, hipStream_t s);
+hipError_t launch_ce_others(const CeLabel& a, bool first, hipStream_t s);
 hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t s);
 hipError_t launch_ce_rows(const CeRows& a, hipStream_t s);
 hipError_t launch_ce_prob(const CeRows& a, unsigned short* prob, size_t pplane, int ldp, bool beside, hipStream_t s);

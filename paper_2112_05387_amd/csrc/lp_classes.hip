@@ -16,6 +16,10 @@
 // fp32: every operand as three bf16 (24 bits) that lie beside each other, six of the nine products (the others are below 2^-25).
 // 73623 classes x 8716 rows of 633 channels: a product in 4.2 ms, 195 TFLOP/s of fp32; the card's fp32 matrix product reaches 151.
 //
+// Of a row that is all but certain p - 1 has lost what tells p from one (lse is fp32: 33 x 2026 -> 234 with a loss of 7e-4, dW off by 4.7e-4,
+// some p above one).  There d is minus the sum of the other classes' p, which the tiles yield beside their probabilities: the label's own is
+// filled in by a small kernel behind them, or, where the classes come in pieces, known from a pass over all pieces ahead of them.
+//
 // Rows whose label is no class (ignored): probability zero in the epilogue by selection, and their features count as zero in
 // dW whatever they hold (a bit a row, read by the loads): no infinity or NaN in them reaches a sum.
 //
@@ -122,7 +126,7 @@ __device__ __forceinline__ void ce_labels(const int* __restrict__ labels, int N,
 // l = X W^T: rows i are classes, columns j are samples, so that a lane has four consecutive classes of one sample and the
 // statistics of a sample are sums inside a lane and over two lanes
 // ---------------------------------------------------------------------------------------------------------------------------------
-enum LogitsMode { LM_STATS, LM_PROB, LM_SLICE };
+enum LogitsMode { LM_STATS, LM_PROB, LM_SLICE, LM_SUM };
 
 // parts of 32 samples' probabilities that fit into LDS for all waves at once
 template <class T> constexpr int prob_parts() { return 3 * T::NW * 32 * (T::TI * 2 + 16) <= 160 * 1024 ? 3 : 2; }
@@ -228,16 +232,41 @@ template <class T, int MODE, int WAVES> __global__ __launch_bounds__(T::NT, WAVE
             const int y = n < a.N ? a.labels[n] : -1;
             const bool valid = is_class(y, a.V_all);
             const float lse = n < a.N ? a.lse[n] : 0.f;
-            // the label's class, where this lane has it: its one is taken off before the parts are formed
+            // the label's class, where this lane has it
             const int at = valid ? y - a.v0 - ib - 4 * h : -1;
+            const bool here = __any(at >= 0 && at < T::TI);
+            float own = 0.f, s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < FI; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float p = valid ? __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * kLog2e) : 0.f;
-                    if (at == i * 32 + 8 * (r >> 2) + (r & 3)) p -= 1.f;
-                    acc[i][j][r] = p;
-                }
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = valid ? __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * kLog2e) : 0.f;
+            if (here) {
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (at == i * 32 + 8 * (r >> 2) + (r & 3)) { own = acc[i][j][r]; acc[i][j][r] = 0.f; }
+            }
+            if (a.others) {
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r & 3] += acc[i][j][r];
+                float t = (s[0] + s[1]) + (s[2] + s[3]);
+                t += __shfl_xor(t, 32);
+                if (h == 0 && n < a.N) a.others[(size_t)n * a.parts + ti * (T::BI / T::TI) + wi] = t;
+            }
+            if constexpr (MODE == LM_SUM) continue;
+            if (here) {
+                // p - 1; where p is near one the difference has lost what tells them apart, and minus the sum of the others stands in for it, now
+                // (dlabel) or as soon as it is known
+                const float d = own > 0.5f ? (a.dlabel && at >= 0 && at < T::TI ? a.dlabel[n] : 0.f) : own - 1.f;
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (at == i * 32 + 8 * (r >> 2) + (r & 3)) acc[i][j][r] = d;
+            }
 #pragma unroll
             for (int k0 = 0; k0 < NP; k0 += AT_ONCE) {
 #pragma unroll
@@ -279,7 +308,7 @@ template <class T, int MODE, int WAVES> __global__ __launch_bounds__(T::NT, WAVE
                 __builtin_amdgcn_s_waitcnt(0xc07f);              // read before the next ones overwrite it
             }
         }
-        if (a.colsum) {
+        if (MODE == LM_PROB && a.colsum) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
 #pragma unroll
@@ -428,6 +457,40 @@ template <bool SLICES, int WPR> __global__ __launch_bounds__(256) void ce_rows_k
     }
     __syncthreads();
     if (s_last) ce_total<true>(a.bsum, a.bcnt, gridDim.x, a.loss);
+}
+
+// Behind the tiles' sums of the probabilities of all classes but the label's, a wave a row: the label's own where p > 1/2 (what the tiles left
+// at zero; any other is -1/2 or below) goes into the parts, and to dlabel for the bias.
+template <bool BESIDE> __global__ __launch_bounds__(256) void ce_label_kernel(const CeLabel a) {
+    const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (n >= a.N) return;
+    const int y = a.labels[n];
+    unsigned short* const row = a.prob + (size_t)n * a.ldp;
+    const bool left = is_class(y, a.V) && (row[plane_at<BESIDE>(is_class(y, a.V) ? y : 0, 0, a.pplane / 2)] & 0x7fffu) == 0;
+    float t = 0.f;
+    if (left) {
+#pragma unroll 4
+        for (int k = lane; k < a.parts; k += 64) t += a.others[(size_t)n * a.parts + k];
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) t += __shfl_xor(t, o);
+    }
+    if (lane == 0) a.dlabel[n] = -t;
+    if (!left || lane != 0) return;
+    unsigned b[3];
+    split_bf16<3>(-t, b);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) row[plane_at<BESIDE>(y, k, a.pplane / 2)] = (unsigned short)b[k];
+}
+// Where the classes come in pieces: minus the sum over all of them, piece by piece, ahead of the probabilities
+__global__ __launch_bounds__(256) void ce_others_kernel(const CeLabel a, bool first) {
+    const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (n >= a.N) return;
+    float t = 0.f;
+#pragma unroll 4
+    for (int k = lane; k < a.parts; k += 64) t += a.others[(size_t)n * a.parts + k];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) t += __shfl_xor(t, o);
+    if (lane == 0) a.dlabel[n] = (first ? 0.f : a.dlabel[n]) - t;
 }
 
 // Probabilities from partial logits (few tiles): a workgroup a row
@@ -601,8 +664,34 @@ template <class T> __global__ __launch_bounds__(256) void ce_finish_kernel(const
     }
     if (a.colsum) {  // bias from the tiles' sums: 32 classes a workgroup, eight groups of threads a part of the tiles each
         __shared__ float s_b[8][32];
-        const int col = threadIdx.x & 31, grp = threadIdx.x >> 5, v = (b - a.blocks_x - a.blocks_w) * 32 + col;
+        extern __shared__ float s_l[];                            // [32][257]: every thread's sums of the label's share, of the rows it has
+        const int col = threadIdx.x & 31, grp = threadIdx.x >> 5, v0 = (b - a.blocks_x - a.blocks_w) * 32, v = v0 + col;
         float t = 0.f;
+        if (a.dlabel) {
+            constexpr int PITCH = 257;
+            float* const mine = s_l + threadIdx.x;
+#pragma unroll
+            for (int k = 0; k < 32; ++k) mine[k * PITCH] = 0.f;
+            constexpr int R = 16;                                 // rows whose loads are under way together
+            for (int n0 = threadIdx.x; n0 < a.N; n0 += 256 * R) {
+                int y[R];
+                float d[R];
+#pragma unroll
+                for (int q = 0; q < R; ++q) {
+                    const int n = min(n0 + q * 256, a.N - 1);
+                    y[q] = a.labels[n];
+                    d[q] = a.dlabel[n];
+                }
+#pragma unroll
+                for (int q = 0; q < R; ++q) {
+                    const unsigned k = (unsigned)(y[q] - v0);
+                    if (n0 + q * 256 < a.N && k < 32u) mine[k * PITCH] += d[q];
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) t += s_l[col * PITCH + grp * 32 + k];
+        }
         if (v < a.V) {
 #pragma unroll 8
             for (int k = grp; k < a.parts; k += 8) t += a.colsum[(size_t)k * a.ld_colsum + v];
@@ -719,6 +808,25 @@ hipError_t launch_ce_prob_tiles(const CeLogits& a, int cfg, hipStream_t s) {
         default: return launch_logits_t<TSmall3<false, false, false>, LM_PROB, 2>(a, 1, s);
     }
 }
+hipError_t launch_ce_sums(const CeLogits& a, int cfg, hipStream_t s) {
+    switch (cfg) {
+        case 0: return launch_logits_t<TBig<false, false, false>, LM_SUM, 2>(a, 1, s);
+        case 1: return launch_logits_t<TMid<false, false, false>, LM_SUM, 2>(a, 1, s);
+        case 2: return launch_logits_t<TSmall<false, false, false>, LM_SUM, 2>(a, 1, s);
+        case 3: return launch_logits_t<TFew<false, false, false>, LM_SUM, 2>(a, 1, s);
+        case 4: return launch_logits_t<TMid3<false, false, false>, LM_SUM, 2>(a, 1, s);
+        default: return launch_logits_t<TSmall3<false, false, false>, LM_SUM, 2>(a, 1, s);
+    }
+}
+hipError_t launch_ce_label(const CeLabel& a, bool beside, hipStream_t s) {
+    if (beside) hipLaunchKernelGGL(ce_label_kernel<true>, dim3((a.N + 3) / 4), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(ce_label_kernel<false>, dim3((a.N + 3) / 4), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+hipError_t launch_ce_others(const CeLabel& a, bool first, hipStream_t s) {
+    hipLaunchKernelGGL(ce_others_kernel, dim3((a.N + 3) / 4), dim3(256), 0, s, a, first);
+    return hipGetLastError();
+}
 hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t s) {
     switch (cfg) {
         case 2: return launch_logits_t<TSmall<false, false, false>, LM_SLICE, 2>(a, slices, s);
@@ -770,8 +878,9 @@ hipError_t launch_ce_dw(const CeGrad& a, int slices, int cfg, hipStream_t s) {
 hipError_t launch_ce_finish(const CeFinish& a, int dtype, hipStream_t s) {
     const int blocks = a.blocks_x + a.blocks_w + a.blocks_b;
     if (blocks == 0) return hipSuccess;
-    if (dtype == 1) hipLaunchKernelGGL(ce_finish_kernel<bf16_t>, dim3(blocks), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(ce_finish_kernel<float>, dim3(blocks), dim3(256), 0, s, a);
+    const int lds = a.blocks_b && a.dlabel ? 32 * 257 * (int)sizeof(float) : 0;
+    if (dtype == 1) hipLaunchKernelGGL(ce_finish_kernel<bf16_t>, dim3(blocks), dim3(256), lds, s, a);
+    else hipLaunchKernelGGL(ce_finish_kernel<float>, dim3(blocks), dim3(256), lds, s, a);
     return hipGetLastError();
 }
 hipError_t launch_ce_zero(float* p, size_t n, hipStream_t s) {

@@ -100,6 +100,14 @@ def test_losses_of_nearly_certain_rows(n, c, v, dtype):
     _compare(got, want, f"losses of nearly certain rows {n} x {c} -> {v} {dtype}")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,v", CERTAIN)
+def test_gradients_of_nearly_certain_rows(n, c, v, dtype):
+    """... and its gradient."""
+    x, w, b, y, want = _certain(n, c, v, dtype)
+    _compare(_run(x, w, b, y), want, f"gradients of nearly certain rows {n} x {c} -> {v} {dtype}")
+
+
 @pytest.mark.parametrize("dtype,n,c,v", [("f32", 12, 32, 40), ("f32", 64, 512, 1000), ("f32", 300, 32, 9000), ("bf16", 300, 32, 9000), ("bf16", 64, 2048, 1000), ("bf16", 3000, 64, 300)])
 def test_every_class_at_the_lowest_value(dtype, n, c, v):
     """The logits are lost in the bias, and all of them are the same: log v a row, and an lse that is the lowest value (log v is lost in it, so that the
@@ -113,3 +121,22 @@ def test_every_class_at_the_lowest_value(dtype, n, c, v):
     assert bool((lse == lowest).all()) and bool((rows[~keep] == 0).all())
     assert float((rows[keep] / math.log(v) - 1).abs().max()) <= 8 * U32 + _steps(v)
     assert abs(float(loss[0]) / math.log(v) - 1) <= 16 * U32 + _steps(v)
+
+
+PIECES = [("bf16", 8000, 2048, 45000), ("bf16", 8192, 60, 45003), ("f32", 8192, 40, 45003)]
+
+
+@pytest.mark.parametrize("certain", [False, True])
+@pytest.mark.parametrize("dtype,n,c,v", PIECES)
+def test_large_pieces_of_the_classes(dtype, n, c, v, certain):
+    """Probabilities of all classes would take more than the workspace holds at once: several pieces, the last one ragged, the gradient of the features added up
+    over them; and rows whose own class lies in one piece and what is left of them in all."""
+    from paper_2112_05387_amd import binding as B
+    d = B.lp_linear_ce_desc(n, c, v, B.LP_BF16 if dtype == "bf16" else B.LP_F32, 0, 0, 0)
+    assert B.lp_linear_ce_workspace_bytes(d, True) < 4 * n * c * 16 + 6 * n * v
+    x, w, b, y = _inputs(n, c, v, dtype, ignored=0.1, seed=7)
+    if certain:
+        x = (x.float() + 16 * w.float()[y.clamp(min=0).long()] * (y >= 0)[:, None]).to(x.dtype)
+    got = _run(x, w, b, y)
+    assert bool((got["row_loss"] >= 0).all())
+    _compare(got, _reference(x, w, b, y, certain=certain), f"pieces {n} x {c} -> {v} {dtype}")
