@@ -361,7 +361,12 @@ lp_status lp_net_set_fused_update(struct lp_net* net, int on, float lr, float mo
  * terminal adjoint dy[k] for lp_module_backward).
  *     lse_n = log sum_v exp(l_nv),  row_loss_n = lse_n - l_n,label(n),  loss = sum row_loss / max(1, number of rows that count)
  * A row counts when its label is in [0, classes); any other label (-1, say) leaves it out: row_loss 0, gradient 0, and
- * nothing of what its features hold reaches a sum (its lse is still written).  A class is switched off by a bias of minus infinity.
+ * nothing of what its features hold reaches a sum (its lse is still written).  A class is switched off by a bias of minus infinity, or
+ * of the type's lowest value.  Features and weight are to be finite otherwise: an infinity or NaN in the features of a row that counts
+ * makes that row's lse, loss and dfeatures NaN (an infinite logit of either sign too: the parts that operands are held in have
+ * no infinity of their own), and with them loss, dweight and dbias, and leaves the other rows' as they are; one in weight makes NaN of all rows.
+ * The gradients start from lse in fp32, so a probability is off by 2^-24 |lse| of itself; a row whose classes are all at the
+ * lowest value has a loss but no gradient.
  * Sums, statistics, loss and the gradients of weight and bias are fp32.  LP_BF16: features, weight and dfeatures are
  * bf16, the probabilities are held as a sum of three bf16, of which dfeatures reads two.  LP_F32: all fp32, products from
  * operands split into three bf16.  Results do not depend on the order in which workgroups run: the same bits on every call. */

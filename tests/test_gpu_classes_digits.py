@@ -140,3 +140,19 @@ def test_large_pieces_of_the_classes(dtype, n, c, v, certain):
     got = _run(x, w, b, y)
     assert bool((got["row_loss"] >= 0).all())
     _compare(got, _reference(x, w, b, y, certain=certain), f"pieces {n} x {c} -> {v} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,v", [(64, 48, 300), (700, 64, 9000), (64, 512, 1000)])
+def test_infinities_stay_in_their_row(n, c, v, dtype):
+    """An infinity or NaN in the features of a row that counts: no value in that row, every other row's loss and gradient as without it."""
+    import torch
+    x, w, b, y = _inputs(n, c, v, dtype, seed=2)
+    want = _reference(x, w, b, y)
+    bad = x.clone()
+    bad[5, 3], bad[6, 3], bad[7, 3] = float("nan"), float("inf"), float("-inf")
+    got = _run(bad, w, b, y)
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[5:8] = False
+    assert bool(got["lse"][~rest].isnan().all()) and bool(got["row_loss"][~rest].isnan().all()) and bool(got["dfeatures"][~rest].isnan().any(1).all())
+    _compare({k: got[k][rest] for k in ("lse", "row_loss", "dfeatures")}, {k: (want[k][0][rest], want[k][1][rest]) for k in ("lse", "row_loss", "dfeatures")}, "beside infinities")
