@@ -142,6 +142,42 @@ def test_large_pieces_of_the_classes(dtype, n, c, v, certain):
     _compare(got, _reference(x, w, b, y, certain=certain), f"pieces {n} x {c} -> {v} {dtype}")
 
 
+@pytest.mark.parametrize("n,c,v", [(30, 12, 40), (300, 32, 9000), (64, 512, 1000), (1500, 24, 3000)])
+def test_gradient_along_itself(n, c, v):
+    """Central differences of the loss along the gradient, where they are far above what they are off by: the losses (row by row, added in 64 bits) by
+    the tolerance of a row's loss over the step, the third derivative of log sum exp by at most 2 (2 m)^3 / 6 h^2 where no logit moves by more
+    than m; h m = 1/32."""
+    import torch
+    from paper_2112_05387_amd import ops
+    x, w, b, y = _inputs(n, c, v, "f32", ignored=0.1, seed=4)
+    want = _reference(x, w, b, y)
+    count = int((y >= 0).sum())
+    _, _, lse = ops.linear_ce_forward(x, w, y, bias=b)
+    grads = ops.linear_ce_backward(x, w, y, lse, bias=b)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    for i, (t, name) in enumerate(((x, "dfeatures"), (w, "dweight"), (b, "dbias"))):
+        ref = want[name][0]
+        d = ref + 0.5 * ref.norm() * torch.randn(ref.shape, generator=gen, device="cuda", dtype=torch.float64) / math.sqrt(ref.numel())
+        d = (d / d.norm()).float()
+        dd = d.double()
+        move = float((dd @ w.double().t() if i == 0 else x.double() @ dd.t() if i == 1 else dd[None]).abs().max())
+        h = 2.0 ** math.floor(math.log2(1 / 32 / move))
+        f, step = [], []
+        for s in (h, -h):
+            a = [x, w, b]
+            a[i] = t + s * d
+            f.append(float(ops.linear_ce_forward(a[0], a[1], y, bias=a[2])[1].double().sum()) / count)
+            step.append((a[i].double() - t.double()))
+        real = step[0] - step[1]                      # (the step that the rounded operands take)
+        slope = f[0] - f[1]
+        mine = float((grads[i].double() * real).sum())
+        tol = 2 * h * (h * h * (2 * move) ** 3 / 3) + 2 * float(want["loss"][1])
+        say(f"{name}: difference {slope:.3e}, gradient {mine:.3e}, tolerance {tol:.1e}")
+        assert abs(mine) > 4 * tol
+        assert abs(slope - mine) <= tol
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,c,v", [(64, 48, 300), (700, 64, 9000), (64, 512, 1000)])
 def test_infinities_stay_in_their_row(n, c, v, dtype):
