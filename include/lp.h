@@ -363,8 +363,8 @@ lp_status lp_net_set_fused_update(struct lp_net* net, int on, float lr, float mo
  * A row counts when its label is in [0, classes); any other label (-1, say) leaves it out: row_loss 0, gradient 0, and
  * nothing of what its features hold reaches a sum (its lse is still written).  A class is switched off by a bias of minus infinity, or
  * of the type's lowest value.  Features and weight are to be finite otherwise: an infinity or NaN in the features of a row that counts
- * makes that row's lse, loss and dfeatures NaN (an infinite logit of either sign too: the parts that operands are held in have
- * no infinity of their own), and with them loss, dweight and dbias, and leaves the other rows' as they are; one in weight makes NaN of all rows.
+ * leaves it no finite lse, and NaN as its loss and dfeatures (an infinite logit has no probability: the parts that operands are held
+ * in have no infinity of their own), and with them as loss, dweight and dbias; other rows keep theirs.  One in weight does so to all rows.
  * The gradients start from lse in fp32, so a probability is off by 2^-24 |lse| of itself; a row whose classes are all at the
  * lowest value has a loss but no gradient.
  * Sums, statistics, loss and the gradients of weight and bias are fp32.  LP_BF16: features, weight and dfeatures are
@@ -506,6 +506,14 @@ lp_status lp_debug_layer_kernels(int dtype, int N, int H, int W, int Cin, int Co
 /* Does the linear layer of a head (N samples, C channels) run in its tiled kernels (host only)?  tiled[2] = {forward, filter
  * gradient}.  Errors: LP_ERR_INVALID_ARG. */
 lp_status lp_debug_linear_kernels(int N, int classes, int C, int* tiled);
+
+/* How calls of the operators run (host only).  lp_linear_ce_forward / _backward: plan[0] waves a row of the kernels for small problems, 0: by
+ * tiles; [1] the channels of the logits are cut; [2] pieces of the classes; then tile and slices of the reduction of the logits
+ * ([3], [4]), of dfeatures ([5], [6]) and of dweight ([7], [8]; backward only).  Tiles: 0 256 x 256, 1 128 x 128, 2 64 x 64, 3 128 x 32; of three planes 4
+ * 128 x 128, 5 64 x 64.  lp_orthogonalize: tile of the symmetric products, of the step (0 256 x 256, 1 256 x 320, 2 128 x 128, 3 64 x 64), and
+ * matrices that stay in one workgroup. */
+lp_status lp_debug_linear_ce_plan(const lp_linear_ce_desc* d, int backward, int* plan);
+lp_status lp_debug_orthogonalize_plan(int n, const lp_matrix* mats, int* plan);
 
 /* A per-thread switch read by lp_net_create: nets created while it is on run the kernels that the specialised ones stand in
  * for (batch norms as passes of their own and over whole rows, the large tiles of wide layers, the general filter gradients),

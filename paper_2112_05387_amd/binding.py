@@ -16,7 +16,7 @@ EXPORTS = ["lp_net_create", "lp_net_destroy", "lp_net_param_bytes", "lp_net_num_
            "lp_net_workspace_bytes", "lp_net_set_workspace", "lp_auxnet_forward", "lp_auxnet_forward_static", "lp_module_forward",
            "lp_local_loss_grad", "lp_module_backward", "lp_al_multiplier_update", "lp_aux_variable_update", "lp_auxnet_distill_grad", "lp_sgd_update", "lp_reauxnet_grad", "lp_linear_ce_workspace_bytes", "lp_linear_ce_forward", "lp_linear_ce_backward", "lp_orthogonalize_workspace_bytes", "lp_orthogonalize", "lp_muon_step_workspace_bytes", "lp_muon_step", "lp_muon_workspace_bytes", "lp_muon_update", "lp_net_set_stream_lanes", "lp_local_step", "lp_net_set_residual_output", "lp_net_set_deterministic",
            "lp_debug_im2col_offsets", "lp_debug_keep_gradients", "lp_debug_unit_count", "lp_debug_unit_info",
-           "lp_debug_module_info", "lp_debug_filter_load_extent", "lp_debug_conv_geometry", "lp_debug_conv_offsets", "lp_debug_mfma_peak", "lp_debug_layer_kernels", "lp_debug_stream_lanes", "lp_debug_separate_passes", "lp_debug_linear_kernels",
+           "lp_debug_module_info", "lp_debug_filter_load_extent", "lp_debug_conv_geometry", "lp_debug_conv_offsets", "lp_debug_mfma_peak", "lp_debug_layer_kernels", "lp_debug_stream_lanes", "lp_debug_separate_passes", "lp_debug_linear_kernels", "lp_debug_linear_ce_plan", "lp_debug_orthogonalize_plan",
            "lp_debug_saved_tensor", "lp_net_set_fused_update", "lp_profile_enable", "lp_profile_fetch", "lp_last_error", "lp_version"]
 
 KIND_NAMES = {0: "clears+filter_relayout", 1: "filter_relayout", 2: "conv_igemm(fwd/dgrad)", 3: "bn_apply", 4: "maxpool_fwd", 5: "head_fwd",
@@ -155,6 +155,8 @@ def lib():
         L.lp_debug_mfma_peak.argtypes = [c_void_p, c_int, c_int, c_int, c_void_p, c_void_p]
         L.lp_debug_stream_lanes.argtypes = [c_void_p, c_int, POINTER(c_int), POINTER(c_int)]
         L.lp_debug_linear_kernels.argtypes = [c_int] * 3 + [POINTER(c_int)]
+        L.lp_debug_linear_ce_plan.argtypes = [cep, c_int, POINTER(c_int)]
+        L.lp_debug_orthogonalize_plan.argtypes = [c_int, POINTER(lp_matrix), POINTER(c_int)]
         L.lp_debug_separate_passes.argtypes = [c_int]
         L.lp_debug_layer_kernels.argtypes = [c_int] * 9 + [POINTER(c_int)]
         L.lp_debug_keep_gradients.argtypes = [c_int]
@@ -452,6 +454,20 @@ def lp_debug_linear_kernels(N, classes, C):
     t = (c_int * 2)()
     _check(lib().lp_debug_linear_kernels(N, classes, C, t))
     return bool(t[0]), bool(t[1])
+
+
+def lp_debug_linear_ce_plan(desc, backward):
+    """(waves a row of the kernels for small problems, channels cut, pieces, tile and slices of the logits, of dfeatures, of dweight)"""
+    t = (c_int * 9)()
+    _check(lib().lp_debug_linear_ce_plan(ctypes.byref(desc), int(backward), t))
+    return list(t)
+
+
+def lp_debug_orthogonalize_plan(mats):
+    """(tile of the symmetric products, of the step, matrices that stay in one workgroup)"""
+    t = (c_int * 3)()
+    _check(lib().lp_debug_orthogonalize_plan(len(mats), mats, t))
+    return list(t)
 
 
 def lp_debug_stream_lanes(net, K, whole_step=True):

@@ -4187,6 +4187,30 @@ lp_status lp_debug_linear_kernels(int N, int classes, int C, int* tiled) {
     return LP_OK;
 }
 
+lp_status lp_debug_linear_ce_plan(const lp_linear_ce_desc* d, int backward, int* plan) {
+    if (!plan) return fail(LP_ERR_INVALID_ARG, "plan is NULL");
+    CePlan p;
+    const lp_status st = ce_plan(d, backward != 0, p);
+    if (st != LP_OK) return st;
+    std::fill(plan, plan + 9, 0);
+    plan[0] = p.direct;
+    if (p.direct) return LP_OK;
+    plan[1] = p.cut; plan[2] = p.pieces; plan[3] = p.tl.cfg; plan[4] = p.tl.slices;
+    if (backward) { plan[5] = p.tx.cfg; plan[6] = p.tx.slices; plan[7] = p.tw.cfg; plan[8] = p.tw.slices; }
+    return LP_OK;
+}
+
+lp_status lp_debug_orthogonalize_plan(int n, const lp_matrix* mats, int* plan) {
+    if (!plan) return fail(LP_ERR_INVALID_ARG, "plan is NULL");
+    return guarded([&] {
+        OrthoPlan o;
+        const lp_status st = ortho_matrices(n, mats, o);
+        if (st != LP_OK) return st;
+        plan[0] = o.cfg_sq; plan[1] = o.cfg_step; plan[2] = o.start[0].back();
+        return LP_OK;
+    });
+}
+
 lp_status lp_debug_stream_lanes(const struct lp_net* net, int whole_step, int* is_folded, int* lanes) {
     if (!net || !is_folded || !lanes) return fail(LP_ERR_INVALID_ARG, "NULL argument");
     *is_folded = folded(net) ? 1 : 0;
