@@ -3336,7 +3336,7 @@ static lp_status ce_plan(const lp_linear_ce_desc* d, bool backward, CePlan& p) {
         p.o_mask = ws.take((N + 63) / 64 * 8);
         p.o_count = ws.take(4);
         p.o_prob = ws.take(kProbSize * N * p.ldv);
-        p.o_dx = ws.take((size_t)p.tx.slices * N * p.K * 4);
+        p.o_dx = p.pieces > 1 || p.tx.slices > 1 ? ws.take((size_t)p.tx.slices * N * p.K * 4) : 0;
         p.o_dw = p.tw.slices > 1 ? ws.take((size_t)p.tw.slices * p.piece * p.K * 4) : 0;
         p.o_others = p.cut ? 0 : ws.take(N * p.parts * 4);
         p.o_dlabel = p.cut ? 0 : ws.take(N * 4);

@@ -51,3 +51,14 @@ def test_orthogonalisation_tiles():
         plans.setdefault((step, shapes[0][0] > shapes[0][1]), shapes)
         plans.setdefault(("symmetric", square), shapes)
     assert set(plans) == {(t, tall) for t in range(4) for tall in (False, True)} | {("symmetric", t) for t in (0, 2, 3)}, plans
+
+
+def test_workspace_of_a_gradient_that_needs_no_sums():
+    """dfeatures comes whole out of its product: no partial results of it are held.  What is: three parts of the probabilities, sums of the other classes (a float
+    for 128 classes of a row) and over the rows (one for 64 rows of a class), the row mask, a float a row, and alignment."""
+    for n, c, v in ((20000, 1024, 4096), (8000, 2048, 20000), (2048, 2048, 8192)):
+        d = B.lp_linear_ce_desc(n, c, v, B.LP_BF16, 0, 0, 0)
+        plan = B.lp_debug_linear_ce_plan(d, True)
+        assert plan[2] == 1 and plan[6] == 1 and plan[8] == 1
+        wide = v + 256
+        assert B.lp_linear_ce_workspace_bytes(d, True) <= 6 * n * wide + 4 * n * (wide // 128 + 2) + 4 * (n // 64 + 4) * wide + 5 * n + 8192 < 6 * n * v + 4 * n * c
