@@ -292,7 +292,9 @@ lp_status lp_sgd_update(struct lp_net* net, void* stream, int aux, uint32_t mask
  * (X^T X for a tall matrix), which take every singular value s > 0 of U / |U|_F towards one (0.7 .. 1.2 after five steps from s
  * > 0.01 or so) and leave the singular vectors.  Each U [rows, cols] in fp32 or bf16, any row stride; the result in either type;
  * `out` may be `in` (with the same row stride and type); otherwise no `out` may overlap another matrix's `in` or `out`.  Sizes may
- * differ from matrix to matrix; rows or cols of 0 are passed over.  Products of operands held in two fp16 parts, sums in fp32, |U| in fp64; bit-identical from call to call. */
+ * differ from matrix to matrix; rows or cols of 0 are passed over.  Products of operands held in two fp16 parts, sums in fp32, |U| in
+ * fp64.  The same list gives the same bits on every call; the tiles are chosen for a list as a whole, so a matrix too large for one
+ * workgroup may differ, within its error, beside others from what it is alone. */
 typedef struct {
     int rows, cols;              /* 0 .. 2^20; the shorter side at most 16384 */
     int dtype_in, dtype_out;     /* lp_dtype */
@@ -369,7 +371,8 @@ lp_status lp_net_set_fused_update(struct lp_net* net, int on, float lr, float mo
  * lowest value has a loss but no gradient.
  * Sums, statistics, loss and the gradients of weight and bias are fp32.  LP_BF16: features, weight and dfeatures are
  * bf16, the probabilities are held as a sum of three bf16, of which dfeatures reads two.  LP_F32: all fp32, products from
- * operands split into three bf16.  Results do not depend on the order in which workgroups run: the same bits on every call. */
+ * operands split into three bf16.  Results do not depend on the order in which workgroups run: the same bits on every call of the same
+ * sizes and strides. */
 typedef struct {
     int rows;              /* 0 .. 2^26 - 4 */
     int channels;          /* 1 .. 65536 */

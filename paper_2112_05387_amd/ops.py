@@ -123,7 +123,8 @@ def linear_ce_backward(features, weight, labels, lse, bias=None, scale=1.0):
 
 def orthogonalize(matrices, steps=5, out_dtype=None):
     """The matrices with their singular values taken towards one by Newton-Schulz products (lp_orthogonalize): a list of new
-    tensors, each of its matrix's type (or `out_dtype`).  float32 or bfloat16, any sizes and row strides, all in the same launches."""
+    tensors, each of its matrix's type (or `out_dtype`).  float32 or bfloat16, any sizes and row strides, all in the same launches (whose tiles are chosen for the
+    list as a whole: a large matrix beside others may differ from itself alone within its error)."""
     matrices = list(matrices)
     dev = _device(*matrices)
     mats = (B.lp_matrix * len(matrices))()
