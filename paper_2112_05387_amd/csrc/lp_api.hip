@@ -3581,8 +3581,10 @@ static lp_status ortho_plan(OrthoPlan& o) {
     WsAlloc ws;
     o.o_table = ws.take(o.table_words() * 4);
     auto large = [](const NsProb& q) { return !(q.flags & NS_PLAIN) && ns_small_lds(q.rows, q.cols) == 0; };
-    // the tile that is fastest for all of them together
+    // the tile that is fastest for all of them together (256 x 256 leaves no registers for the parts of a long sum)
     double best_sq = 1e300, best_step = 1e300;
+    bool thin = false;
+    for (const NsProb& q : o.p) thin = thin || (large(q) && NsWork(q.rows, q.cols).thin());
     for (int c = 0; c < NT_COUNT; ++c) {
         int bi, bj;
         ns_tile_size(c, &bi, &bj);
@@ -3594,7 +3596,7 @@ static lp_status ortho_plan(OrthoPlan& o) {
                 step += (long)div_up(w.r, bj) * div_up(w.c, bi);
             }
         const double tq = ns_tile_time(c, sq), ts = ns_tile_time(c, step);
-        if (bi == bj && tq < best_sq) { best_sq = tq; o.cfg_sq = c; }
+        if (bi == bj && tq < best_sq && !(thin && c == NT_256)) { best_sq = tq; o.cfg_sq = c; }
         if (ts < best_step) { best_step = ts; o.cfg_step = c; }
     }
     int bs, bi, bj;

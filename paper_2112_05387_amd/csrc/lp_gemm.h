@@ -61,7 +61,7 @@ typedef __attribute__((address_space(3))) void* gemm_lds_t;
 typedef const __attribute__((address_space(4))) unsigned long long* GemmMask;      // read by scalar loads
 typedef __attribute__((ext_vector_type(4))) short gemm_s16x4;
 
-template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGES, bool MASKED = false, int PL = 1> struct GemmTile {
+template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGES, bool MASKED = false, int PL = 1, bool PARTS = false> struct GemmTile {
     static constexpr int NW = WI * WJ;
     static constexpr bool TURNS = NW == 8, LOADERS = !TURNS;        // two waves a SIMD, one of either group; as many waves again that load (see run)
     static constexpr int NT = NW * 64 * (LOADERS ? 2 : 1);
@@ -73,6 +73,7 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
     static_assert(NW % 2 == 0 && NSA * NW * 1024 == A_BYTES && NL * NW * 1024 == STAGE, "every wave loads the same number of slabs");
     static_assert(TURNS || NW == 4, "one or two multiplying waves a SIMD");
     static_assert(!TRIPLE || (LOADERS && NSA % 3 == 0 && NSB % 3 == 0), "loads of three slabs, by waves of their own");
+    static_assert(!PARTS || LOADERS, "registers for a second sum");
     typedef f32x16 Acc[FI][FJ];
 
     static constexpr unsigned kOOB = 0x80000000u;       // beyond any buffer of 2^31 - 1 bytes
@@ -217,8 +218,10 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
     // Adds to acc the products of rows i0.. of A and j0.. of B over k in [kb, ke), kb a multiple of 64.  (Several planes: one pair, and operands
     // with k contiguous are zero behind ke up to a multiple of 32.)  mask (MASKED): bit k & 63
     // of word k >> 6 is set where A's row k counts.  Ends with every load landed and all waves past their last LDS read.
+    // PARTS: every `every` k-tiles (0: never) acc is added to a sum of its own and starts from zero again, as a product that is added to a
+    // long sum is cut to that sum's last bit.
     __device__ static __forceinline__ void run(const GemmOperand& A, const GemmOperand& B, const GemmPairs& pairs, int i0, int j0, int kb, int ke,
-                                               GemmMask mask, unsigned char* smem, Acc& acc) {
+                                               GemmMask mask, unsigned char* smem, Acc& acc, int every = 0) {
         const int tid = threadIdx.x, lane = tid & 63, number = __builtin_amdgcn_readfirstlane(tid >> 6);
         const bool loader = LOADERS && number >= NW;
         const int wave = loader ? number - NW : number;
@@ -404,7 +407,27 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
             each(std::make_integer_sequence<int, NR>(), [&](auto q) __attribute__((always_inline)) { fragment(k0, q, 0u); });
             arrived(0);
             unsigned st = 0;
-            int sn = 0;
+            int sn = 0, left = every;
+            Acc whole;
+            auto join = [&](bool last) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+#pragma unroll
+                    for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            whole[i][j][e] += acc[i][j][e];
+                            acc[i][j][e] = last ? whole[i][j][e] : 0.f;
+                        }
+            };
+            if constexpr (PARTS) {
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+#pragma unroll
+                    for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) whole[i][j][e] = 0.f;
+            }
             for (int t = 0; t < total; ++t) {
                 step(k1, st, 0);
                 if constexpr (PL == 1) {
@@ -417,7 +440,10 @@ template <class E, bool AKR, bool BKR, int WI, int WJ, int FI, int FJ, int STAGE
                 if (++sn == STAGES) sn = 0;
                 st = (unsigned)(sn * STAGE);
                 step(k0, st, 1);                               // (behind the last k-tile it reads zeros, not used)
+                if constexpr (PARTS)
+                    if (--left == 0) { join(false); left = every; }
             }
+            if constexpr (PARTS) join(true);
         }
         wait_vmcnt<0>();
         asm volatile("" ::: "memory");

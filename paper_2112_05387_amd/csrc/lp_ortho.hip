@@ -307,7 +307,7 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
         for (int j = 0; j < T::TJ / 32; ++j)
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
-    if constexpr (MODE == NS_GRAM) T::run(ox, ox, one, i0, j0, 0, W.c, (GemmMask)nullptr, smem, acc);
+    if constexpr (MODE == NS_GRAM) T::run(ox, ox, one, i0, j0, 0, W.c, (GemmMask)nullptr, smem, acc, W.thin() ? kNsPart : 0);
     else if constexpr (MODE == NS_POLY) T::run(os, os, one, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
     else T::run(ox, ob, one, i0, j0, 0, r, (GemmMask)nullptr, smem, acc);
 
@@ -414,8 +414,8 @@ template <class T, int MODE> __global__ __launch_bounds__(T::NT, 2) void ns_gemm
 
 template <bool AKR> using NBig = GemmTile<f16_t, AKR, false, 2, 4, 4, 2, 2, false, 2>;
 template <bool AKR> using NWide = GemmTile<f16_t, AKR, false, 4, 2, 2, 5, 2, false, 2>;
-template <bool AKR> using NMid = GemmTile<f16_t, AKR, false, 2, 2, 2, 2, 4, false, 2>;
-template <bool AKR> using NSmall = GemmTile<f16_t, AKR, false, 2, 2, 1, 1, 4, false, 2>;
+template <bool AKR, int MODE> using NMid = GemmTile<f16_t, AKR, false, 2, 2, 2, 2, 4, false, 2, MODE == NS_GRAM>;
+template <bool AKR, int MODE> using NSmall = GemmTile<f16_t, AKR, false, 2, 2, 1, 1, 4, false, 2, MODE == NS_GRAM>;
 
 template <class T, int MODE> hipError_t launch_gemm(const NsArgs& a, hipStream_t s) {
     static OncePerDevice once;
@@ -432,8 +432,8 @@ template <bool AKR, int MODE> hipError_t launch_mode(const NsArgs& a, int cfg, h
         if (cfg == NT_256x320) return launch_gemm<NWide<AKR>, MODE>(a, s);
     switch (cfg) {
         case NT_256: return launch_gemm<NBig<AKR>, MODE>(a, s);
-        case NT_128: return launch_gemm<NMid<AKR>, MODE>(a, s);
-        default: return launch_gemm<NSmall<AKR>, MODE>(a, s);
+        case NT_128: return launch_gemm<NMid<AKR, MODE>, MODE>(a, s);
+        default: return launch_gemm<NSmall<AKR, MODE>, MODE>(a, s);
     }
 }
 
