@@ -3,11 +3,11 @@
 //   l_nv = sum_c x_nc w_vc + b_v,   lse_n = log sum_v exp l_nv,   loss_n = lse_n - l_n,y(n)
 //   d_nv = (exp(l_nv - lse_n) - [v = y(n)]) / count,   dX = d W,   dW = d^T X,   db_v = sum_n d_nv
 //
-// Four products, each on the matrix cores with what follows it as its epilogue.  Forward: l = X W^T, of which a workgroup keeps the
+// Products on the matrix cores, each with what follows it as its epilogue.  Forward: l = X W^T, of which a workgroup keeps the
 // maximum and the sum of exponentials of its classes for every row (the statistics of all tiles are joined by a small kernel; the label's
 // class is kept apart until then).  Backward: the same product once more, whose epilogue turns a tile into
-// probabilities; they go to memory, piece of the classes by piece, and are read from there by the two gradient products.  Keeping
-// the logits would save one product of four and cost 4 bytes a logit.
+// probabilities; they go to memory, all at once or piece of the classes by piece, and are read from there by the two gradient products.
+// Keeping the logits would save one product (of seven in bf16: dW takes three, dX two) and cost 4 bytes a logit.
 //
 // Precision.  bf16: products of bf16 are exact, sums are fp32.  The probabilities are kept as three bf16 (24 bits), all of which dW and
 // the bias read, which are fp32 (with two dW is off by 1.8e-6, with three by the 2e-7 of its sums).  dX, rounded to bf16 itself,
@@ -835,7 +835,7 @@ hipError_t launch_ce_slices(const CeLogits& a, int slices, int cfg, hipStream_t 
     }
 }
 hipError_t launch_ce_rows(const CeRows& a, hipStream_t s) {
-    // (a wave a row 15 us for 8192 rows of 256 parts and 11 for 10000 of eight; four waves a row 5 for 777)
+    // (a wave a row 9 us for 8192 rows of 256 parts and for 10000 of 172; four waves a row 5 for 777)
     const bool wide = a.slices || a.N < 2048;
     const int blocks = wide ? a.N : (a.N + 3) / 4;
     // counting workgroups costs 12 ns each (64 rows: 6.3 us against 5.6 and 1.7 of a launch for the sum; 777: 13.8 against 5.1 and 4.6)

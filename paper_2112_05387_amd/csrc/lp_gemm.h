@@ -18,9 +18,9 @@
 // A k-tile is 128 (192) bytes of a row long.  Eight waves (256 x 256 and 256 x 320, one workgroup a compute unit) are two groups that
 // take turns, the loads of the next k-tile between their products.  Four waves (tiles of 128 and less) have four more beside them
 // that only load; one barrier a k-tile, ahead of the products of its last 16 k, both frees its stage and shows the next.
-// What bounds it: power.  8192 x 8192 x 4096 in bf16 1105 (k contiguous), 1220 (one operand with rows along k), 1240 TFLOP/s
-// (both), DUAL 1440 of its three products, at 1.6 to 1.9 GHz; without the loads 1270 to 1570, the matrix cores busy for 85 % of
-// the clocks.  All eight waves in step: 1013, 1128, 1203, 1370; half as many waves of 128 x 128 each, a third fewer LDS
+// What bounds it: power, and the loads.  8192 x 8192 x 4096 in bf16 1105 (k contiguous), 1220 (one operand with rows along k), 1240
+// TFLOP/s (both), DUAL 1440 of its three products, at 1.6 to 1.9 GHz, the matrix cores busy for 60 to 70 % of the clocks; without the
+// loads 1270 to 1570 and 85 %.  All eight waves in step: 1013, 1128, 1203, 1370; half as many waves of 128 x 128 each, a third fewer LDS
 // reads: 5 % less than that; fragments two k-steps ahead: the same.  DUAL in tiles of 128 x 128 over 8192, 64 and 256
 // workgroups: 145 and 186 us without loading waves, 118 and 173 with.  TRIPLE: 73623 x 8716 over 633 1170 TFLOP/s of its six
 // products, with the planes apart in 256 x 256 tiles 810; 230 workgroups of 128 x 128 over 1781 64 us, with planes apart 116.
