@@ -192,3 +192,60 @@ def test_infinities_stay_in_their_row(n, c, v, dtype):
     rest[5:8] = False
     assert bool(got["lse"][~rest].isnan().all()) and bool(got["row_loss"][~rest].isnan().all()) and bool(got["dfeatures"][~rest].isnan().any(1).all())
     _compare({k: got[k][rest] for k in ("lse", "row_loss", "dfeatures")}, {k: (want[k][0][rest], want[k][1][rest]) for k in ("lse", "row_loss", "dfeatures")}, "beside infinities")
+
+
+@pytest.mark.parametrize("dtype,n,c,v", [("bf16", 950, 8, 94619), ("f32", 6, 8, 1059975)])
+def test_pieces_one_gradient_at_a_time_and_replayed(dtype, n, c, v):
+    """Each gradient alone gives the bits that it has beside the others, and so does a captured pass, replayed with eager ones between."""
+    import torch
+    from paper_2112_05387_amd import binding as B
+    from paper_2112_05387_amd import ops
+    d = B.lp_linear_ce_desc(n, c, v, B.LP_BF16 if dtype == "bf16" else B.LP_F32, 0, 0, 0)
+    assert B.lp_debug_linear_ce_plan(d, True)[2] > 1
+    x, w, b, y = _inputs(n, c, v, dtype, ignored=0.1, seed=3)
+    x = (x.float() + 16 * w.float()[y.clamp(min=0).long()] * (torch.arange(n, device="cuda") % 2 == 0)[:, None]).to(x.dtype)      # half of the rows all but certain
+    lse = ops.linear_ce_forward(x, w, y, bias=b)[2]
+    both = ops.linear_ce_backward(x, w, y, lse, bias=b)
+    size = B.lp_linear_ce_workspace_bytes(d, True)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    for k, t in enumerate(both):
+        out = torch.full_like(t, 7.0)
+        ws.fill_(255)
+        B.lp_linear_ce_backward(d, torch.cuda.current_stream().cuda_stream, x.data_ptr(), w.data_ptr(), b.data_ptr(), y.data_ptr(), lse.data_ptr(), 1.0,
+                                *[out.data_ptr() if k == i else None for i in range(3)], ws.data_ptr(), size)
+        assert torch.equal(out, t), k
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = ops.linear_ce_backward(x, w, y, lse, bias=b)
+    for turn in range(3):
+        x.copy_(_inputs(n, c, v, dtype, ignored=0.1, seed=3 + turn)[0])
+        lse.copy_(ops.linear_ce_forward(x, w, y, bias=b)[2])
+        graph.replay()
+        eager = ops.linear_ce_backward(x, w, y, lse, bias=b)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, e) for a, e in zip(out, eager)), turn
+
+
+@pytest.mark.parametrize("dtype,n,c,v", [("bf16", 700, 64, 9000), ("f32", 300, 40, 9000), ("bf16", 64, 512, 1000)])
+def test_whatever_the_workspace_holds(dtype, n, c, v):
+    """Nothing is read from the workspace that the call has not written: the same bits over zeros and over NaN."""
+    import torch
+    from paper_2112_05387_amd import binding as B
+    x, w, b, y = _inputs(n, c, v, dtype, ignored=0.2, seed=5)
+    d = B.lp_linear_ce_desc(n, c, v, B.LP_BF16 if dtype == "bf16" else B.LP_F32, 0, 0, 0)
+    results = []
+    for fill in (0, 255):
+        loss, rows, lse = (torch.empty(k, device="cuda") for k in (1, n, n))
+        dx, dw, db = torch.empty_like(x), torch.empty(v, c, device="cuda"), torch.empty(v, device="cuda")
+        s = torch.cuda.current_stream().cuda_stream
+        for backward in (False, True):
+            ws = torch.full((B.lp_linear_ce_workspace_bytes(d, backward),), fill, dtype=torch.uint8, device="cuda")
+            if backward:
+                B.lp_linear_ce_backward(d, s, x.data_ptr(), w.data_ptr(), b.data_ptr(), y.data_ptr(), lse.data_ptr(), 1.0, dx.data_ptr(), dw.data_ptr(), db.data_ptr(), ws.data_ptr(), ws.numel())
+            else:
+                B.lp_linear_ce_forward(d, s, x.data_ptr(), w.data_ptr(), b.data_ptr(), y.data_ptr(), loss.data_ptr(), rows.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel())
+            torch.cuda.synchronize()
+        results.append((loss, rows, lse, dx, dw, db))
+    for a, e in zip(*results):
+        assert torch.equal(a, e) and bool(a.isfinite().all())
