@@ -12,6 +12,15 @@ def _dev():
     return torch.device("cuda:0")
 
 
+def _check_like(name, tensors, grads, mask):
+    """Tensors laid out like the gradients, for every set that `mask` selects: the library reads their addresses and knows no sizes."""
+    if tensors is None or len(tensors) < len(grads):
+        raise ValueError(f"{name}: {'none' if tensors is None else len(tensors)} of {len(grads)} tensors, one for every parameter set")
+    for k, (t, g) in enumerate(zip(tensors, grads)):
+        if (mask >> k) & 1 and (t is None or t.dtype != torch.float32 or not t.is_contiguous() or t.device != g.device or t.numel() < g.numel()):
+            raise ValueError(f"{name}[{k}]: expected {g.numel()} float32 on {g.device}, contiguous, got " + ("None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}"))
+
+
 class LocalStep:
     """Owns the net handle, workspace, packed parameters and interface tensors of one configuration.
 
@@ -228,14 +237,17 @@ class LocalStep:
                     mask=None, head=False, aux=False):
         """Update by orthogonalised momentum (lp_muon_update) of the modules in `mask` (default all), or of the AuxNets: filters
         orthogonalised, batch-norm tensors and the head (its weight too unless `head`) by momentum with rest_lr (default lr).
-        velocity, master: lists of tensors laid out like the gradients.  The workspace is torch's, on the current stream."""
+        velocity, master: lists of fp32 tensors laid out like the gradients, one for every set (None for those not in `mask`).  The workspace is torch's, on the current stream."""
         m = ((1 << (self.K - 1)) - 1 if aux else self._mask(None)) if mask is None else mask
+        grads = self.daux_params if aux else self.dparams
+        _check_like("velocity", velocity, grads, m)
+        if master is not None:
+            _check_like("master", master, grads, m)
         opts = B.lp_muon_opts(lr, momentum, weight_decay, lr if rest_lr is None else rest_lr, int(nesterov), steps)
         size = B.lp_muon_workspace_bytes(self.net, aux, m, head)
         ws = torch.empty(size, dtype=torch.uint8, device=self.dev)
         B.lp_muon_update(self.net, self._stream(), aux, m, head, self._p(self.aux_params if aux else self.params),
-                         self._p(self.daux_params if aux else self.dparams), self._p(velocity),
-                         None if master is None else self._p(master), opts, ws.data_ptr(), size)
+                         self._p(grads), self._p(velocity), None if master is None else self._p(master), opts, ws.data_ptr(), size)
 
     def set_fused_update(self, on, lr=0.0, momentum=0.0, weight_decay=0.0, velocity=None, master=None):
         """Parameter update inside the backward pass (in the epilogues of the filter-gradient kernels); `velocity` and
